@@ -14,8 +14,11 @@
  * (fd_attn_draft_verify, fd_verify_accept, fd_kv_commit) and the steps next to them: the
  * all-hypotheses form of the attention and the branch selection (Eq. 2), the draft-side
  * tail (Eq. 4, Eq. 5), verification by sampling at temperature > 0 (Sec. 3), the KV
- * append, and a whole step from host buffers.  Everything runs in hand-written CUDA
- * kernels; there is no CPU fallback.
+ * append, and a whole step from host buffers.  Around them stand what a serving loop needs
+ * next: pages out of a free list (fd_kv_reserve), norm, rotation and append in one pass
+ * (fd_qk_norm_rope_append), and a cache held in 4 bits with the attention that reads it
+ * (fd_kv_append_fp4, fd_kv_read_fp4, fd_attn_draft_verify_fp4).  Everything runs in
+ * hand-written CUDA kernels; there is no CPU fallback.
  *
  * Conventions (all entry points)
  *   - "device pointer": memory on the GPU that is current when fd_create() ran, owned
@@ -65,7 +68,20 @@ enum {
                                  page table, or row totals that do not match the call's row count */
     FD_DEV_BAD_PAGE = 2,      /* a page id needed by a sequence is outside [0, num_pages) */
     FD_DEV_TIMEOUT = 4,       /* a bounded device-side wait ran out; the kernel returned early */
-    FD_DEV_BAD_ACCEPT = 8     /* fd_kv_commit: accepted_len[b] >= q_lens[b] */
+    FD_DEV_BAD_ACCEPT = 8,    /* fd_kv_commit: accepted_len[b] >= q_lens[b] */
+    FD_DEV_NO_PAGES = 16      /* fd_kv_reserve: the free list holds fewer pages than the query blocks need */
+};
+
+/* How a paged KV cache holds its values (fd_qk_norm_rope_append). */
+enum {
+    FD_KV_BF16 = 0,           /* [num_pages, 2, Hkv, P, d] bf16, the cache of fd_attn_draft_verify */
+    FD_KV_FP4 = 1             /* 4-bit pages, the cache of fd_attn_draft_verify_fp4 (see there) */
+};
+
+/* Which two elements of a head fd_qk_norm_rope_append rotates together (R = rot_dim). */
+enum {
+    FD_ROPE_HALVES = 0,       /* (i, i + R / 2) for i < R / 2 */
+    FD_ROPE_ADJACENT = 1      /* (2 i, 2 i + 1) */
 };
 
 /* Which attention kernel fd_attn_draft_verify launches. */
@@ -276,6 +292,121 @@ fd_status fd_attn_draft_verify_blocks(fd_ctx* ctx, int batch, int total_q_rows,
                                       const int32_t* page_table, const int32_t* prefix_lens,
                                       const int32_t* q_lens, const int32_t* n_mask,
                                       const int32_t* n_blocks, void* out, void* stream);
+
+/*
+ * Pages for the query blocks of a step, and where each of its rows goes: the counterpart of fd_kv_commit, which
+ * releases pages.  (The paper describes no page management; the bookkeeping implemented here mirrors the commit's.)
+ * The free list is a stack of page ids, free_pages[0 .. n_free).  First the n_freed ids the last commit released
+ * are pushed onto it (freed_pages / n_freed exactly as fd_kv_commit wrote them; both NULL: nothing to push).  Then,
+ * for b ascending:
+ *
+ *     for p = ceil(n_b / P) .. ceil((n_b + Lq_b) / P) - 1 ascending:
+ *         page_table[b][p] = the id popped from the top of the free list
+ *
+ * (what was in those entries is not looked at: after a commit they hold -1), and for row i of sequence b, at
+ * logical position j = n_b + i:
+ *
+ *     slot_map[row0_b + i]  = page_table[b][j / P] * P + j % P
+ *     positions[row0_b + i] = j                         for a candidate row (i < C_b)
+ *                           = n_b + r + 1 + u           for token u of the mask block of hypothesis r (r = C_b - nb_b + g
+ *                                                       for block g, as in fd_attn_draft_verify_blocks): the branch
+ *                                                       continues behind the r drafts it presumes accepted
+ *
+ *   total_q_rows    T; must equal sum_b q_lens[b]
+ *   page_table      device, [B, max_pages_per_seq] int32, in/out
+ *   prefix_lens, q_lens, n_mask   device, [B] int32;  n_blocks   device, [B] int32 or NULL (one block each)
+ *   freed_pages     device, int32, read only;  n_freed   device, [1] int32
+ *   free_pages      device, [num_pages] int32, in/out
+ *   n_free          device, [1] int32: ids on the free list before the call
+ *   n_free_out      device, [1] int32: ids on it after the call; may be n_free itself
+ *   num_pages       size of the page pool, num_pages * P < 2^31
+ *   slot_map, positions   device, [T] int32, overwritten
+ *
+ * Fewer ids on the list than pages needed: nothing is popped and the table stays as it is, every slot is -1, the
+ * positions are written (FD_DEV_NO_PAGES; the pushed ids are on the list).  Inconsistent lengths, or a list longer
+ * than the pool: nothing is pushed or popped, every slot and position is -1, n_free_out = n_free
+ * (FD_DEV_BAD_LENGTHS).  A page id outside the pool: its entry becomes -1 if it was popped, and the slots that need
+ * it are -1 (FD_DEV_BAD_PAGE).  n_freed ids are pushed once per call: pass a commit's output to one call only.
+ */
+fd_status fd_kv_reserve(fd_ctx* ctx, int batch, int total_q_rows, int32_t* page_table, const int32_t* prefix_lens,
+                        const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks,
+                        const int32_t* freed_pages, const int32_t* n_freed, int32_t* free_pages,
+                        const int32_t* n_free, int32_t* n_free_out, int num_pages, int32_t* slot_map,
+                        int32_t* positions, void* stream);
+
+/*
+ * From the projection to the cache in one pass (the target model's own step between its QKV projection and
+ * fd_attn_draft_verify; the paper's target models norm each query and key head and rotate it by its position).
+ * Row t of qkv holds Hq query heads, then Hkv key heads, then Hkv value heads of d elements.  For a head x of q or k:
+ *
+ *     y = x / sqrt(mean_i x_i^2 + eps) * weight                          (weight NULL: y = x)
+ *     for each pair (a, b) of FD_ROPE_* among the first R = rot_dim elements, pair number i, with c = cos_sin[pos][i],
+ *     s = cos_sin[pos][R / 2 + i]:        y_a, y_b = y_a c - y_b s,  y_b c + y_a s
+ *
+ * with pos = positions[t].  q goes to q_out[t]; k and v go to the cache slot slot_map[t] (page slot / P, token slot % P).
+ *
+ *   total_q_rows    T >= 0; at most max_batch * max_q_len
+ *   qkv             device, bf16, 16-byte aligned; row t starts at element t * row_stride (a multiple of 8, at least
+ *                   (Hq + 2 Hkv) * d)
+ *   q_weight, k_weight   device, [d] bf16, 16-byte aligned, or NULL: no norm
+ *   eps             >= 0
+ *   cos_sin         device, [max_positions, rot_dim] fp32, 16-byte aligned: cosines of a row, then its sines
+ *   rot_dim         R: a multiple of 16, 0 <= R <= d (0: no rotation, cos_sin and positions may be NULL)
+ *   rope_style      FD_ROPE_HALVES or FD_ROPE_ADJACENT
+ *   positions, slot_map   device, [T] int32 (fd_kv_reserve writes both)
+ *   q_out           device, [T, Hq, d] bf16, 16-byte aligned, does not overlap qkv
+ *   kv_cache        device, the cache of kv_format: bf16 pages (128-byte aligned) or 4-bit pages (16-byte aligned)
+ *   kv_format       FD_KV_BF16 or FD_KV_FP4
+ *   k_scale, v_scale   FD_KV_FP4: as in fd_kv_append_fp4; FD_KV_BF16: not used
+ *
+ * A row whose slot is negative is padding: nothing is written for it.  A slot beyond the pool: k and v of the row are
+ * not written (FD_DEV_BAD_PAGE).  A position outside [0, max_positions): nothing is written for the row
+ * (FD_DEV_BAD_LENGTHS).  Two rows with the same slot leave one of the two there.
+ * Arithmetic: fp32 throughout, each result rounded once, to bf16 or to 4 bits.
+ */
+fd_status fd_qk_norm_rope_append(fd_ctx* ctx, int total_q_rows, const void* qkv, int64_t row_stride,
+                                 const void* q_weight, const void* k_weight, float eps, const float* cos_sin,
+                                 int max_positions, int rot_dim, int rope_style, const int32_t* positions,
+                                 const int32_t* slot_map, void* q_out, void* kv_cache, int num_pages, int kv_format,
+                                 float k_scale, float v_scale, void* stream);
+
+/*
+ * A KV cache held in 4 bits: attention over it, and the ways into and out of it.  At long context the step is bound by the
+ * bytes of the cache; these pages are 9/32 the size of bf16 pages.  (The paper keeps its cache in bf16; this is the
+ * library's own.)  Every 16 consecutive elements of a head's row share an e4m3 scale and are held as e2m1 codes
+ * (bit 3 the sign; 0..7 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6); all of K is scaled by k_scale on top, all of V by v_scale
+ * (positive, finite; the same numbers in every call on a cache):
+ *
+ *     value = code * scale * k_scale
+ *     scale = the e4m3 number nearest to max_i |x_i / k_scale| / 6, at most 448         (nearest, ties to even)
+ *     code  = the e2m1 number whose multiple of the scale is nearest to x / k_scale      (nearest, ties to even; 6 at most)
+ *
+ * A NaN is held as 0, an infinity as the largest value of its group's scale.  Zero scale: all codes of the group are 0.
+ *
+ *   cache layout    [num_pages, Hkv, 2, P * (d / 2 + d / 16)] bytes, 16-byte aligned: for each page and kv-head K then V,
+ *                   each as [P][d / 2] bytes of codes (element 2 i in the low half of byte i) followed by [P][d / 16]
+ *                   bytes of scales
+ *
+ * fd_kv_append_fp4 is fd_kv_append for it, fd_kv_read_fp4 the reverse: k_out / v_out [T, Hkv, d] bf16 get the values held
+ * at positions n_b .. n_b + Lq_b - 1 (any range of the sequence: pass the range's start as prefix_lens), rounded to bf16.
+ * A sequence that is skipped, or a slot whose page id is outside the pool, leaves its rows of k_out / v_out as zeros.
+ * Arguments and device-detected errors are fd_kv_append's.
+ *
+ * fd_attn_draft_verify_fp4 is fd_attn_draft_verify_blocks for it: same arguments (n_blocks may be NULL), same mask, same
+ * errors, same forms (FD_TC_*), pinned plans and overlap of consecutive calls included.  Slots no valid token owns may hold
+ * any bit pattern.  Arithmetic: the values of the cache enter exactly, q is held in at least as many bits as bf16
+ * relative to its row's largest element, the softmax weights in 11 bits, sums in fp32; bf16 output.
+ */
+fd_status fd_kv_append_fp4(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
+                           void* kv_cache, int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
+                           const int32_t* q_lens, float k_scale, float v_scale, void* stream);
+fd_status fd_kv_read_fp4(fd_ctx* ctx, int batch, int total_q_rows, const void* kv_cache, int num_pages,
+                         const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens, float k_scale,
+                         float v_scale, void* k_out, void* v_out, void* stream);
+fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, const void* q, const void* kv_cache,
+                                   int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
+                                   const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks,
+                                   float k_scale, float v_scale, void* out, void* stream);
 
 /*
  * Draft-side tail of the step (Sec. 4.2, Eq. 4; Sec. 4.3 "Selective verification", Eq. 5).  One row of

@@ -22,10 +22,14 @@ FD_DEV_BAD_LENGTHS, FD_DEV_BAD_PAGE, FD_DEV_TIMEOUT, FD_DEV_BAD_ACCEPT = 1, 2, 4
 FD_ATTN_AUTO, FD_ATTN_SIMT, FD_ATTN_TCGEN05 = 0, 1, 2
 FD_ATTN_TCGEN05_PLANNED, FD_ATTN_TCGEN05_SELF_PLANNED = 3, 4
 FD_TC_PLANNED, FD_TC_SELF_PLANNED, FD_TC_CLUSTER = 0, 1, 2
+FD_DEV_NO_PAGES = 16
+FD_KV_BF16, FD_KV_FP4 = 0, 1
+FD_ROPE_HALVES, FD_ROPE_ADJACENT = 0, 1
 
 EXPORTS = ["fd_create", "fd_destroy", "fd_attn_draft_verify", "fd_verify_accept", "fd_kv_commit",
            "fd_last_device_status", "fd_attn_path", "fd_attn_last_mode", "fd_launch_count", "fd_status_string",
-           "fd_verify_accept_static", "fd_host_reserve", "fd_step_host", "fd_step_host_append", "fd_step_device", "fd_selftest_wait_timeout", "fd_attn_draft_verify_blocks", "fd_select_branch", "fd_draft_select", "fd_kv_append", "fd_plan_pin", "fd_plan_unpin", "fd_calls_back_to_back", "fd_verify_accept_sample", "fd_plan_ranges_host"]
+           "fd_verify_accept_static", "fd_host_reserve", "fd_step_host", "fd_step_host_append", "fd_step_device", "fd_selftest_wait_timeout", "fd_attn_draft_verify_blocks", "fd_select_branch", "fd_draft_select", "fd_kv_append", "fd_plan_pin", "fd_plan_unpin", "fd_calls_back_to_back", "fd_verify_accept_sample", "fd_plan_ranges_host",
+           "fd_kv_reserve", "fd_qk_norm_rope_append", "fd_kv_append_fp4", "fd_kv_read_fp4", "fd_attn_draft_verify_fp4"]
 
 
 class fd_config(ctypes.Structure):
@@ -76,6 +80,12 @@ def load() -> ctypes.CDLL:
         lib.fd_draft_select.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
         lib.fd_step_host.argtypes = [vp, ci, ci, ci, ci, ctypes.POINTER(vp), ci] + [vp] * 14
         lib.fd_step_host_append.argtypes = [vp, ci, ci, ci, ci, ctypes.POINTER(vp), ci] + [vp] * 16
+        cf = ctypes.c_float
+        lib.fd_kv_reserve.argtypes = [vp, ci, ci] + [vp] * 10 + [ci, vp, vp, vp]
+        lib.fd_qk_norm_rope_append.argtypes = [vp, ci, vp, ctypes.c_int64, vp, vp, cf, vp, ci, ci, ci, vp, vp, vp, vp, ci, ci, cf, cf, vp]
+        lib.fd_kv_append_fp4.argtypes = [vp, ci, ci, vp, vp, vp, ci, vp, vp, vp, cf, cf, vp]
+        lib.fd_kv_read_fp4.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, cf, cf, vp, vp, vp]
+        lib.fd_attn_draft_verify_fp4.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, cf, cf, vp, vp]
         lib.fd_last_device_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), vp]
         lib.fd_attn_path.argtypes = [vp]
         lib.fd_attn_last_mode.argtypes = [vp]
@@ -178,6 +188,50 @@ def fd_kv_append(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, pa
     code = load().fd_kv_append(ctx, batch, total_q_rows, _ptr(k_new), _ptr(v_new), _ptr(kv_cache), num_pages,
                                _ptr(page_table), _ptr(prefix_lens), _ptr(q_lens), _stream(stream))
     return _check("fd_kv_append", code, raise_on_error)
+
+
+def fd_kv_reserve(ctx, batch, total_q_rows, page_table, prefix_lens, q_lens, n_mask, n_blocks, freed_pages, n_freed, free_pages,
+                  n_free, n_free_out, num_pages, slot_map, positions, stream=None, raise_on_error=True) -> int:
+    code = load().fd_kv_reserve(ctx, batch, total_q_rows, _ptr(page_table), _ptr(prefix_lens), _ptr(q_lens), _ptr(n_mask),
+                                _ptr(n_blocks), _ptr(freed_pages), _ptr(n_freed), _ptr(free_pages), _ptr(n_free), _ptr(n_free_out),
+                                num_pages, _ptr(slot_map), _ptr(positions), _stream(stream))
+    return _check("fd_kv_reserve", code, raise_on_error)
+
+
+def fd_qk_norm_rope_append(ctx, total_q_rows, qkv, row_stride, q_weight, k_weight, eps, cos_sin, max_positions, rot_dim, rope_style,
+                           positions, slot_map, q_out, kv_cache, num_pages, kv_format=FD_KV_BF16, k_scale=1.0, v_scale=1.0, stream=None,
+                           raise_on_error=True) -> int:
+    code = load().fd_qk_norm_rope_append(ctx, total_q_rows, _ptr(qkv), row_stride, _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos_sin),
+                                         max_positions, rot_dim, rope_style, _ptr(positions), _ptr(slot_map), _ptr(q_out),
+                                         _ptr(kv_cache), num_pages, kv_format, k_scale, v_scale, _stream(stream))
+    return _check("fd_qk_norm_rope_append", code, raise_on_error)
+
+
+def fd_kv_append_fp4(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale=1.0,
+                     v_scale=1.0, stream=None, raise_on_error=True) -> int:
+    code = load().fd_kv_append_fp4(ctx, batch, total_q_rows, _ptr(k_new), _ptr(v_new), _ptr(kv_cache), num_pages, _ptr(page_table),
+                                   _ptr(prefix_lens), _ptr(q_lens), k_scale, v_scale, _stream(stream))
+    return _check("fd_kv_append_fp4", code, raise_on_error)
+
+
+def fd_kv_read_fp4(ctx, batch, total_q_rows, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale, v_scale, k_out, v_out,
+                   stream=None, raise_on_error=True) -> int:
+    code = load().fd_kv_read_fp4(ctx, batch, total_q_rows, _ptr(kv_cache), num_pages, _ptr(page_table), _ptr(prefix_lens), _ptr(q_lens),
+                                 k_scale, v_scale, _ptr(k_out), _ptr(v_out), _stream(stream))
+    return _check("fd_kv_read_fp4", code, raise_on_error)
+
+
+def fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, q, kv_cache, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
+                             k_scale, v_scale, out, stream=None, raise_on_error=True) -> int:
+    code = load().fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, _ptr(q), _ptr(kv_cache), num_pages, _ptr(page_table),
+                                           _ptr(prefix_lens), _ptr(q_lens), _ptr(n_mask), _ptr(n_blocks), k_scale, v_scale, _ptr(out),
+                                           _stream(stream))
+    return _check("fd_attn_draft_verify_fp4", code, raise_on_error)
+
+
+def fd_kv_fp4_page_bytes(head_dim: int, page_size: int = 16) -> int:
+    """Bytes that one page of one kv-head takes in a 4-bit cache, for K or for V: codes, then scales."""
+    return page_size * (head_dim // 2 + head_dim // 16)
 
 
 def fd_draft_select(ctx, batch, total_mask_rows, max_blocks, draft_logits, bias, n_mask, n_blocks, threshold, mask_tokens,

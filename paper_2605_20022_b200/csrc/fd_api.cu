@@ -5,6 +5,7 @@
 #include <utility>
 #include <new>
 
+#include "fd_fp4.cuh"
 #include "fd_internal.cuh"
 
 struct fd_ctx {
@@ -33,6 +34,7 @@ struct fd_ctx {
     int4* sv_seq;
     float* sv_chunk_w;
     unsigned char* sv_flags;
+    unsigned int* rs_ticket;     // page reservation
     int* status;
     int max_rows;      // capacity of keys
     int max_rb;        // capacity of the row-block arrays of the plan
@@ -96,8 +98,16 @@ static fd::AttnParams attn_params(fd_ctx* c, int batch, int total_q_rows, const 
     p.q_box_t = fd::q_box_rows(p.G);
     p.piece_cost = c->attn_path == FD_ATTN_SIMT ? 0 : FD_PIECE_COST;
     p.min_range_tiles = c->attn_path == FD_ATTN_SIMT ? 1 : FD_MIN_RANGE_TILES;
+    p.out_scale = 1.f;
     return p;
 }
+
+// A scale of a 4-bit cache: positive and finite.
+static bool good_scale(float s) { return s > 0.f && s <= 3.4028234e38f; }
+
+static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, bool fp4, float k_scale, float v_scale,
+                           int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
+                           const int32_t* n_mask, const int32_t* n_blocks, void* out, void* stream);
 
 
 extern "C" {
@@ -156,7 +166,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->attn_path = (cfg->attn_path == FD_ATTN_SIMT || !tc_ok) ? FD_ATTN_SIMT : FD_ATTN_TCGEN05;
     // SIMT kernel: two 74 KB CTAs fit an SM; tensor-core kernel: one persistent CTA per SM
     c->n_ctas = c->attn_path == FD_ATTN_SIMT ? 2 * c->n_sms : c->n_sms;
-    if (c->attn_path == FD_ATTN_SIMT && fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
+    if (fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
 
     const int B = cfg->max_batch, d = cfg->head_dim;
     const size_t slots = 2 * (size_t)c->n_ctas;
@@ -194,6 +204,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     const size_t o_svs = take((size_t)B * sizeof(int4));
     const size_t o_svw = take((size_t)B * ds_chunks * sizeof(float));
     const size_t o_svf = take((size_t)c->max_rows);
+    const size_t o_rst = take(sizeof(unsigned int));
     const size_t o_stat = take(sizeof(int));
     if (cudaMalloc(&c->pool, off) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_WORKSPACE; }
     if (cudaMemset(c->pool, 0, off) != cudaSuccess) { cudaFree(c->pool); delete c; return FD_ERR_CUDA; }
@@ -223,6 +234,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->sv_seq = reinterpret_cast<int4*>(c->pool + o_svs);
     c->sv_chunk_w = reinterpret_cast<float*>(c->pool + o_svw);
     c->sv_flags = c->pool + o_svf;
+    c->rs_ticket = reinterpret_cast<unsigned int*>(c->pool + o_rst);
     c->status = reinterpret_cast<int*>(c->pool + o_stat);
     *out = c;
     return FD_OK;
@@ -435,83 +447,17 @@ fd_status fd_attn_draft_verify_blocks(fd_ctx* c, int batch, int total_q_rows, co
                                       int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
                                       const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks,
                                       void* out, void* stream) {
-    if (!c || batch < 0 || total_q_rows < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
-    if (batch > c->cfg.max_batch || (long long)total_q_rows > (long long)batch * c->cfg.max_q_len)
-        return FD_ERR_INVALID_ARG;
-    if (batch == 0) return total_q_rows == 0 ? FD_OK : FD_ERR_INVALID_ARG;
-    if (!page_table || !prefix_lens || !q_lens || !n_mask) return FD_ERR_INVALID_ARG;
-    if (total_q_rows > 0 && (!q || !out)) return FD_ERR_INVALID_ARG;
-    if (!kv_cache || num_pages == 0) return FD_ERR_INVALID_ARG;
-    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(kv_cache, 128) || !aligned(page_table, 4)) return FD_ERR_INVALID_ARG;
-    if ((long long)num_pages * 2 * c->cfg.n_kv_heads * 16 > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    return attn_call(c, batch, total_q_rows, q, kv_cache, false, 1.f, 1.f, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
+                     out, stream);
+}
 
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    fd::AttnParams p = attn_params(c, batch, total_q_rows, prefix_lens, q_lens, n_mask, n_blocks);
-    p.num_pages = num_pages;
-    p.q = static_cast<const __nv_bfloat16*>(q);
-    p.kv = static_cast<const __nv_bfloat16*>(kv_cache);
-    p.page_table = page_table;
-    p.out = static_cast<__nv_bfloat16*>(out);
-
-    const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;  // no rows: the plan alone checks the lengths
-    if (tc) {
-        if (fd::attn_tc_prepare(&c->tc_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
-    }
-    c->epoch = c->epoch == 0x7fffffff ? 1 : c->epoch + 1;
-    p.epoch = c->epoch;
-    // a pinned plan serves this call if it was made for exactly these lengths; anything else replaces it
-    const bool reuse = c->pinned && batch == c->pin_batch && total_q_rows == c->pin_rows && prefix_lens == c->pin_pl &&
-                       q_lens == c->pin_ql && n_mask == c->pin_nm && n_blocks == c->pin_nb;
-    // How the tensor-core kernel finds its work.  A call of few segments runs one cluster per segment; a call of
-    // few sequences plans for itself (unless a pinned plan is there to use); everything else uses the plan kernel.
-    int mode = fd::kTcPlanned;
-    if (tc && p.rb_per_seq == 1 && c->tc_choice != FD_ATTN_TCGEN05_PLANNED) {
-        const int n_seg = batch * p.Hkv;
-        // (a table too narrow for four tiles per sequence leaves a cluster nothing to split)
-        const bool splittable = (long long)p.max_pages * 16 >= 4 * fd::kTileTokens;
-        const int cl = (c->tc_choice == FD_ATTN_TCGEN05 && batch <= fd::kSelfPlanMaxRb && n_seg <= fd::kClusterMaxSegments && splittable)
-                           ? fd::attn_tc_cluster_size(c->tc_state, n_seg, c->n_sms) : 0;
-        if (cl >= 2) { mode = fd::kTcCluster; p.cluster = cl; }
-        else if (batch <= fd::kSelfPlanMaxRb && !reuse) mode = fd::kTcSelfPlanned;
-    }
-    if (mode == fd::kTcPlanned && !reuse) {
-        c->pinned = false;
-        fd::launch_plan(p, s);
-        c->launches += 1;
-    }
-    // under a pinned plan, behind another call it served: the plan, the lengths and the page table are not what the
-    // launch before this one writes, and may be read while it still runs
-    p.early = (reuse && c->pinned && c->pin_chain) ? 1 : 0;
-    if (!p.early) c->chain_out.clear();
-    // ... and so may q and the cache, if no call of the chain writes them: the attention calls before this one write
-    // their `out` (several of them may still be running: each starts as the one before it retires CTAs, and waits for
-    // it only before its own first write), the append writes the cache
-    if (p.early && tc && c->back_to_back) {
-        const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), q1 = q0 + (size_t)total_q_rows * p.Hq * p.d * 2;
-        const uintptr_t k0 = reinterpret_cast<uintptr_t>(kv_cache), k1 = k0 + (size_t)num_pages * 2 * p.Hkv * 16 * p.d * 2;
-        bool clash = c->chain_out.size() >= 1024;  // (a chain that long is not a step of a model: stop keeping track)
-        for (const auto& w : c->chain_out) clash = clash || (w.first < q1 && q0 < w.second) || (w.first < k1 && k0 < w.second);
-        // (behind the append, which writes the block's own slots of this cache: everything but those is read ahead)
-        if (!clash) p.early = c->chain_append ? 3 : 2;
-    }
-    if (total_q_rows > 0 && c->chain_out.size() < 1024) {
-        const uintptr_t o0 = reinterpret_cast<uintptr_t>(out);
-        c->chain_out.emplace_back(o0, o0 + (size_t)total_q_rows * p.Hq * p.d * 2);
-    }
-    c->chain_append = false;
-    c->after_attn = tc;
-    c->pin_chain = reuse && c->pinned;
-    if (c->attn_path == FD_ATTN_TCGEN05 && !tc) {
-    } else if (tc) {
-        fd::launch_attn_tc(c->tc_state, p, mode, s);  // merges split segments in its own epilogue
-        c->launches += 1;
-        c->last_mode = mode;
-    } else {
-        fd::launch_attn_simt(p, s);
-        fd::launch_merge(p, s);
-        c->launches += 2;
-    }
-    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+fd_status fd_attn_draft_verify_fp4(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, int num_pages,
+                                   const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
+                                   const int32_t* n_mask, const int32_t* n_blocks, float k_scale, float v_scale, void* out,
+                                   void* stream) {
+    if (!good_scale(k_scale) || !good_scale(v_scale)) return FD_ERR_INVALID_ARG;
+    return attn_call(c, batch, total_q_rows, q, kv_cache, true, k_scale, v_scale, num_pages, page_table, prefix_lens, q_lens, n_mask,
+                     n_blocks, out, stream);
 }
 
 fd_status fd_plan_pin(fd_ctx* c, int batch, int total_q_rows, const int32_t* prefix_lens, const int32_t* q_lens,
@@ -708,6 +654,110 @@ fd_status fd_kv_append(fd_ctx* c, int batch, int total_q_rows, const void* k_new
     return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
 }
 
+fd_status fd_kv_reserve(fd_ctx* c, int batch, int total_q_rows, int32_t* page_table, const int32_t* prefix_lens,
+                        const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks, const int32_t* freed_pages,
+                        const int32_t* n_freed, int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out,
+                        int num_pages, int32_t* slot_map, int32_t* positions, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
+    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || total_q_rows > c->max_rows || num_pages < 1) return FD_ERR_INVALID_ARG;
+    if (!free_pages || !n_free || !n_free_out || (freed_pages == nullptr) != (n_freed == nullptr)) return FD_ERR_INVALID_ARG;
+    if (batch == 0 && total_q_rows > 0) return FD_ERR_INVALID_ARG;
+    if (batch > 0 && (!page_table || !prefix_lens || !q_lens || !n_mask)) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && (!slot_map || !positions)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    fd::ReserveParams p;
+    p.batch = batch; p.total_rows = total_q_rows; p.num_pages = num_pages; p.max_pages = c->cfg.max_pages_per_seq;
+    p.max_q_len = c->cfg.max_q_len;
+    p.page_table = page_table; p.prefix_lens = prefix_lens; p.q_lens = q_lens; p.n_mask = n_mask; p.n_blocks = n_blocks;
+    p.freed = freed_pages; p.n_freed = n_freed; p.free_pages = free_pages; p.n_free = n_free; p.n_free_out = n_free_out;
+    p.slot_map = slot_map; p.positions = positions; p.ticket = c->rs_ticket; p.n_sms = c->n_sms; p.status = c->status;
+    fd::launch_reserve(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, int64_t row_stride, const void* q_weight,
+                                 const void* k_weight, float eps, const float* cos_sin, int max_positions, int rot_dim,
+                                 int rope_style, const int32_t* positions, const int32_t* slot_map, void* q_out,
+                                 void* kv_cache, int num_pages, int kv_format, float k_scale, float v_scale, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
+    if (!c || total_q_rows < 0 || total_q_rows > c->max_rows || num_pages < 0 || !(eps >= 0.f)) return FD_ERR_INVALID_ARG;
+    if (kv_format != FD_KV_BF16 && kv_format != FD_KV_FP4) return FD_ERR_INVALID_ARG;
+    if (rope_style != FD_ROPE_HALVES && rope_style != FD_ROPE_ADJACENT) return FD_ERR_INVALID_ARG;
+    const int d = c->cfg.head_dim, heads = c->cfg.n_q_heads + 2 * c->cfg.n_kv_heads;
+    if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return FD_ERR_INVALID_ARG;
+    if (row_stride < (int64_t)heads * d || row_stride % 8 != 0 || row_stride > 0x7fffffffLL) return FD_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (max_positions < 1 || !cos_sin || (total_q_rows > 0 && !positions))) return FD_ERR_INVALID_ARG;
+    if (kv_format == FD_KV_FP4 && (!good_scale(k_scale) || !good_scale(v_scale))) return FD_ERR_INVALID_ARG;
+    if (total_q_rows == 0) return FD_OK;
+    if (!qkv || !slot_map || !q_out || !kv_cache) return FD_ERR_INVALID_ARG;
+    if (!aligned(qkv, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(cos_sin, 16) || !aligned(q_out, 16) ||
+        !aligned(kv_cache, kv_format == FD_KV_FP4 ? 16 : 128))
+        return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    // every row reads all of its heads before another thread's q could land there only if the two do not share bytes
+    const uintptr_t i0 = reinterpret_cast<uintptr_t>(qkv), o0 = reinterpret_cast<uintptr_t>(q_out);
+    const uintptr_t i1 = i0 + ((size_t)(total_q_rows - 1) * row_stride + (size_t)heads * d) * 2, o1 = o0 + (size_t)total_q_rows * c->cfg.n_q_heads * d * 2;
+    if (i0 < o1 && o0 < i1) return FD_ERR_INVALID_ARG;
+    fd::NormRopeParams p = {};
+    p.total_rows = total_q_rows; p.num_pages = num_pages; p.Hq = c->cfg.n_q_heads; p.Hkv = c->cfg.n_kv_heads; p.d = d;
+    p.qkv = static_cast<const __nv_bfloat16*>(qkv); p.row_stride = row_stride;
+    p.q_weight = static_cast<const __nv_bfloat16*>(q_weight); p.k_weight = static_cast<const __nv_bfloat16*>(k_weight);
+    p.eps = eps; p.cos_sin = cos_sin; p.max_positions = max_positions; p.rot_dim = rot_dim; p.adjacent = rope_style == FD_ROPE_ADJACENT;
+    p.positions = positions; p.slot_map = slot_map;
+    p.q_out = static_cast<__nv_bfloat16*>(q_out);
+    if (kv_format == FD_KV_FP4) p.kv4 = static_cast<unsigned char*>(kv_cache);
+    else p.kv = static_cast<__nv_bfloat16*>(kv_cache);
+    p.k_scale = k_scale; p.v_scale = v_scale; p.n_sms = c->n_sms; p.status = c->status;
+    fd::launch_norm_rope(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+// Rows into (append) or out of (read) a 4-bit cache: the checks and parameters the two share.
+static fd_status fp4_rows(fd_ctx* c, int batch, int total_q_rows, const void* k, const void* v, const void* kv_cache, int num_pages,
+                          const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens, float k_scale, float v_scale,
+                          fd::Fp4RowsParams* p) {
+    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
+    if (!good_scale(k_scale) || !good_scale(v_scale)) return FD_ERR_INVALID_ARG;
+    p->batch = batch;
+    if (batch == 0) return total_q_rows == 0 ? FD_OK : FD_ERR_INVALID_ARG;
+    if (!page_table || !prefix_lens || !q_lens || !kv_cache) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && (!k || !v)) return FD_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(kv_cache, 16)) return FD_ERR_INVALID_ARG;
+    p->total_rows = total_q_rows; p->num_pages = num_pages; p->Hkv = c->cfg.n_kv_heads; p->d = c->cfg.head_dim;
+    p->max_pages = c->cfg.max_pages_per_seq; p->max_q_len = c->cfg.max_q_len;
+    p->k = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->v = static_cast<__nv_bfloat16*>(const_cast<void*>(v));
+    p->kv4 = static_cast<unsigned char*>(const_cast<void*>(kv_cache));
+    p->page_table = page_table; p->prefix_lens = prefix_lens; p->q_lens = q_lens;
+    p->k_scale = k_scale; p->v_scale = v_scale; p->n_sms = c->n_sms; p->status = c->status;
+    return FD_OK;
+}
+
+fd_status fd_kv_append_fp4(fd_ctx* c, int batch, int total_q_rows, const void* k_new, const void* v_new, void* kv_cache,
+                           int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
+                           float k_scale, float v_scale, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (the next attention call waits for this launch)
+    fd::Fp4RowsParams p;
+    const fd_status st = fp4_rows(c, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale, v_scale, &p);
+    if (st != FD_OK || batch == 0) return st;
+    fd::launch_kv_append_fp4(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_read_fp4(fd_ctx* c, int batch, int total_q_rows, const void* kv_cache, int num_pages, const int32_t* page_table,
+                         const int32_t* prefix_lens, const int32_t* q_lens, float k_scale, float v_scale, void* k_out,
+                         void* v_out, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
+    fd::Fp4RowsParams p;
+    const fd_status st = fp4_rows(c, batch, total_q_rows, k_out, v_out, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale, v_scale, &p);
+    if (st != FD_OK || batch == 0) return st;
+    fd::launch_kv_read_fp4(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
 fd_status fd_draft_select(fd_ctx* c, int batch, int total_mask_rows, int max_blocks, const float* draft_logits,
                           const float* bias, const int32_t* n_mask, const int32_t* n_blocks, float threshold,
                           int32_t* mask_tokens, float* mask_probs, int32_t* keep_len, void* stream) {
@@ -780,3 +830,93 @@ fd_status fd_last_device_status(fd_ctx* c, int32_t* code, void* stream) {
 }
 
 }  // extern "C"
+
+// The attention call on either cache.
+static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, bool fp4, float k_scale, float v_scale,
+                           int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
+                           const int32_t* n_mask, const int32_t* n_blocks, void* out, void* stream) {
+    if (!c || batch < 0 || total_q_rows < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
+    if (batch > c->cfg.max_batch || (long long)total_q_rows > (long long)batch * c->cfg.max_q_len)
+        return FD_ERR_INVALID_ARG;
+    if (batch == 0) return total_q_rows == 0 ? FD_OK : FD_ERR_INVALID_ARG;
+    if (!page_table || !prefix_lens || !q_lens || !n_mask) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && (!q || !out)) return FD_ERR_INVALID_ARG;
+    if (!kv_cache || num_pages == 0) return FD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(kv_cache, fp4 ? 16 : 128) || !aligned(page_table, 4)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * 2 * c->cfg.n_kv_heads * 16 > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    fd::AttnParams p = attn_params(c, batch, total_q_rows, prefix_lens, q_lens, n_mask, n_blocks);
+    p.num_pages = num_pages;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    if (fp4) {
+        p.kv4 = static_cast<const unsigned char*>(kv_cache);
+        p.scale_log2e *= k_scale;
+        p.out_scale = v_scale;
+    } else {
+        p.kv = static_cast<const __nv_bfloat16*>(kv_cache);
+    }
+    p.page_table = page_table;
+    p.out = static_cast<__nv_bfloat16*>(out);
+
+    const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0 && !fp4;  // no rows: the plan alone checks the lengths
+    if (tc) {
+        if (fd::attn_tc_prepare(&c->tc_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
+    }
+    c->epoch = c->epoch == 0x7fffffff ? 1 : c->epoch + 1;
+    p.epoch = c->epoch;
+    // a pinned plan serves this call if it was made for exactly these lengths; anything else replaces it
+    const bool reuse = c->pinned && batch == c->pin_batch && total_q_rows == c->pin_rows && prefix_lens == c->pin_pl &&
+                       q_lens == c->pin_ql && n_mask == c->pin_nm && n_blocks == c->pin_nb;
+    // How the tensor-core kernel finds its work.  A call of few segments runs one cluster per segment; a call of
+    // few sequences plans for itself (unless a pinned plan is there to use); everything else uses the plan kernel.
+    int mode = fd::kTcPlanned;
+    if (tc && p.rb_per_seq == 1 && c->tc_choice != FD_ATTN_TCGEN05_PLANNED) {
+        const int n_seg = batch * p.Hkv;
+        // (a table too narrow for four tiles per sequence leaves a cluster nothing to split)
+        const bool splittable = (long long)p.max_pages * 16 >= 4 * fd::kTileTokens;
+        const int cl = (c->tc_choice == FD_ATTN_TCGEN05 && batch <= fd::kSelfPlanMaxRb && n_seg <= fd::kClusterMaxSegments && splittable)
+                           ? fd::attn_tc_cluster_size(c->tc_state, n_seg, c->n_sms) : 0;
+        if (cl >= 2) { mode = fd::kTcCluster; p.cluster = cl; }
+        else if (batch <= fd::kSelfPlanMaxRb && !reuse) mode = fd::kTcSelfPlanned;
+    }
+    if (mode == fd::kTcPlanned && !reuse) {
+        c->pinned = false;
+        fd::launch_plan(p, s);
+        c->launches += 1;
+    }
+    // under a pinned plan, behind another call it served: the plan, the lengths and the page table are not what the
+    // launch before this one writes, and may be read while it still runs
+    p.early = (reuse && c->pinned && c->pin_chain) ? 1 : 0;
+    if (!p.early) c->chain_out.clear();
+    // ... and so may q and the cache, if no call of the chain writes them: the attention calls before this one write
+    // their `out` (several of them may still be running: each starts as the one before it retires CTAs, and waits for
+    // it only before its own first write), the append writes the cache
+    if (p.early && tc && c->back_to_back) {
+        const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), q1 = q0 + (size_t)total_q_rows * p.Hq * p.d * 2;
+        const size_t page = fp4 ? (size_t)fd::fp4_page_bytes(p.d) : (size_t)16 * p.d * 2;  // bytes of one head's K, or V
+        const uintptr_t k0 = reinterpret_cast<uintptr_t>(kv_cache), k1 = k0 + (size_t)num_pages * 2 * p.Hkv * page;
+        bool clash = c->chain_out.size() >= 1024;  // (a chain that long is not a step of a model: stop keeping track)
+        for (const auto& w : c->chain_out) clash = clash || (w.first < q1 && q0 < w.second) || (w.first < k1 && k0 < w.second);
+        // (behind the append, which writes the block's own slots of this cache: everything but those is read ahead)
+        if (!clash) p.early = c->chain_append ? 3 : 2;
+    }
+    if (total_q_rows > 0 && c->chain_out.size() < 1024) {
+        const uintptr_t o0 = reinterpret_cast<uintptr_t>(out);
+        c->chain_out.emplace_back(o0, o0 + (size_t)total_q_rows * p.Hq * p.d * 2);
+    }
+    c->chain_append = false;
+    c->after_attn = tc;
+    c->pin_chain = reuse && c->pinned;
+    if (c->attn_path == FD_ATTN_TCGEN05 && total_q_rows == 0) {
+    } else if (tc) {
+        fd::launch_attn_tc(c->tc_state, p, mode, s);  // merges split segments in its own epilogue
+        c->launches += 1;
+        c->last_mode = mode;
+    } else {
+        fd::launch_attn_simt(p, s);
+        fd::launch_merge(p, s);
+        c->launches += 2;
+    }
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}

@@ -6,9 +6,35 @@
 // materialised: a row carries the first key position it may NOT see (`limit`), which is
 // n + i + 1 for a candidate row (causal, no mask token) and kv_len for a mask row (prefix,
 // candidates, whole mask block).  Softmax is the online form in the log2 domain.
+//
+// FP4: the same over 4-bit pages.  A page is widened to bf16 as it enters shared memory, which is exact (fd_fp4.cuh);
+// everything behind that is the same code.
+#include "fd_fp4.cuh"
 #include "fd_internal.cuh"
 
 namespace fd {
+
+// One page of K or V of one kv-head, 4-bit -> [16][D] bf16 in shared memory, 16 elements at a time.
+template <int D>
+__device__ inline void widen_page(const unsigned char* src, __nv_bfloat16* dst) {
+    for (int e = threadIdx.x; e < D; e += kMaxRows) {  // 16 tokens x D / 16 groups
+        const int tok = e / (D / 16), g = e % (D / 16);
+        const uint2 codes = *reinterpret_cast<const uint2*>(src + tok * (D / 2) + g * 8);
+        const float s = e4m3_to_float(src[fp4_scale_offset(D) + e]);
+        uint32_t h[2][4];
+        e2m1x8_to_half(codes.x, h[0]);
+        e2m1x8_to_half(codes.y, h[1]);
+        __align__(16) __nv_bfloat162 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float2 f = __half22float2(as_half2(h[k >> 2][k & 3]));
+            v[k] = __floats2bfloat162_rn(f.x * s, f.y * s);
+        }
+        uint4* d4 = reinterpret_cast<uint4*>(dst + tok * D + g * 16);
+        d4[0] = reinterpret_cast<const uint4*>(v)[0];
+        d4[1] = reinterpret_cast<const uint4*>(v)[1];
+    }
+}
 
 template <int D>
 __device__ inline void store_out_row(__nv_bfloat16* dst, const float* o, float inv) {
@@ -21,7 +47,7 @@ __device__ inline void store_out_row(__nv_bfloat16* dst, const float* o, float i
     }
 }
 
-template <int D>
+template <int D, bool FP4>
 __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     float* qT = reinterpret_cast<float*>(smem_raw);                                   // [D][128], pre-scaled
@@ -82,12 +108,17 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
                     if (r == 0) flag_sequence(p, b);
                     phys = 0;
                 }
-                const __nv_bfloat16* kp = p.kv + (((long long)phys * 2 + 0) * p.Hkv + kvh) * 16 * D;
-                const __nv_bfloat16* vp = p.kv + (((long long)phys * 2 + 1) * p.Hkv + kvh) * 16 * D;
                 __syncthreads();  // everyone is done with the previous page
-                for (int e = r; e < 16 * D / 8; e += kMaxRows) {
-                    reinterpret_cast<uint4*>(ks)[e] = reinterpret_cast<const uint4*>(kp)[e];
-                    reinterpret_cast<uint4*>(vs)[e] = reinterpret_cast<const uint4*>(vp)[e];
+                if (FP4) {
+                    widen_page<D>(p.kv4 + fp4_page_offset(phys, p.Hkv, kvh, 0, D), ks);
+                    widen_page<D>(p.kv4 + fp4_page_offset(phys, p.Hkv, kvh, 1, D), vs);
+                } else {
+                    const __nv_bfloat16* kp = p.kv + (((long long)phys * 2 + 0) * p.Hkv + kvh) * 16 * D;
+                    const __nv_bfloat16* vp = p.kv + (((long long)phys * 2 + 1) * p.Hkv + kvh) * 16 * D;
+                    for (int e = r; e < 16 * D / 8; e += kMaxRows) {
+                        reinterpret_cast<uint4*>(ks)[e] = reinterpret_cast<const uint4*>(kp)[e];
+                        reinterpret_cast<uint4*>(vs)[e] = reinterpret_cast<const uint4*>(vp)[e];
+                    }
                 }
                 __syncthreads();
                 if (r >= rows) continue;
@@ -140,7 +171,7 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
         const bool complete = (t == seg_start) && (t_end == seg_end);
         if (r < rows) {
             if (complete) {
-                store_out_row<D>(p.out + ((long long)(row0 + i) * p.Hq + kvh * p.G + g) * D, acc, 1.f / l);
+                store_out_row<D>(p.out + ((long long)(row0 + i) * p.Hq + kvh * p.G + g) * D, acc, p.out_scale / l);
             } else {
                 const int slot = 2 * cta + (t == s_c ? 0 : 1);
                 p.part.m[slot * kMaxRows + r] = m;
@@ -157,16 +188,21 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
 // 66 KB + 8 KB of dynamic shared memory needs the opt-in; a per-device attribute, set once per context at fd_create.
 cudaError_t attn_simt_prepare(int d) {
     if (d != 128) return cudaSuccess;
-    return cudaFuncSetAttribute(attn_simt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * kMaxRows * 4 + 2 * 16 * 128 * 2);
+    const int smem = 128 * kMaxRows * 4 + 2 * 16 * 128 * 2;
+    const cudaError_t e = cudaFuncSetAttribute(attn_simt_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(attn_simt_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
 
 void launch_attn_simt(const AttnParams& p, cudaStream_t s) {
     if (p.batch == 0) return;
     const int smem = p.d * kMaxRows * 4 + 2 * 16 * p.d * 2;
+    const bool fp4 = p.kv4 != nullptr;
     if (p.d == 64) {
-        attn_simt_kernel<64><<<p.n_ctas, kMaxRows, smem, s>>>(p);
+        if (fp4) attn_simt_kernel<64, true><<<p.n_ctas, kMaxRows, smem, s>>>(p);
+        else attn_simt_kernel<64, false><<<p.n_ctas, kMaxRows, smem, s>>>(p);
     } else {
-        attn_simt_kernel<128><<<p.n_ctas, kMaxRows, smem, s>>>(p);
+        if (fp4) attn_simt_kernel<128, true><<<p.n_ctas, kMaxRows, smem, s>>>(p);
+        else attn_simt_kernel<128, false><<<p.n_ctas, kMaxRows, smem, s>>>(p);
     }
 }
 

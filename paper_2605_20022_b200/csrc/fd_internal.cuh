@@ -95,6 +95,8 @@ struct AttnParams {
                       // 3: as 2, but the launch before this one is the KV append of this cache: tiles of the prefix are
                       //    read early, a tile that reaches into the query block after the wait
     int* status;
+    const unsigned char* kv4;  // the 4-bit cache (fd_fp4.cuh), nullptr in a call on bf16 pages
+    float out_scale;           // what the merged output is multiplied by: 1, or v_scale of a 4-bit cache
 };
 
 // A sequence in which this call met a page id outside the pool: its rows are written as zeros.  The flag is the
@@ -288,7 +290,7 @@ __device__ inline void merge_row(const AttnParams& p, const CtaStarts& cs, int c
             acc[4 * k + 3] += w * v[k].w;
         }
     }
-    store_cols_bf16<CW>(dst, acc, 1.f / l);
+    store_cols_bf16<CW>(dst, acc, p.out_scale / l);
 }
 
 // How a tensor-core attention call finds its work: from the plan kernel's arrays; from scans each CTA makes
@@ -298,7 +300,7 @@ enum { kTcPlanned = 0, kTcSelfPlanned = 1, kTcCluster = 2 };
 // Launchers (defined next to their kernels).
 void launch_plan(const AttnParams& p, cudaStream_t s);
 cudaError_t attn_simt_prepare(int d);
-void launch_attn_simt(const AttnParams& p, cudaStream_t s);
+void launch_attn_simt(const AttnParams& p, cudaStream_t s);  // either cache: p.kv4 says which
 bool attn_tc_supported(int d, int G, int max_q_len);
 cudaError_t attn_tc_prepare(void** state, const AttnParams& p);  // tensor map for this kv pool
 void launch_attn_tc(void* state, const AttnParams& p, int mode, cudaStream_t s);  // mode: kTcPlanned, kTcSelfPlanned, kTcCluster
@@ -396,6 +398,62 @@ struct AppendParams {
                   //    writes it reads: the copies run while that call finishes, the kernel waits for it before it ends
 };
 void launch_kv_append(const AppendParams& p, cudaStream_t s);
+
+// Rows into the cache and out of it in 4 bits (the members of AppendParams, with the 4-bit cache).
+struct Fp4RowsParams {
+    int batch, total_rows, num_pages, Hkv, d, max_pages, max_q_len;
+    __nv_bfloat16* k;         // append: read only
+    __nv_bfloat16* v;
+    unsigned char* kv4;       // read: read only
+    const int32_t* page_table;
+    const int32_t* prefix_lens;
+    const int32_t* q_lens;
+    float k_scale, v_scale;
+    int n_sms;
+    int* status;
+};
+void launch_kv_append_fp4(const Fp4RowsParams& p, cudaStream_t s);
+void launch_kv_read_fp4(const Fp4RowsParams& p, cudaStream_t s);
+
+struct NormRopeParams {
+    int total_rows, num_pages, Hq, Hkv, d;
+    const __nv_bfloat16* qkv;
+    long long row_stride;
+    const __nv_bfloat16* q_weight;  // may be nullptr: no norm
+    const __nv_bfloat16* k_weight;
+    float eps;
+    const float* cos_sin;
+    int max_positions, rot_dim, adjacent;
+    const int32_t* positions;
+    const int32_t* slot_map;
+    __nv_bfloat16* q_out;
+    __nv_bfloat16* kv;        // one of the two caches
+    unsigned char* kv4;
+    float k_scale, v_scale;
+    int n_sms;
+    int* status;
+};
+void launch_norm_rope(const NormRopeParams& p, cudaStream_t s);
+
+struct ReserveParams {
+    int batch, total_rows, num_pages, max_pages, max_q_len;
+    int32_t* page_table;
+    const int32_t* prefix_lens;
+    const int32_t* q_lens;
+    const int32_t* n_mask;
+    const int32_t* n_blocks;  // may be nullptr
+    const int32_t* freed;     // may be nullptr, with n_freed
+    const int32_t* n_freed;
+    int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* n_free_out;
+    int32_t* slot_map;
+    int32_t* positions;
+    unsigned int* ticket;     // [1] CTAs finished, zero between calls
+    int n_sms;
+    int* status;
+};
+void launch_reserve(const ReserveParams& p, cudaStream_t s);
 
 struct SelectParams {
     int batch, max_kb;
