@@ -395,7 +395,8 @@ fd_status fd_qk_norm_rope_append(fd_ctx* ctx, int total_q_rows, const void* qkv,
  * fd_attn_draft_verify_fp4 is fd_attn_draft_verify_blocks for it: same arguments (n_blocks may be NULL), same mask, same
  * errors, same forms (FD_TC_*), pinned plans and overlap of consecutive calls included.  Slots no valid token owns may hold
  * any bit pattern.  Arithmetic: the values of the cache enter exactly, q is held in at least as many bits as bf16
- * relative to its row's largest element, the softmax weights in 11 bits, sums in fp32; bf16 output.
+ * relative to its row's largest element, the softmax weights in 11 bits down to 2^-21 of the row's largest (below that to
+ * within 2^-32 of it), sums in fp32; bf16 output.
  */
 fd_status fd_kv_append_fp4(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
                            void* kv_cache, int num_pages, const int32_t* page_table, const int32_t* prefix_lens,

@@ -166,7 +166,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->attn_path = (cfg->attn_path == FD_ATTN_SIMT || !tc_ok) ? FD_ATTN_SIMT : FD_ATTN_TCGEN05;
     // SIMT kernel: two 74 KB CTAs fit an SM; tensor-core kernel: one persistent CTA per SM
     c->n_ctas = c->attn_path == FD_ATTN_SIMT ? 2 * c->n_sms : c->n_sms;
-    if (fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
+    if (c->attn_path == FD_ATTN_SIMT && fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
 
     const int B = cfg->max_batch, d = cfg->head_dim;
     const size_t slots = 2 * (size_t)c->n_ctas;
@@ -859,7 +859,7 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
     p.page_table = page_table;
     p.out = static_cast<__nv_bfloat16*>(out);
 
-    const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0 && !fp4;  // no rows: the plan alone checks the lengths
+    const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;  // no rows: the plan alone checks the lengths
     if (tc) {
         if (fd::attn_tc_prepare(&c->tc_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
     }
@@ -876,7 +876,7 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
         // (a table too narrow for four tiles per sequence leaves a cluster nothing to split)
         const bool splittable = (long long)p.max_pages * 16 >= 4 * fd::kTileTokens;
         const int cl = (c->tc_choice == FD_ATTN_TCGEN05 && batch <= fd::kSelfPlanMaxRb && n_seg <= fd::kClusterMaxSegments && splittable)
-                           ? fd::attn_tc_cluster_size(c->tc_state, n_seg, c->n_sms) : 0;
+                           ? fd::attn_tc_cluster_size(c->tc_state, fp4, n_seg, c->n_sms) : 0;
         if (cl >= 2) { mode = fd::kTcCluster; p.cluster = cl; }
         else if (batch <= fd::kSelfPlanMaxRb && !reuse) mode = fd::kTcSelfPlanned;
     }
@@ -908,7 +908,7 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
     c->chain_append = false;
     c->after_attn = tc;
     c->pin_chain = reuse && c->pinned;
-    if (c->attn_path == FD_ATTN_TCGEN05 && total_q_rows == 0) {
+    if (c->attn_path == FD_ATTN_TCGEN05 && !tc) {
     } else if (tc) {
         fd::launch_attn_tc(c->tc_state, p, mode, s);  // merges split segments in its own epilogue
         c->launches += 1;

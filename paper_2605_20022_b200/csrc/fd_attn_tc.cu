@@ -44,6 +44,7 @@
 
 #include <vector>
 
+#include "fd_fp4.cuh"
 #include "fd_internal.cuh"
 #include "fd_sm100.cuh"
 
@@ -53,8 +54,8 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kThreads = 384;  // warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads
-constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10;  // warp 11 loads Q
+// warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads (FP4: 8 loads both, 9 idle, 12-15 widen)
+constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10, kQWarp = 11;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kEarlyLoadMaxTiles = 96;     // longest range of a CTA that starts on its KV before the previous launch has completed
 // Who issues the P V of a tile.  In a range of at least kGroupPvMinTiles tiles warp 0 of the softmax group that wrote P
@@ -78,24 +79,32 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 #define FD_STAGGER 1
 #endif
 
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 struct Cfg {
-    static constexpr int kStages = (D == 128) ? 3 : 6;   // buffers in the K ring, and again in the V ring
+    static constexpr int kThreads = FP4 ? 512 : 384;     // FP4: warps 12-15 widen the tiles
+    // buffers in the K ring, and again in the V ring (FP4: of widened tiles, fed from the raw ring)
+    static constexpr int kStages = FP4 ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
     static constexpr int kQBytes = kMaxRows * D * 2;
     static constexpr int kKBytes = kTileTokens * D * 2;  // one K (or V) tile
-    static constexpr int kBarOffset = kQBytes + 2 * kStages * kKBytes;
+    static constexpr int kRawStages = FP4 ? (D == 128 ? 3 : 6) : 0;
+    static constexpr int kRawPage = 2 * fp4_page_bytes(D);   // K and V of one page of the kv-head lie side by side in the cache
+    static constexpr int kRawBytes = 8 * kRawPage;           // ... of a tile
+    static constexpr int kRawOffset = kQBytes + 2 * kStages * kKBytes;
+    static constexpr int kBarOffset = kRawOffset + kRawStages * kRawBytes;
     static constexpr int kCsOffset = kBarOffset + 320;           // window of the CTA range starts
     static constexpr int kDescOffset = kBarOffset + 448;         // ring of piece descriptors
     static constexpr int kScanOffset = kBarOffset + 720;         // SelfScans: the scans of a call that plans for itself
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
-    static constexpr int kSmemBytes = kBarOffset + 3072;         // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kFp4Offset = kBarOffset + 3072;         // FP4: Fp4Shared
+    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 2304 : 0);  // the dynamic shared memory is declared 1024-byte aligned
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
     // A K or V tile in shared memory: [8-token group][half of d][8 rows][128 B] -- what one TMA box per page
     // (two groups) lands; for either half the 16 groups lie kGroupBytes apart, the stride the MMA descriptors name.
     static constexpr int kGroupBytes = kHalves * 1024;
     static constexpr int kPageBytes = 2 * kGroupBytes;
+    static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 };
 
 struct Bars {
@@ -113,6 +122,16 @@ struct Bars {
     int bad;                   // a load warp of this CTA met a page id outside the pool
 };
 constexpr int kDescSlots = 4;
+
+// What a call on 4-bit pages keeps beside Bars.
+struct Fp4Shared {
+    uint64_t raw_full[6], raw_empty[6];  // a tile of codes and scales has landed / has been widened
+    uint64_t q_ready;                    // the Q tile of a piece has been turned into fp16
+    // Per query row: what its scores are multiplied by (slot = piece & 3; a slot is written again three pieces later,
+    // when the epilogue of the piece it served is over: the P V of a piece waits for the epilogue before it).
+    float row_scale[4][kMaxRows];
+};
+static_assert(sizeof(Fp4Shared) <= 2304, "Fp4Shared must fit behind the row blocks");
 
 // The plan of a call that plans for itself (at most kSelfPlanMaxRb sequences, one row block each), in shared memory.
 struct SelfScans {
@@ -242,7 +261,7 @@ struct Walk {
 template <int D, int MODE>
 __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnParams& p, int n_rb, unsigned char* ring, uint64_t* full,
                                           uint64_t* empty, int which, const Range rg, uint64_t* k0_full, volatile int* bad, volatile int* abort) {
-    using C = Cfg<D, MODE>;
+    using C = Cfg<D, MODE, false>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     constexpr int kOps = 8;  // pages of a tile: one box each
     const int pg = lane;
@@ -324,15 +343,189 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
     }
 }
 
+// FP4 load warp: codes and scales of K and V of a page lie side by side in the cache, so one untiled bulk copy a page
+// brings both (2304 bytes at d = 128).  Otherwise the K load warp's walk: see load_role.
+template <int D, int MODE>
+__device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, unsigned char* raw, Fp4Shared* f4, const Range rg,
+                                              volatile int* bad, volatile int* abort) {
+    using C = Cfg<D, MODE, true>;
+    const int lane = threadIdx.x & 31, cta = blockIdx.x;
+    int issued = 0;
+    const uint64_t policy = make_policy_evict_first();
+    const int s_c = rg.s_c, e_c = rg.e_c;
+    Walk w = {s_c, 0, {0, 0}, 0, rg.first};
+    bool ok = true, waited = !p.early;
+    int bad_early = -1;
+    while (w.t < e_c && ok) {
+        const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
+        const int32_t* table = p.page_table + (long long)pc.b * p.max_pages;
+        auto load_ids = [&](int batch) -> int {  // four tiles (32 pages, one per lane), one batch ahead
+            const int j = batch * 4 + (lane >> 3);
+            const int pos = ((pc.tile0 + j) * 8 + (lane & 7)) * 16;
+            if (!(j < pc.nt && pos < pc.kv_len)) return -1;
+            int id = table[pos >> 4];
+            if ((unsigned)id >= (unsigned)p.num_pages) {  // never form an address from a bad id
+                if (!waited && p.early >= 2) { wait_prior_launch(); waited = true; }
+                if (waited) flag_sequence(p, pc.b); else bad_early = pc.b;
+                *bad = 1;
+                id = 0;
+            }
+            return id;
+        };
+        int ids_cur = load_ids(0), ids_next = load_ids(1);
+        for (int j = 0; j < pc.nt; ++j) {
+            const int g = w.g0 + j, st = g % C::kRawStages, use = g / C::kRawStages;
+            if (j > 0 && (j & 3) == 0) { ids_cur = ids_next; ids_next = load_ids((j >> 2) + 1); }
+            const int phys = __shfl_sync(0xffffffffu, ids_cur, (j & 3) * 8 + (lane & 7));
+            if (!waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n))) {
+                wait_prior_launch();
+                waited = true;
+                if (bad_early >= 0) flag_sequence(p, bad_early);
+            }
+            if (!wait_all(&f4->raw_empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
+            const int npg = min(8, (pc.kv_len - (pc.tile0 + j) * kTileTokens + 15) >> 4);
+            if (lane == 0) mbar_arrive_expect_tx(&f4->raw_full[st], npg * C::kRawPage);
+            __syncwarp();
+            if (lane < 8 && phys >= 0)
+                bulk_load_hint(raw + st * C::kRawBytes + lane * C::kRawPage, p.kv4 + fp4_page_offset(phys, p.Hkv, pc.kvh, 0, D), C::kRawPage,
+                               &f4->raw_full[st], policy);
+            issued = g + 1;
+        }
+        w.advance(pc);
+    }
+    if (*abort) {  // drain copies still in flight before the shared memory is given back
+        for (int g = max(0, issued - C::kRawStages); g < issued; ++g) {
+            const unsigned long long t0 = global_ns();
+            for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
+                if (mbar_try_wait(&f4->raw_full[g % C::kRawStages], (g / C::kRawStages) & 1)) break;
+        }
+    }
+}
+
+// One K or V tile: codes and scales -> fp16 in the layout the MMA reads (code * scale is exact: fd_fp4.cuh).  A thread
+// widens 32 elements of a token at a time (16 bytes of codes, two scales, four 16-byte stores).  Four neighbouring lanes
+// share a token, so the reads are contiguous; of a 16-byte store's eight lanes -- two tokens, four chunks -- the
+// chunks of the upper half of d store their words in the order 2 3 0 1, which puts all eight on different banks.
+// ZERO_TAIL: tokens at or beyond `valid` become zeros (no token owns them: they may hold a NaN, and 0 * NaN is not 0).
+template <int D, bool ZERO_TAIL>
+__device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned char* tile, int valid) {
+    constexpr int kChunks = D / 32;        // 32-element chunks of a token
+    constexpr int kRawPage = 2 * fp4_page_bytes(D);
+    constexpr int kHalves = D / 64;
+    const int t = threadIdx.x & 127, c = t % kChunks;
+#pragma unroll
+    for (int it = 0; it < kChunks; ++it) { // 128 threads x 1 chunk per pass, kTileTokens * kChunks chunks
+        const int tok = t / kChunks + it * (128 / kChunks);
+        const unsigned char* page = raw + (tok >> 4) * kRawPage;
+        const uint4 codes = *reinterpret_cast<const uint4*>(page + (tok & 15) * (D / 2) + c * 16);
+        const uint32_t sc = e4m3x2_to_half(*reinterpret_cast<const uint16_t*>(page + fp4_scale_offset(D) + (tok & 15) * (D / 16) + c * 2));
+        const __half2 s_lo = __half2half2(__low2half(as_half2(sc))), s_hi = __half2half2(__high2half(as_half2(sc)));
+        const bool dead = ZERO_TAIL && tok >= valid;
+        const bool swap = kHalves == 2 && (c & 2);
+        const uint32_t wd[4] = {swap ? codes.z : codes.x, swap ? codes.w : codes.y, swap ? codes.x : codes.z, swap ? codes.y : codes.w};
+        const __half2 s01 = swap ? s_hi : s_lo, s23 = swap ? s_lo : s_hi;
+        unsigned char* row = tile + (tok >> 3) * (kHalves * 1024) + (c >> 1) * 1024 + (tok & 7) * 128;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t h[4];
+            e2m1x8_to_half(wd[k], h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = dead ? 0u : as_u32(__hmul2(as_half2(h[i]), k < 2 ? s01 : s23));
+            const int unit = (c & 1) * 4 + (swap ? k ^ 2 : k);
+            *reinterpret_cast<uint4*>(row + ((unit ^ (tok & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+    }
+}
+
+// The Q tile of a piece, bf16 -> fp16 in place, a thread a row.  A row is multiplied by the power of two that brings its
+// largest element into [2^14, 2^15): bf16's 8 bits then fit fp16 exactly down to 2^-31 of that element (below, the loss is
+// smaller than what the fp32 sum of the score drops), and the factor goes into the scale of the row's scores.
+template <int D>
+__device__ __forceinline__ void q_to_half(unsigned char* sq, float* row_scale, float scale_log2e) {
+    const int r = threadIdx.x & 127;
+    unsigned char* row = sq + r * 128;
+    uint32_t mx = 0;
+#pragma unroll
+    for (int u = 0; u < D / 8; ++u) {
+        const uint4 v = *reinterpret_cast<const uint4*>(row + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4));
+        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+    }
+    const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);  // biased exponent of the largest magnitude
+    const float f = __uint_as_float((uint32_t)(127 + 141 - e) << 23);  // 2^(141 - e), e in [14, 255]
+#pragma unroll
+    for (int u = 0; u < D / 8; ++u) {
+        uint4* at = reinterpret_cast<uint4*>(row + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4));
+        uint4 v = *at;
+        uint32_t* wd = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            wd[k] = as_u32(__floats2half2_rn(__uint_as_float(wd[k] << 16) * f, __uint_as_float(wd[k] & 0xffff0000u) * f));
+        *at = v;
+    }
+    // never 0 (a hidden score is -inf, and 0 * -inf is not): a score of at most 2^35 times 2^-126 is 0 for every purpose
+    row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 141)), 1.17549435e-38f), 3.4028234e38f);
+}
+
+// FP4: warps 12-15.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
+// is widened before its Q is touched, while that Q is still on its way.
+template <int D, int MODE>
+__device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv,
+                                           const unsigned char* raw, Bars* bars, Fp4Shared* f4, const Piece* ring, const Range rg,
+                                           volatile int* abort) {
+    using C = Cfg<D, MODE, true>;
+    const int lane = threadIdx.x & 31;
+    Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
+    while (w.t < rg.e_c) {
+        if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
+        const Piece pc = ring[w.piece & (kDescSlots - 1)];
+        auto do_k = [&](int j) -> bool {
+            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            if (!wait_all(&f4->raw_full[rs], (g / C::kRawStages) & 1, abort)) return false;
+            if (!wait_all(&bars->k_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
+            widen_tile<D, false>(raw + rs * C::kRawBytes, sk + st * C::kKBytes, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->k_full[st]);
+            return true;
+        };
+        auto do_v = [&](int j) -> bool {
+            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
+            const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
+            const unsigned char* rv = raw + rs * C::kRawBytes + fp4_page_bytes(D);
+            if (valid >= kTileTokens) widen_tile<D, false>(rv, sv + st * C::kKBytes, 0);
+            else widen_tile<D, true>(rv, sv + st * C::kKBytes, valid);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&bars->v_full[st]);
+                mbar_arrive(&f4->raw_empty[rs]);
+            }
+            return true;
+        };
+        if (!do_k(0)) return;
+        if (!wait_all(&bars->q_full, w.piece & 1, abort)) return;
+        q_to_half<D>(sq, f4->row_scale[w.piece & 3], p.scale_log2e);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&f4->q_ready);
+        for (int j = 0; j < pc.nt; ++j) {
+            if (j + 1 < pc.nt && !do_k(j + 1)) return;
+            if (!do_v(j)) return;
+        }
+        w.advance(pc);
+    }
+}
+
 // Q load warp: the G * Lq rows of a piece -> shared memory, K-major, 128-byte swizzle.  q is seen as
 // [T][Hq][d]; one TMA box is 64 elements of d x the G q-heads of the kv-head x q_box_t block rows, which
 // lands as q_box_t * G consecutive 128-byte rows, row (i, g) at i * G + g: the order the MMA wants.  The
 // last box of a piece may reach past the block (rows of the next sequence, or zeros past T): each query
 // row only ever influences its own output row, and those rows are never stored.
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 __device__ __forceinline__ void q_role(const CUtensorMap& qmap, const AttnParams& p, int n_rb, unsigned char* sq, Bars* bars, Piece* ring,
                                        const Range rg, volatile int* abort) {
-    using C = Cfg<D, MODE>;
+    using C = Cfg<D, MODE, FP4>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     const int bt = p.q_box_t;
     const int s_c = rg.s_c, e_c = rg.e_c;
@@ -383,13 +576,13 @@ __device__ __forceinline__ void zero_v_tail(unsigned char* vt, int valid, int la
 }
 
 // MMA issuing warp.
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv, Bars* bars,
-                                         const Piece* ring, uint32_t tmem, const Range rg, volatile int* abort) {
-    using C = Cfg<D, MODE>;
+                                         Fp4Shared* f4, const Piece* ring, uint32_t tmem, const Range rg, volatile int* abort) {
+    using C = Cfg<D, MODE, FP4>;
     const int lane = threadIdx.x & 31;
-    constexpr uint32_t idesc_qk = make_idesc_bf16(128, kTileTokens, false);
-    constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
+    constexpr uint32_t idesc_qk = FP4 ? make_idesc_f16(128, kTileTokens, false) : make_idesc_bf16(128, kTileTokens, false);
+    constexpr uint32_t idesc_pv = FP4 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
     const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
     const bool group_pv = pv_by_group<MODE>(rg.e_c - rg.s_c);
     if (p.early == 1) wait_prior_launch();  // (this role touches shared and tensor memory only; p.early >= 2 lets it run ahead)
@@ -400,12 +593,12 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     while (w.t < e_c && ok) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) break;
         const Piece pc = ring[w.piece & (kDescSlots - 1)];
-        if (!wait_all(&bars->q_full, w.piece & 1, abort)) break;
+        if (!wait_all(FP4 ? &f4->q_ready : &bars->q_full, w.piece & 1, abort)) break;
         auto issue_pv = [&](int jj) {  // (ranges whose P V this warp issues: see kGroupPvMinTiles)
             const int gg = w.g0 + jj, s = jj & 1, st = gg % C::kStages, u = w.u_base[s] + (jj >> 1);
             if (!wait_all(&bars->v_full[st], (gg / C::kStages) & 1, abort)) { ok = false; return; }
             unsigned char* vt = sv + st * C::kKBytes;
-            zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + jj) * kTileTokens, lane);
+            if (!FP4) zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + jj) * kTileTokens, lane);  // (FP4: widened as zeros)
             // the first P V of a stream in a piece overwrites O: the previous piece's epilogue must have read it
             if (jj < 2 && w.piece > 0 && !wait_all(&bars->o_free, (w.piece - 1) & 1, abort)) { ok = false; return; }
             // (descriptors are made before the last wait: what follows it is the MMA instructions alone.  The address
@@ -485,9 +678,10 @@ __host__ __device__ constexpr int cluster_share(int c) { return (kMaxRows + c - 
 // What one CTA hands one owner: the O rows as [d / 4 words][share rows][16 bytes], then (m, l) per row.
 __host__ __device__ constexpr uint32_t cluster_block_bytes(int c, int d) { return (uint32_t)((cluster_share(c) * (d * 4 + 8) + 15) / 16 * 16); }
 // Do the two scratch slots of a CTA, and the K ring where the blocks land, hold the c blocks of a cluster of c?
-__host__ __device__ constexpr bool cluster_fits(int c, int d) {
+// (FP4: the K and V rings, which lie side by side and are both idle by then.)
+__host__ __device__ constexpr bool cluster_fits(int c, int d, bool fp4) {
     return (uint32_t)c * cluster_block_bytes(c, d) <= 2u * kMaxRows * d * 4 &&
-           (uint32_t)c * cluster_block_bytes(c, d) <= (uint32_t)(d == 128 ? 3 : 6) * kTileTokens * d * 2;
+           (uint32_t)c * cluster_block_bytes(c, d) <= (uint32_t)(fp4 ? (d == 128 ? 4 : 8) : (d == 128 ? 3 : 6)) * kTileTokens * d * 2;
 }
 
 // Addresses of the exchange.  In global memory: CTA `cta` of the grid owns scratch slots 2 cta and 2 cta + 1, one block
@@ -561,7 +755,7 @@ __device__ __forceinline__ void cluster_reduce(const AttnParams& p, const Exchan
             }
         }
         if (!act) continue;
-        float inv = l > 0.f ? 1.f / l : 0.f;
+        float inv = l > 0.f ? p.out_scale / l : 0.f;
         if (flagged) {  // by assignment: what came from a stand-in page may be inf or NaN
             inv = 0.f;
             acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -580,20 +774,20 @@ __device__ __forceinline__ void cluster_reduce(const AttnParams& p, const Exchan
 // this CTA's own piece -- the own_pos-th of the segment in CTA order -- is in registers (own: the thread's D / 2
 // columns).  Same arithmetic, same order as merge_row: the result does not depend on who merges.  Called by all 256
 // threads of the softmax groups (it holds barriers); `active`: the thread has a row to write.
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 struct Stage {
-    static constexpr uint32_t kBytes = Cfg<D, MODE>::kQBytes + 2 * Cfg<D, MODE>::kStages * Cfg<D, MODE>::kKBytes;
+    static constexpr uint32_t kBytes = Cfg<D, MODE, FP4>::kQBytes + 2 * Cfg<D, MODE, FP4>::kStages * Cfg<D, MODE, FP4>::kKBytes;
     static constexpr uint32_t kPieceBytes = kMaxRows * D * 4;
     static constexpr int kRound = (kBytes - 8192) / kPieceBytes;
     static constexpr uint32_t kMlOffset = kRound * kPieceBytes;
     static constexpr int kMaxOthers = (kBytes - kMlOffset) / (2 * kMaxRows * 4) - 1;
 };
 
-template <int D, int MODE, class IssueRound>
+template <int D, int MODE, bool FP4, class IssueRound>
 __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, const unsigned char* stage, int n_other, int own_pos,
                                              const float* own, int r, int cg, bool active, bool flagged, int kvh, int row0,
                                              volatile int* abort, IssueRound issue_round) {
-    using S = Stage<D, MODE>;
+    using S = Stage<D, MODE, FP4>;
     constexpr int CW = D / 2;
     const float* ml = reinterpret_cast<const float*>(stage + S::kMlOffset);  // [1 + n_other][2][128]
     float acc[CW];
@@ -644,23 +838,34 @@ __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, co
         store_cols_bf16<CW>(dst, acc, 0.f);
         return;
     }
-    store_cols_bf16<CW>(dst, acc, 1.f / l);
+    store_cols_bf16<CW>(dst, acc, p.out_scale / l);
+}
+
+// Two weights in the 16-bit type of the P V product.
+template <bool FP4>
+__device__ __forceinline__ uint32_t pack16(float2 v) {
+    if (FP4) return as_u32(__floats2half2_rn(v.x, v.y));
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
+    return *reinterpret_cast<const uint32_t*>(&b);
 }
 
 // The two softmax groups (256 threads).
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, float* ex, int* s_cs, const CtaStarts cs, const Piece* ring,
                                              uint32_t tmem, const Range rg, const Exchange<D> exch, int cl_rank, unsigned char* stage,
-                                             unsigned char* sv, volatile int* abort) {
-    using C = Cfg<D, MODE>;
-    constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
+                                             unsigned char* sv, const Fp4Shared* f4, volatile int* abort) {
+    using C = Cfg<D, MODE, FP4>;
+    constexpr uint32_t idesc_pv = FP4 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     const int s_c = rg.s_c, e_c = rg.e_c;
     const int s = warp >> 2;                  // stream
     const int r = (warp & 3) * 32 + lane;     // query row == TMEM lane
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
-    const float c = p.scale_log2e;
+    float c = p.scale_log2e;  // (FP4: of this row and piece, from the conversion of q)
+    // FP4 holds P in fp16: everything is scaled by 2^7, so that weights between 2^-21 and, with the deferred rescaling, 2^15 keep
+    // all of their bits; m carries the factor, so sums, partials and merges need not know
+    constexpr float kHead = FP4 ? 7.f : 0.f;
     // fill the window of range starts; the barrier below orders it before its first use
     if (MODE == kTcPlanned && tid < kCsWindow) {  // (a call that plans for itself has filled it while planning)
         const int cc = cs.base + tid;
@@ -692,6 +897,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
             const int u = w.u_base[s] + (j >> 1);
             if (!wait_all(&bars->s_full[s], u & 1, abort)) { ok = false; break; }
             tc_fence_after();
+            if (FP4 && j < 2) c = f4->row_scale[w.piece & 3][r];
             {
                 const int pos0 = (pc.tile0 + j) * kTileTokens;
                 // tile reaches into the query block (or past kv_len): the row's mask applies, in tile-local columns
@@ -722,7 +928,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         mx[2] = max3(mx[2], __uint_as_float(sv[ch][k + 4]), __uint_as_float(sv[ch][k + 5]));
                         mx[3] = max3(mx[3], __uint_as_float(sv[ch][k + 6]), __uint_as_float(sv[ch][k + 7]));
                     }
-                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
+                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c - kHead);
                 float alpha = 1.f;
                 if (j < 2 || m == -INFINITY) {
                     m = m_new;  // nothing accumulated yet (O is overwritten, or exactly zero)
@@ -759,9 +965,8 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         const float2 pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
                         sum0 = __fadd2_rn(sum0, pa);
                         sum1 = __fadd2_rn(sum1, pb);
-                        const __nv_bfloat162 ba = __floats2bfloat162_rn(pa.x, pa.y), bb = __floats2bfloat162_rn(pb.x, pb.y);
-                        pk[k >> 1] = *reinterpret_cast<const uint32_t*>(&ba);
-                        pk[16 + (k >> 1)] = *reinterpret_cast<const uint32_t*>(&bb);
+                        pk[k >> 1] = pack16<FP4>(pa);
+                        pk[16 + (k >> 1)] = pack16<FP4>(pb);
                     }
                     tmem_st32(s_addr + hp * 32, pk);  // overwrites S columns that are already in registers
                 }
@@ -777,7 +982,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 const int gg = w.g0 + j, st = gg % C::kStages;
                 unsigned char* vt = sv + st * C::kKBytes;
                 if (!wait_all(&bars->v_full[st], (gg / C::kStages) & 1, abort)) { ok = false; break; }
-                zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + j) * kTileTokens, lane);
+                if (!FP4) zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + j) * kTileTokens, lane);  // (FP4: widened as zeros)
                 // the first P V of a stream in a piece overwrites O: the previous piece's epilogue (both groups) must have read it
                 if (j < 2 && w.piece > 0 && !wait_all(&bars->o_free, (w.piece - 1) & 1, abort)) { ok = false; break; }
                 // (the address field of a descriptor is its low 14 bits, in 16-byte units, so a K step is an addition)
@@ -809,7 +1014,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         const int seg_t0 = w.t - pc.tile0, seg_t1 = seg_t0 + pc.seg_nt;
         int c_first = cta, c_last = cta, n_pieces = 1, ticket = -1;  // (no ticket drawn: never the merger)
         int* seg_cnt = p.plan.seg_count + 2 * (pc.v * p.Hkv + pc.kvh);  // [0] tickets drawn, [1] partials delivered
-        using St = Stage<D, MODE>;
+        using St = Stage<D, MODE, FP4>;
         if (MODE != kTcCluster && !pc.complete) {
             segment_ctas(cs, p.n_ctas, cta, seg_t0, seg_t1, c_first, c_last);
             if (tid == 0 && !*abort) {
@@ -838,7 +1043,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
             a0 = (m == -INFINITY) ? 0.f : exp2f(m - mm);
             a1 = (m1 == -INFINITY) ? 0.f : exp2f(m1 - mm);
             L = a0 * l + (two ? a1 * l1 : 0.f);
-            if (pc.complete) { const float inv = 1.f / L; a0 *= inv; a1 *= inv; }
+            if (pc.complete) { const float inv = p.out_scale / L; a0 *= inv; a1 *= inv; }
             ex[r] = a0;
             ex[kMaxRows + r] = a1;
         }
@@ -991,7 +1196,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         if (rr < pc.rows)
                             merge_row<D, D / 2>(p, cs, c_first, c_last, pc.b, pc.kvh, pc.row0, seg_t0, seg_t1, rr, cg, &o[0][0], cta);
                     } else {
-                        merge_staged<D, MODE>(p, bars, stage, (int)((bars->epi_flag >> 8) & 0xff), (int)(bars->epi_flag >> 16), &o[0][0], rr, cg,
+                        merge_staged<D, MODE, FP4>(p, bars, stage, (int)((bars->epi_flag >> 8) & 0xff), (int)(bars->epi_flag >> 16), &o[0][0], rr, cg,
                                               rr < pc.rows, (bars->epi_flag & 8) != 0, pc.kvh, pc.row0, abort, issue_round);
                     }
                 }
@@ -1061,10 +1266,10 @@ __device__ __forceinline__ void self_plan(const AttnParams& p, SelfScans* sc, Ro
     }
 }
 
-template <int D, int MODE>
-__global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
+template <int D, int MODE, bool FP4>
+__global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
                                                               const AttnParams p_in) {
-    using C = Cfg<D, MODE>;
+    using C = Cfg<D, MODE, FP4>;
     extern __shared__ __align__(1024) unsigned char smem[];  // the swizzled tiles need 1024-byte alignment
     unsigned char* sq = smem;
     unsigned char* sk = smem + C::kQBytes;                      // K ring
@@ -1075,6 +1280,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     Piece* ring = reinterpret_cast<Piece*>(smem + C::kDescOffset);
     SelfScans* scans = reinterpret_cast<SelfScans*>(smem + C::kScanOffset);
     RowBlock* rbs = reinterpret_cast<RowBlock*>(smem + C::kRbOffset);
+    Fp4Shared* f4 = reinterpret_cast<Fp4Shared*>(smem + C::kFp4Offset);  // FP4 only
     volatile int* abort = &bars->abort;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -1088,8 +1294,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     //      griddepcontrol.wait below is where that launch's results are needed
     if (warp == 1 && lane == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(&bars->k_full[i], 1); mbar_init(&bars->k_empty[i], 1);
-            mbar_init(&bars->v_full[i], 1); mbar_init(&bars->v_empty[i], 1);
+            mbar_init(&bars->k_full[i], FP4 ? 4 : 1); mbar_init(&bars->k_empty[i], 1);  // FP4: the four widening warps
+            mbar_init(&bars->v_full[i], FP4 ? 4 : 1); mbar_init(&bars->v_empty[i], 1);
+        }
+        if (FP4) {
+            for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], 4); }
+            mbar_init(&f4->q_ready, 4);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
@@ -1214,14 +1424,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         // Warp-specialised register budgets: the softmax groups keep a whole 128-column row of S in registers.
         // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168, what the launch allocated: the increase is served exactly by what
         // the decrease released (a request for more than that does not return).
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        softmax_role<D, MODE>(p, bars, ex, s_cs, cs, ring, tmem, rg, exch, cl_rank, sq, sv, abort);
+        // FP4: 8 x 32 x 184 + 4 x 32 x 56 + 4 x 32 x 88 = 512 x 128, likewise.
+        if (FP4) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        softmax_role<D, MODE, FP4>(p, bars, ex, s_cs, cs, ring, tmem, rg, exch, cl_rank, sq, sv, f4, abort);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (warp == kKWarp) load_role<D, MODE>(tmap, p, n_rb, sk, bars->k_full, bars->k_empty, 0, rg, &bars->k_full[0], &bars->bad, abort);
-        else if (warp == kVWarp) load_role<D, MODE>(tmap, p, n_rb, sv, bars->v_full, bars->v_empty, 1, rg, &bars->k_full[0], &bars->bad, abort);
-        else if (warp == kMmaWarp) mma_role<D, MODE>(p, sq, sk, sv, bars, ring, tmem, rg, abort);
-        else q_role<D, MODE>(qmap, p, n_rb, sq, bars, ring, rg, abort);
+        if (FP4 && warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if constexpr (FP4) {
+            unsigned char* raw = smem + C::kRawOffset;
+            if (warp == kKWarp) load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
+            else if (warp >= 12) widen_role<D, MODE>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
+        } else {
+            if (warp == kKWarp) load_role<D, MODE>(tmap, p, n_rb, sk, bars->k_full, bars->k_empty, 0, rg, &bars->k_full[0], &bars->bad, abort);
+            else if (warp == kVWarp) load_role<D, MODE>(tmap, p, n_rb, sv, bars->v_full, bars->v_empty, 1, rg, &bars->k_full[0], &bars->bad, abort);
+        }
+        if (warp == kMmaWarp) mma_role<D, MODE, FP4>(p, sq, sk, sv, bars, f4, ring, tmem, rg, abort);
+        else if (warp == kQWarp) q_role<D, MODE, FP4>(qmap, p, n_rb, sq, bars, ring, rg, abort);
         if (MODE == kTcCluster) cluster_sync_all();  // the cluster barrier of the merge counts every thread
     }
     // ---- common tail: everything of this CTA has completed, or it is giving up
@@ -1267,35 +1486,37 @@ struct TcState {
     int d, hkv;
     const CUtensorMap* current;
     const CUtensorMap* qcurrent;
-    int max_clusters[kMaxCluster + 1];  // [C]: clusters of C CTAs of the cluster kernel the device holds at once (0 = not launchable)
+    // per cache format (0: bf16, 1: FP4): set up by its first call
+    bool ready[2];
+    int max_clusters[2][kMaxCluster + 1];  // [C]: clusters of C CTAs of the cluster kernel the device holds at once (0 = not launchable)
 };
 
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 cudaError_t configure_kernel() {
-    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MODE>::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MODE, FP4>::kSmemBytes);
     if (e == cudaSuccess && MODE == kTcCluster)
-        e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FP4>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     return e;
 }
 
 // How many clusters of `c` CTAs of the cluster kernel can be resident together (0 if such a launch is refused).
-template <int D>
+template <int D, bool FP4>
 int query_clusters(int c, int n_sms) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((n_sms / c) * c);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Cfg<D, kTcCluster>::kSmemBytes;
+    cfg.blockDim = dim3(Cfg<D, kTcCluster, FP4>::kThreads);
+    cfg.dynamicSmemBytes = Cfg<D, kTcCluster, FP4>::kSmemBytes;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kTcCluster>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
+    if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kTcCluster, FP4>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
     return n;
 }
 
-template <int D, int MODE>
+template <int D, int MODE, bool FP4>
 void launch_mode(const TcState* st, const AttnParams& p, cudaStream_t s) {
     // Programmatic dependent launch: the CTAs may start while the previous launch on the stream (the plan kernel,
     // or the previous layer's call) is still running; they do their set-up and then wait for it inside the kernel.
@@ -1304,18 +1525,39 @@ void launch_mode(const TcState* st, const AttnParams& p, cudaStream_t s) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.n_ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(Cfg<D, MODE, FP4>::kThreads);
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cfg.dynamicSmemBytes = Cfg<D, MODE>::kSmemBytes;
+    cfg.dynamicSmemBytes = Cfg<D, MODE, FP4>::kSmemBytes;
     if (MODE == kTcCluster) {
         cfg.gridDim = dim3(p.batch * p.Hkv * p.cluster);  // one cluster per (sequence, kv-head) segment
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = p.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
-    cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, MODE>, *st->current, *st->qcurrent, p);
+    cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, MODE, FP4>, *st->current, *st->qcurrent, p);
+}
+
+template <int D, bool FP4>
+cudaError_t configure_format(TcState* st) {
+    cudaError_t e = configure_kernel<D, kTcPlanned, FP4>();
+    if (e == cudaSuccess) e = configure_kernel<D, kTcSelfPlanned, FP4>();
+    if (e == cudaSuccess) e = configure_kernel<D, kTcCluster, FP4>();
+    if (e != cudaSuccess) return e;
+    int n_sms = 0, dev = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev);
+    for (int c = 0; c <= kMaxCluster; ++c) st->max_clusters[FP4][c] = c >= 2 && cluster_fits(c, D, FP4) ? query_clusters<D, FP4>(c, n_sms) : 0;
+    st->ready[FP4] = true;
+    return cudaSuccess;
+}
+
+template <int D, bool FP4>
+void launch_format(const TcState* st, const AttnParams& p, int mode, cudaStream_t s) {
+    if (mode == kTcCluster) launch_mode<D, kTcCluster, FP4>(st, p, s);
+    else if (mode == kTcSelfPlanned) launch_mode<D, kTcSelfPlanned, FP4>(st, p, s);
+    else launch_mode<D, kTcPlanned, FP4>(st, p, s);
 }
 
 }  // namespace
@@ -1336,25 +1578,14 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
         cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", reinterpret_cast<void**>(&st->encode), cudaEnableDefault, &qres);
         if (e != cudaSuccess || !st->encode) { delete st; return e != cudaSuccess ? e : cudaErrorNotSupported; }
         st->d = p.d; st->hkv = p.Hkv;
-        if (p.d == 64) {
-            e = configure_kernel<64, kTcPlanned>();
-            if (e == cudaSuccess) e = configure_kernel<64, kTcSelfPlanned>();
-            if (e == cudaSuccess) e = configure_kernel<64, kTcCluster>();
-        } else {
-            e = configure_kernel<128, kTcPlanned>();
-            if (e == cudaSuccess) e = configure_kernel<128, kTcSelfPlanned>();
-            if (e == cudaSuccess) e = configure_kernel<128, kTcCluster>();
-        }
-        if (e != cudaSuccess) { delete st; return e; }
-        int n_sms = 0, dev = 0;
-        cudaGetDevice(&dev);
-        cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev);
-        for (int c = 0; c <= kMaxCluster; ++c) st->max_clusters[c] = 0;
-        for (int c = 2; c <= kMaxCluster; ++c) {
-            const bool fits = cluster_fits(c, p.d);
-            st->max_clusters[c] = !fits ? 0 : p.d == 64 ? query_clusters<64>(c, n_sms) : query_clusters<128>(c, n_sms);
-        }
+        st->ready[0] = st->ready[1] = false;
         *state = st;
+    }
+    const bool fp4 = p.kv4 != nullptr;
+    if (!st->ready[fp4]) {
+        const cudaError_t e = p.d == 64 ? (fp4 ? configure_format<64, true>(st) : configure_format<64, false>(st))
+                                        : (fp4 ? configure_format<128, true>(st) : configure_format<128, false>(st));
+        if (e != cudaSuccess) return e;
     }
     // q: a 3-D view [T][Hq][d], box = 64 elements x G q-heads (one kv-head) x q_box_t block rows
     st->qcurrent = st->q.find(p.q, p.total_q_rows);
@@ -1373,6 +1604,10 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
         e.n = p.total_q_rows;
         e.map = map;
         st->qcurrent = &e.map;
+    }
+    if (fp4) {  // pages come by untiled bulk copies: no map of the pool (the kernel's first map goes unused)
+        st->current = st->qcurrent;
+        return cudaSuccess;
     }
     st->current = st->kv.find(p.kv, p.num_pages);
     if (st->current) return cudaSuccess;
@@ -1398,26 +1633,19 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
 // CTAs per cluster for a call with one cluster per segment: the largest size (any, not only powers of two: a GPC holds
 // a limited number of clusters of each size) for which all clusters of the call are resident together, so every SM it
 // can use streams at once and a CTA has the fewest tiles; 0 if there is none.
-int attn_tc_cluster_size(const void* state, int n_segments, int n_sms) {
+int attn_tc_cluster_size(const void* state, bool fp4, int n_segments, int n_sms) {
     const TcState* st = static_cast<const TcState*>(state);
     if (!st || n_segments <= 0) return 0;
     for (int c = kMaxCluster; c >= 2; --c)
-        if (n_segments * c <= n_sms && st->max_clusters[c] >= n_segments) return c;
+        if (n_segments * c <= n_sms && st->max_clusters[fp4][c] >= n_segments) return c;
     return 0;
 }
 
 void launch_attn_tc(void* state, const AttnParams& p, int mode, cudaStream_t s) {
     if (p.batch == 0) return;
     const TcState* st = static_cast<const TcState*>(state);
-    if (p.d == 64) {
-        if (mode == kTcCluster) launch_mode<64, kTcCluster>(st, p, s);
-        else if (mode == kTcSelfPlanned) launch_mode<64, kTcSelfPlanned>(st, p, s);
-        else launch_mode<64, kTcPlanned>(st, p, s);
-    } else {
-        if (mode == kTcCluster) launch_mode<128, kTcCluster>(st, p, s);
-        else if (mode == kTcSelfPlanned) launch_mode<128, kTcSelfPlanned>(st, p, s);
-        else launch_mode<128, kTcPlanned>(st, p, s);
-    }
+    if (p.kv4) p.d == 64 ? launch_format<64, true>(st, p, mode, s) : launch_format<128, true>(st, p, mode, s);
+    else p.d == 64 ? launch_format<64, false>(st, p, mode, s) : launch_format<128, false>(st, p, mode, s);
 }
 
 void attn_tc_free(void* state) { delete static_cast<TcState*>(state); }

@@ -302,9 +302,9 @@ void launch_plan(const AttnParams& p, cudaStream_t s);
 cudaError_t attn_simt_prepare(int d);
 void launch_attn_simt(const AttnParams& p, cudaStream_t s);  // either cache: p.kv4 says which
 bool attn_tc_supported(int d, int G, int max_q_len);
-cudaError_t attn_tc_prepare(void** state, const AttnParams& p);  // tensor map for this kv pool
+cudaError_t attn_tc_prepare(void** state, const AttnParams& p);  // tensor maps of this call (either cache)
 void launch_attn_tc(void* state, const AttnParams& p, int mode, cudaStream_t s);  // mode: kTcPlanned, kTcSelfPlanned, kTcCluster
-int attn_tc_cluster_size(const void* state, int n_segments, int n_sms);    // CTAs per cluster for a call of n_segments, or 0
+int attn_tc_cluster_size(const void* state, bool fp4, int n_segments, int n_sms);  // CTAs per cluster for a call of n_segments, or 0
 void attn_tc_free(void* state);
 void launch_wait_timeout_selftest(int* status, unsigned long long limit_ns, cudaStream_t s);
 void launch_merge(const AttnParams& p, cudaStream_t s);
