@@ -54,6 +54,10 @@ using namespace sm100;
 
 namespace {
 
+// Warps that widen 4-bit tiles (4 or 8).
+#ifndef FD_WIDEN_WARPS
+#define FD_WIDEN_WARPS 8
+#endif
 // warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads (FP4: 8 loads both, 9 idle, 12-15 widen)
 constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10, kQWarp = 11;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
@@ -81,7 +85,14 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 
 template <int D, int MODE, bool FP4>
 struct Cfg {
-    static constexpr int kThreads = FP4 ? 512 : 384;     // FP4: warps 12-15 widen the tiles
+    static constexpr int kWidenWarps = FP4 ? FD_WIDEN_WARPS : 0;  // FP4: the warps behind warp 11 widen the tiles
+    static constexpr int kThreads = 384 + 32 * kWidenWarps;
+    // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps: the launch allocates 168 (no widening
+    // warps), 128 (four) or 96 (eight) to each, and what the groups take adds up to no more than that.
+    static constexpr int kRegSoftmax = !FP4 ? 224 : kWidenWarps == 4 ? 152 : 144;
+    static constexpr int kRegHelper = !FP4 || kWidenWarps == 4 ? 56 : 48;
+    static constexpr int kRegWiden = kWidenWarps == 4 ? 128 : 64;
+    static_assert(!FP4 || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * (kWidenWarps == 4 ? 128 : 96), "register split");
     // buffers in the K ring, and again in the V ring (FP4: of widened tiles, fed from the raw ring)
     static constexpr int kStages = FP4 ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
     static constexpr int kQBytes = kMaxRows * D * 2;
@@ -407,22 +418,33 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
 // share a token, so the reads are contiguous; of a 16-byte store's eight lanes -- two tokens, four chunks -- the
 // chunks of the upper half of d store their words in the order 2 3 0 1, which puts all eight on different banks.
 // ZERO_TAIL: tokens at or beyond `valid` become zeros (no token owns them: they may hold a NaN, and 0 * NaN is not 0).
+constexpr int kWidenThreads = 32 * FD_WIDEN_WARPS;
+
 template <int D, bool ZERO_TAIL>
 __device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned char* tile, int valid) {
     constexpr int kChunks = D / 32;        // 32-element chunks of a token
+    constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
     constexpr int kRawPage = 2 * fp4_page_bytes(D);
     constexpr int kHalves = D / 64;
-    const int t = threadIdx.x & 127, c = t % kChunks;
+    const int t = (int)threadIdx.x - 384, c = t % kChunks;
+    const bool swap = kHalves == 2 && (c & 2);
+    uint4 codes[kPasses];                  // all reads go out first: a store orders the reads behind it
+    uint32_t sc[kPasses];
 #pragma unroll
-    for (int it = 0; it < kChunks; ++it) { // 128 threads x 1 chunk per pass, kTileTokens * kChunks chunks
-        const int tok = t / kChunks + it * (128 / kChunks);
+    for (int it = 0; it < kPasses; ++it) {
+        const int tok = t / kChunks + it * (kWidenThreads / kChunks);
         const unsigned char* page = raw + (tok >> 4) * kRawPage;
-        const uint4 codes = *reinterpret_cast<const uint4*>(page + (tok & 15) * (D / 2) + c * 16);
-        const uint32_t sc = e4m3x2_to_half(*reinterpret_cast<const uint16_t*>(page + fp4_scale_offset(D) + (tok & 15) * (D / 16) + c * 2));
-        const __half2 s_lo = __half2half2(__low2half(as_half2(sc))), s_hi = __half2half2(__high2half(as_half2(sc)));
+        codes[it] = *reinterpret_cast<const uint4*>(page + (tok & 15) * (D / 2) + c * 16);
+        sc[it] = *reinterpret_cast<const uint16_t*>(page + fp4_scale_offset(D) + (tok & 15) * (D / 16) + c * 2);
+    }
+#pragma unroll
+    for (int it = 0; it < kPasses; ++it) {
+        const int tok = t / kChunks + it * (kWidenThreads / kChunks);
+        const __half2 s2 = as_half2(e4m3x2_to_half((uint16_t)sc[it]));
+        const __half2 s_lo = __half2half2(__low2half(s2)), s_hi = __half2half2(__high2half(s2));
         const bool dead = ZERO_TAIL && tok >= valid;
-        const bool swap = kHalves == 2 && (c & 2);
-        const uint32_t wd[4] = {swap ? codes.z : codes.x, swap ? codes.w : codes.y, swap ? codes.x : codes.z, swap ? codes.y : codes.w};
+        const uint4 cd = codes[it];
+        const uint32_t wd[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
         const __half2 s01 = swap ? s_hi : s_lo, s23 = swap ? s_lo : s_hi;
         unsigned char* row = tile + (tok >> 3) * (kHalves * 1024) + (c >> 1) * 1024 + (tok & 7) * 128;
 #pragma unroll
@@ -437,36 +459,47 @@ __device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned ch
     }
 }
 
-// The Q tile of a piece, bf16 -> fp16 in place, a thread a row.  A row is multiplied by the power of two that brings its
+// The Q tile of a piece, bf16 -> fp16 in place, kPer neighbouring threads a row (of two, the second starts at unit 4 of its
+// part: its words then lie on the other banks).  A row is multiplied by the power of two that brings its
 // largest element into [2^14, 2^15): bf16's 8 bits then fit fp16 exactly down to 2^-31 of that element (below, the loss is
 // smaller than what the fp32 sum of the score drops), and the factor goes into the scale of the row's scores.
 template <int D>
 __device__ __forceinline__ void q_to_half(unsigned char* sq, float* row_scale, float scale_log2e) {
-    const int r = threadIdx.x & 127;
-    unsigned char* row = sq + r * 128;
+    constexpr int kPer = kWidenThreads / kMaxRows, kUnits = D / 8 / kPer;  // 16-byte units of a row, per thread
+    static_assert(kPer == 1 || kPer == 2, "128 or 256 widening threads");
+    const int t = (int)threadIdx.x - 384, r = t / kPer, part = t % kPer;
+    auto at = [&](int i) -> uint4* {  // the thread's i-th unit
+        const int u = part * kUnits + (kPer == 2 && part && kUnits >= 8 ? i ^ 4 : i);
+        return reinterpret_cast<uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4));
+    };
     uint32_t mx = 0;
 #pragma unroll
-    for (int u = 0; u < D / 8; ++u) {
-        const uint4 v = *reinterpret_cast<const uint4*>(row + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4));
+    for (int i = 0; i < kUnits; ++i) {
+        const uint4 v = *at(i);
         mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
     }
+    if (kPer == 2) mx = __vmaxu2(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);  // biased exponent of the largest magnitude
     const float f = __uint_as_float((uint32_t)(127 + 141 - e) << 23);  // 2^(141 - e), e in [14, 255]
 #pragma unroll
-    for (int u = 0; u < D / 8; ++u) {
-        uint4* at = reinterpret_cast<uint4*>(row + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4));
-        uint4 v = *at;
-        uint32_t* wd = reinterpret_cast<uint32_t*>(&v);
+    for (int i0 = 0; i0 < kUnits; i0 += 4) {  // four words in flight: a store in place orders the loads behind it
+        uint4 v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            wd[k] = as_u32(__floats2half2_rn(__uint_as_float(wd[k] << 16) * f, __uint_as_float(wd[k] & 0xffff0000u) * f));
-        *at = v;
+        for (int i = 0; i < 4; ++i) v[i] = *at(i0 + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t* wd = reinterpret_cast<uint32_t*>(&v[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                wd[k] = as_u32(__floats2half2_rn(__uint_as_float(wd[k] << 16) * f, __uint_as_float(wd[k] & 0xffff0000u) * f));
+            *at(i0 + i) = v[i];
+        }
     }
     // never 0 (a hidden score is -inf, and 0 * -inf is not): a score of at most 2^35 times 2^-126 is 0 for every purpose
-    row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 141)), 1.17549435e-38f), 3.4028234e38f);
+    if (part == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 141)), 1.17549435e-38f), 3.4028234e38f);
 }
 
-// FP4: warps 12-15.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
+// FP4: the widening warps.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
 // is widened before its Q is touched, while that Q is still on its way.
 template <int D, int MODE>
 __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv,
@@ -849,6 +882,111 @@ __device__ __forceinline__ uint32_t pack16(float2 v) {
     return *reinterpret_cast<const uint32_t*>(&b);
 }
 
+// One row of a tile in the FP4 kernel, whose softmax warps have fewer registers than a whole row of S takes.  The common
+// case goes over S once, 32 columns at a time, and forms the weights against the running maximum as it stands; they
+// are kept -- packed, half the size of the scores -- if the tile's own maximum then turns out not to pass it by more than
+// the threshold.  Otherwise, and in the first tile of a piece (no maximum yet) and the tiles the mask cuts, S is gone
+// over twice: for the maximum, then for the weights, written as they are formed (a chunk's weights only ever land on
+// scores that have been read).
+template <int D>
+__device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_addr, float c, float head, bool masked, int lim, int blo, int bhi,
+                                                 bool first, float& m, float& l) {
+    auto take_max = [&](const uint32_t (&sv)[32], float& a, float& b) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+            a = max3(a, __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
+            b = max3(b, __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
+        }
+    };
+    auto weights = [&](const uint32_t (&x)[32], float2 c2, float2 nm2, float2& sum0, float2& sum1, uint32_t* pk) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+            const float2 xa = __ffma2_rn(make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, nm2);
+            const float2 xb = __ffma2_rn(make_float2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), c2, nm2);
+            const float2 pa = make_float2(ex2_approx(xa.x), ex2_approx(xa.y)), pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
+            sum0 = __fadd2_rn(sum0, pa);
+            sum1 = __fadd2_rn(sum1, pb);
+            pk[k >> 1] = pack16<true>(pa);
+            pk[(k >> 1) + 1] = pack16<true>(pb);
+        }
+    };
+    const float2 c2 = make_float2(c, c);
+    bool slow = masked || __any_sync(0xffffffffu, first || m == -INFINITY);  // (warp-uniform: masked is)
+    if (!slow) {
+        const float2 nm2 = make_float2(-m, -m);
+        float a = -INFINITY, b = -INFINITY;
+        float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+        uint32_t pk[2][32], sv[2][32];
+        tmem_ld32(s_addr, sv[0]);
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+            tc_wait_ld();
+            if (ch < 3) tmem_ld32(s_addr + (ch + 1) * 32, sv[(ch + 1) & 1]);
+            take_max(sv[ch & 1], a, b);
+            weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 1][(ch & 1) * 16]);
+        }
+        slow = __any_sync(0xffffffffu, fmaxf(a, b) * c - head > m + kRescaleThreshold);
+        if (!slow) {
+            tmem_st32(s_addr, pk[0]);
+            tmem_st32(s_addr + 32, pk[1]);
+            l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+        }
+    }
+    if (slow) {
+        auto low_bits = [](int n) -> uint32_t { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
+        auto load = [&](int ch, uint32_t (&sv)[32]) {
+            tmem_ld32(s_addr + ch * 32, sv);
+            tc_wait_ld();
+            if (masked) {  // the columns of the chunk the row sees, as a bit each
+                const uint32_t vis = low_bits(lim - ch * 32) | (low_bits(bhi - ch * 32) & ~low_bits(blo - ch * 32));
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (!((vis >> k) & 1u)) sv[k] = 0xff800000u;  // -inf by select: S may be NaN there
+            }
+        };
+        float a = -INFINITY, b = -INFINITY;
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {
+            uint32_t sv[32];
+            load(ch, sv);
+            take_max(sv, a, b);
+        }
+        const float m_new = fmaxf(a, b) * c - head;
+        float alpha = 1.f;
+        if (first || m == -INFINITY) {
+            m = m_new;  // nothing accumulated yet (O is overwritten, or exactly zero)
+        } else if (m_new > m + kRescaleThreshold) {
+            alpha = exp2f(m - m_new);
+            m = m_new;
+        }
+        if (__any_sync(0xffffffffu, alpha != 1.f)) {
+            // the previous P V of this stream has completed (the reuse of S and P orders it), so O is quiescent
+#pragma unroll 1
+            for (int ch = 0; ch < D / 16; ++ch) {
+                uint32_t o[16];
+                tmem_ld16(o_addr + ch * 16, o);
+                tc_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                tmem_st16(o_addr + ch * 16, o);
+            }
+            l *= alpha;
+        }
+        const float mc = (m == -INFINITY) ? 0.f : m;
+        const float2 nm2 = make_float2(-mc, -mc);
+        float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {
+            uint32_t sv[32], pk[16];
+            load(ch, sv);
+            weights(sv, c2, nm2, sum0, sum1, pk);
+            tmem_st16(s_addr + ch * 16, pk);
+        }
+        l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+    }
+    tc_wait_st();
+}
+
 // The two softmax groups (256 threads).
 template <int D, int MODE, bool FP4>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, float* ex, int* s_cs, const CtaStarts cs, const Piece* ring,
@@ -905,6 +1043,9 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 const int lim = rm.limit - pos0, blo = rm.blk_lo - pos0, bhi = rm.blk_hi - pos0;
                 const uint32_t s_addr = tmem + lane_base + col_s[s];
 
+                if constexpr (FP4) {
+                    softmax_tile_fp4<D>(s_addr, tmem + lane_base + col_o[s], c, kHead, masked, lim, blo, bhi, j < 2, m, l);
+                } else {
                 // ---- the whole row of S in one round trip: TMEM loads queue behind the MMAs in flight,
                 //      so every ld -> wait pair costs up to one MMA tile; registers come from setmaxnreg
                 uint32_t sv[4][32];
@@ -972,6 +1113,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tc_wait_st();
+                }
             }
             tc_fence_before();
             mbar_arrive(&bars->p_full[s]);
@@ -1294,12 +1436,12 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
     //      griddepcontrol.wait below is where that launch's results are needed
     if (warp == 1 && lane == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(&bars->k_full[i], FP4 ? 4 : 1); mbar_init(&bars->k_empty[i], 1);  // FP4: the four widening warps
-            mbar_init(&bars->v_full[i], FP4 ? 4 : 1); mbar_init(&bars->v_empty[i], 1);
+            mbar_init(&bars->k_full[i], FP4 ? C::kWidenWarps : 1); mbar_init(&bars->k_empty[i], 1);  // FP4: the widening warps
+            mbar_init(&bars->v_full[i], FP4 ? C::kWidenWarps : 1); mbar_init(&bars->v_empty[i], 1);
         }
         if (FP4) {
-            for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], 4); }
-            mbar_init(&f4->q_ready, 4);
+            for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], C::kWidenWarps); }
+            mbar_init(&f4->q_ready, C::kWidenWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
@@ -1424,13 +1566,14 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         // Warp-specialised register budgets: the softmax groups keep a whole 128-column row of S in registers.
         // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168, what the launch allocated: the increase is served exactly by what
         // the decrease released (a request for more than that does not return).
-        // FP4: 8 x 32 x 184 + 4 x 32 x 56 + 4 x 32 x 88 = 512 x 128, likewise.
-        if (FP4) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        // FP4: see Cfg.
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegSoftmax));
         softmax_role<D, MODE, FP4>(p, bars, ex, s_cs, cs, ring, tmem, rg, exch, cl_rank, sq, sv, f4, abort);
     } else {
-        if (FP4 && warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (FP4 && warp >= 12) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegWiden));
+        }
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegHelper));
         if constexpr (FP4) {
             unsigned char* raw = smem + C::kRawOffset;
             if (warp == kKWarp) load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
