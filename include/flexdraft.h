@@ -381,7 +381,7 @@ fd_status fd_qk_norm_rope_append(fd_ctx* ctx, int total_q_rows, const void* qkv,
  *     scale = the e4m3 number nearest to max_i |x_i / k_scale| / 6, at most 448         (nearest, ties to even)
  *     code  = the e2m1 number whose multiple of the scale is nearest to x / k_scale      (nearest, ties to even; 6 at most)
  *
- * A NaN is held as 0, an infinity as the largest value of its group's scale.  Zero scale: all codes of the group are 0.
+ * A NaN is held as 0, an infinity as the largest value of its group's scale.  Zero scale: all codes of the group are zeros.
  *
  *   cache layout    [num_pages, Hkv, 2, P * (d / 2 + d / 16)] bytes, 16-byte aligned: for each page and kv-head K then V,
  *                   each as [P][d / 2] bytes of codes (element 2 i in the low half of byte i) followed by [P][d / 16]

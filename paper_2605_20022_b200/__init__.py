@@ -2,7 +2,8 @@
 
 Every function has the name and the argument order of its C entry point in
 ``include/flexdraft.h``; tensors are torch CUDA tensors whose ``data_ptr()`` is
-handed through unchanged.  All arithmetic runs inside the library's CUDA kernels.
+handed through unchanged (by ctypes, or for the calls made several times per layer by the
+native ``_marshal``).  All arithmetic runs inside the library's CUDA kernels.
 If the library has not been built, or no CUDA device is present, the calls raise:
 there is no fallback path.
 """
@@ -46,6 +47,7 @@ class FlexDraftError(RuntimeError):
 
 
 _lib = None
+_native = None  # the _marshal extension, bound to the loaded library
 
 
 def library_path() -> str:
@@ -54,7 +56,7 @@ def library_path() -> str:
 
 def load() -> ctypes.CDLL:
     """dlopen libflexdraft.so (built in-tree by ``_build.build()``); raises if it is missing."""
-    global _lib
+    global _lib, _native
     if _lib is None:
         if not os.path.exists(_build.SO):
             raise FileNotFoundError(f"{_build.SO} is not built: run `python -m paper_2605_20022_b200._build`")
@@ -80,12 +82,6 @@ def load() -> ctypes.CDLL:
         lib.fd_draft_select.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
         lib.fd_step_host.argtypes = [vp, ci, ci, ci, ci, ctypes.POINTER(vp), ci] + [vp] * 14
         lib.fd_step_host_append.argtypes = [vp, ci, ci, ci, ci, ctypes.POINTER(vp), ci] + [vp] * 16
-        cf = ctypes.c_float
-        lib.fd_kv_reserve.argtypes = [vp, ci, ci] + [vp] * 10 + [ci, vp, vp, vp]
-        lib.fd_qk_norm_rope_append.argtypes = [vp, ci, vp, ctypes.c_int64, vp, vp, cf, vp, ci, ci, ci, vp, vp, vp, vp, ci, ci, cf, cf, vp]
-        lib.fd_kv_append_fp4.argtypes = [vp, ci, ci, vp, vp, vp, ci, vp, vp, vp, cf, cf, vp]
-        lib.fd_kv_read_fp4.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, cf, cf, vp, vp, vp]
-        lib.fd_attn_draft_verify_fp4.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, cf, cf, vp, vp]
         lib.fd_last_device_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), vp]
         lib.fd_attn_path.argtypes = [vp]
         lib.fd_attn_last_mode.argtypes = [vp]
@@ -93,8 +89,18 @@ def load() -> ctypes.CDLL:
         lib.fd_launch_count.restype = ctypes.c_int64
         lib.fd_status_string.argtypes = [ci]
         lib.fd_status_string.restype = ctypes.c_char_p
+        if not os.path.exists(_build.MARSHAL):
+            raise FileNotFoundError(f"{_build.MARSHAL} is not built: run `python -m paper_2605_20022_b200._build`")
+        from . import _marshal
+        _marshal.bind(_build.SO)
+        _native = _marshal
         _lib = lib
     return _lib
+
+
+def _load_native():
+    load()
+    return _native
 
 
 def status_string(code: int) -> str:
@@ -109,10 +115,24 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_current_stream = None  # () -> cudaStream_t of torch's current stream, as an int
+
+
+def _find_current_stream():
+    global _current_stream
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    torch.cuda.init()
+    if raw is not None and device is not None:  # what torch.cuda.current_stream() calls, without the object around it
+        _current_stream = lambda: raw(device())
+    else:
+        _current_stream = lambda: torch.cuda.current_stream().cuda_stream
+    return _current_stream
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        return (_current_stream or _find_current_stream())() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -192,41 +212,40 @@ def fd_kv_append(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, pa
 
 def fd_kv_reserve(ctx, batch, total_q_rows, page_table, prefix_lens, q_lens, n_mask, n_blocks, freed_pages, n_freed, free_pages,
                   n_free, n_free_out, num_pages, slot_map, positions, stream=None, raise_on_error=True) -> int:
-    code = load().fd_kv_reserve(ctx, batch, total_q_rows, _ptr(page_table), _ptr(prefix_lens), _ptr(q_lens), _ptr(n_mask),
-                                _ptr(n_blocks), _ptr(freed_pages), _ptr(n_freed), _ptr(free_pages), _ptr(n_free), _ptr(n_free_out),
-                                num_pages, _ptr(slot_map), _ptr(positions), _stream(stream))
-    return _check("fd_kv_reserve", code, raise_on_error)
+    code = (_native or _load_native()).fd_kv_reserve(ctx, batch, total_q_rows, page_table, prefix_lens, q_lens, n_mask, n_blocks,
+                                                     freed_pages, n_freed, free_pages, n_free, n_free_out, num_pages, slot_map,
+                                                     positions, _stream(stream))
+    return _check("fd_kv_reserve", code, raise_on_error) if code else code
 
 
 def fd_qk_norm_rope_append(ctx, total_q_rows, qkv, row_stride, q_weight, k_weight, eps, cos_sin, max_positions, rot_dim, rope_style,
                            positions, slot_map, q_out, kv_cache, num_pages, kv_format=FD_KV_BF16, k_scale=1.0, v_scale=1.0, stream=None,
                            raise_on_error=True) -> int:
-    code = load().fd_qk_norm_rope_append(ctx, total_q_rows, _ptr(qkv), row_stride, _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos_sin),
-                                         max_positions, rot_dim, rope_style, _ptr(positions), _ptr(slot_map), _ptr(q_out),
-                                         _ptr(kv_cache), num_pages, kv_format, k_scale, v_scale, _stream(stream))
-    return _check("fd_qk_norm_rope_append", code, raise_on_error)
+    code = (_native or _load_native()).fd_qk_norm_rope_append(ctx, total_q_rows, qkv, row_stride, q_weight, k_weight, eps, cos_sin,
+                                                              max_positions, rot_dim, rope_style, positions, slot_map, q_out, kv_cache,
+                                                              num_pages, kv_format, k_scale, v_scale, _stream(stream))
+    return _check("fd_qk_norm_rope_append", code, raise_on_error) if code else code
 
 
 def fd_kv_append_fp4(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale=1.0,
                      v_scale=1.0, stream=None, raise_on_error=True) -> int:
-    code = load().fd_kv_append_fp4(ctx, batch, total_q_rows, _ptr(k_new), _ptr(v_new), _ptr(kv_cache), num_pages, _ptr(page_table),
-                                   _ptr(prefix_lens), _ptr(q_lens), k_scale, v_scale, _stream(stream))
-    return _check("fd_kv_append_fp4", code, raise_on_error)
+    code = (_native or _load_native()).fd_kv_append_fp4(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table,
+                                                        prefix_lens, q_lens, k_scale, v_scale, _stream(stream))
+    return _check("fd_kv_append_fp4", code, raise_on_error) if code else code
 
 
 def fd_kv_read_fp4(ctx, batch, total_q_rows, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale, v_scale, k_out, v_out,
                    stream=None, raise_on_error=True) -> int:
-    code = load().fd_kv_read_fp4(ctx, batch, total_q_rows, _ptr(kv_cache), num_pages, _ptr(page_table), _ptr(prefix_lens), _ptr(q_lens),
-                                 k_scale, v_scale, _ptr(k_out), _ptr(v_out), _stream(stream))
-    return _check("fd_kv_read_fp4", code, raise_on_error)
+    code = (_native or _load_native()).fd_kv_read_fp4(ctx, batch, total_q_rows, kv_cache, num_pages, page_table, prefix_lens, q_lens,
+                                                      k_scale, v_scale, k_out, v_out, _stream(stream))
+    return _check("fd_kv_read_fp4", code, raise_on_error) if code else code
 
 
 def fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, q, kv_cache, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
                              k_scale, v_scale, out, stream=None, raise_on_error=True) -> int:
-    code = load().fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, _ptr(q), _ptr(kv_cache), num_pages, _ptr(page_table),
-                                           _ptr(prefix_lens), _ptr(q_lens), _ptr(n_mask), _ptr(n_blocks), k_scale, v_scale, _ptr(out),
-                                           _stream(stream))
-    return _check("fd_attn_draft_verify_fp4", code, raise_on_error)
+    code = (_native or _load_native()).fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, q, kv_cache, num_pages, page_table, prefix_lens,
+                                                                q_lens, n_mask, n_blocks, k_scale, v_scale, out, _stream(stream))
+    return _check("fd_attn_draft_verify_fp4", code, raise_on_error) if code else code
 
 
 def fd_kv_fp4_page_bytes(head_dim: int, page_size: int = 16) -> int:

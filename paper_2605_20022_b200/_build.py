@@ -1,13 +1,17 @@
-"""Compile libflexdraft.so (all CUDA kernels + the C ABI) for sm_100a with nvcc, in-tree."""
+"""Compile libflexdraft.so (all CUDA kernels + the C ABI) for sm_100a with nvcc, and the binding's native argument
+marshalling with gcc, in-tree."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libflexdraft.so")
+MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.c")
+MARSHAL = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-shared"]
 
@@ -24,8 +28,18 @@ def _stale() -> bool:
     return any(os.path.getmtime(f) > t for f in deps)
 
 
+def build_marshal(force: bool = False) -> str:
+    """The native argument marshalling of the binding (a CPython extension, no CUDA).  Returns its path."""
+    if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < os.path.getmtime(MARSHAL_SRC):
+        tmp = MARSHAL + f".tmp{os.getpid()}"
+        subprocess.run(["gcc", "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-o", tmp, MARSHAL_SRC, "-ldl"], check=True)
+        os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Build if the library is missing or older than a source.  Returns its path."""
+    build_marshal(force)
     if force or _stale():
         nvcc = os.environ.get("NVCC", "nvcc")
         tmp = SO + f".tmp{os.getpid()}"

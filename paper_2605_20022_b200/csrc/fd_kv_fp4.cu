@@ -1,7 +1,9 @@
 // K and V of the query block into the 4-bit cache and out of it.
 //
 // A thread owns one scale group: 16 elements, 32 bytes of bf16 on one side, 8 bytes of codes and a scale byte on the other.
-// Neighbouring threads own neighbouring groups of a row, so both sides are contiguous across a warp.
+// Neighbouring threads own neighbouring groups of a row, so both sides are contiguous across a warp.  A CTA takes a run of
+// rows: first a thread per row finds the row's sequence and page (a search and a dependent load), then all threads stream
+// the run's groups with nothing but loads and stores between them.
 #include <algorithm>
 
 #include "fd_fp4.cuh"
@@ -15,6 +17,7 @@ constexpr int kThreads = 256;
 
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxBatch = 4096;  // what fd_create allows
+constexpr int kRun = 64;         // most rows of a run
 
 // Exclusive scan of the query lengths into cu[0 .. B] (negative lengths count as 0, sums beyond 32 bits saturate).
 __device__ __forceinline__ void scan_lengths(const int32_t* q_lens, int B, int* cu, long long* wsum) {
@@ -41,99 +44,149 @@ __device__ __forceinline__ void scan_lengths(const int32_t* q_lens, int B, int* 
     __syncthreads();
 }
 
-// The sequence that owns query row `row`: the last b with cu[b] <= row (a whole warp; 32 probes a round, at most three rounds).
-__device__ __forceinline__ int owner_of_row(const int* cu, int B, long long row) {
-    int lo = 0, n = B;  // the answer lies in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + 31) / 32, at = lo + (int)(threadIdx.x & 31) * step;
-        const unsigned below = __ballot_sync(0xffffffffu, at < lo + n && cu[min(at, B)] <= row);
-        const int k = 31 - __clz(below | 1u);
-        lo += k * step;
-        n = min(step, n - k * step);
-    }
-    return lo;
-}
-
-__device__ __forceinline__ void load_group(const __nv_bfloat16* src, float by, float (&x)[kFp4Group]) {
-    __align__(16) __nv_bfloat16 e[kFp4Group];
-    reinterpret_cast<uint4*>(e)[0] = reinterpret_cast<const uint4*>(src)[0];
-    reinterpret_cast<uint4*>(e)[1] = reinterpret_cast<const uint4*>(src)[1];
-#pragma unroll
-    for (int k = 0; k < kFp4Group; ++k) x[k] = __fdiv_rn(__bfloat162float(e[k]), by);
-}
-
 }  // namespace
 
 template <bool READ>
-__global__ void __launch_bounds__(kThreads) kv_rows_fp4_kernel(Fp4RowsParams p) {
+__global__ void __launch_bounds__(kThreads, READ ? 4 : 3) kv_rows_fp4_kernel(Fp4RowsParams p, int run, unsigned per_row_inv) {
     __shared__ int cu[kMaxBatch + 1];
     __shared__ long long wsum[kWarps];
-    const int tid = threadIdx.x, lane = tid & 31;
+    __shared__ long long s_page[kRun];  // where the row's page starts in the cache; -1: no page to read or write
+    __shared__ int s_tok[kRun];         // its token there
+    const int tid = threadIdx.x;
     scan_lengths(p.q_lens, p.batch, cu, wsum);
-    const int groups = p.d / kFp4Group, per_row = p.Hkv * groups;  // of K, and again of V
+    const int g_shift = p.d == 64 ? 2 : 3, per_row = p.Hkv << g_shift;  // groups of K, and again of V
+    const int page_bytes = fp4_page_bytes(p.d);
     const long long rows = min(cu[p.batch], p.total_rows);
-    bool bad_page = false;
     if (blockIdx.x == 0)  // a sequence that is skipped: the status alone (its rows are met below, by whoever owns them)
         for (int b = tid; b < p.batch; b += kThreads) {
             const long long n = p.prefix_lens[b], Lq = p.q_lens[b];
             if (Lq > 0 && (n < 0 || cu[b] + Lq > p.total_rows || n + Lq > (long long)p.max_pages * 16)) atomicOr(p.status, FD_DEV_BAD_LENGTHS);
         }
-    for (long long row = (long long)blockIdx.x * kWarps + (tid >> 5); row < rows; row += (long long)gridDim.x * kWarps) {  // a warp a row
-        const int b = owner_of_row(cu, p.batch, row);
-        const int n = p.prefix_lens[b], Lq = p.q_lens[b];
-        const bool skip = n < 0 || (long long)cu[b] + Lq > p.total_rows || (long long)n + Lq > (long long)p.max_pages * 16;
-        if (skip && !READ) continue;
-        const int j = skip ? 0 : n + (int)(row - cu[b]);
-        const int page = skip ? -1 : p.page_table[(long long)b * p.max_pages + (j >> 4)];
-        const bool ok = (unsigned)page < (unsigned)p.num_pages;  // never form an address from a bad id
-        bad_page = bad_page || (!ok && !skip);
-        for (int e = lane; e < 2 * per_row; e += 32) {
-            const int which = e / per_row, h = e % per_row / groups, g = e % groups;
-            __nv_bfloat16* rowp = (which ? p.v : p.k) + (row * p.Hkv + h) * p.d + g * kFp4Group;
-            const float by = which ? p.v_scale : p.k_scale;
-            if (!ok) {
-                if (READ) {
-                    reinterpret_cast<uint4*>(rowp)[0] = make_uint4(0, 0, 0, 0);
-                    reinterpret_cast<uint4*>(rowp)[1] = make_uint4(0, 0, 0, 0);
-                }
-                continue;
+    const Fp4Quantiser by_k(p.k_scale), by_v(p.v_scale);
+    for (long long r0 = (long long)blockIdx.x * run; r0 < rows; r0 += (long long)gridDim.x * run) {
+        const int n_rows = (int)min((long long)run, rows - r0);
+        __syncthreads();  // the run before has been worked through
+        if (tid < n_rows) {
+            const long long row = r0 + tid;
+            int lo = 0, hi = p.batch;  // the sequence that owns the row: the last one that starts at or before it
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (cu[mid] <= row) lo = mid; else hi = mid;
             }
-            unsigned char* base = p.kv4 + fp4_page_offset(page, p.Hkv, h, which, p.d);
-            uint2* codes = reinterpret_cast<uint2*>(base + (j & 15) * (p.d / 2) + g * 8);
-            unsigned char* scale = base + fp4_scale_offset(p.d) + (j & 15) * groups + g;
-            if (READ) {
-                const uint2 c = *codes;
-                const float s = e4m3_to_float(*scale);
-                uint32_t h4[2][4];
-                e2m1x8_to_half(c.x, h4[0]);
-                e2m1x8_to_half(c.y, h4[1]);
-                __align__(16) __nv_bfloat162 v[8];
+            const int n = p.prefix_lens[lo], Lq = p.q_lens[lo];
+            long long at = -1;
+            int tok = 0;
+            if (n >= 0 && (long long)cu[lo] + Lq <= p.total_rows && (long long)n + Lq <= (long long)p.max_pages * 16) {
+                const int j = n + (int)(row - cu[lo]);
+                const int page = p.page_table[(long long)lo * p.max_pages + (j >> 4)];
+                tok = j & 15;
+                if ((unsigned)page < (unsigned)p.num_pages) at = fp4_page_offset(page, p.Hkv, 0, 0, p.d);  // never form an address from a bad id
+                else atomicOr(p.status, FD_DEV_BAD_PAGE);
+            }
+            s_page[tid] = at;
+            s_tok[tid] = tok;
+        }
+        __syncthreads();
+        const int items = n_rows * 2 * per_row;
+        auto locate = [&](int e, bool& ok, int& which, __nv_bfloat16*& rowp, unsigned char*& codes, unsigned char*& scale) {
+            const int i = (int)__umulhi((unsigned)e, per_row_inv), rem = e - i * 2 * per_row;  // row of the run, group of the row
+            which = rem >= per_row;
+            const int hg = rem - which * per_row, h = hg >> g_shift, g = hg & ((1 << g_shift) - 1);
+            const long long at = s_page[i];
+            const int tok = s_tok[i];
+            ok = at >= 0;
+            rowp = (which ? p.v : p.k) + ((r0 + i) * per_row + hg) * kFp4Group;
+            unsigned char* base = p.kv4 + at + (h * 2 + which) * page_bytes;
+            codes = base + tok * (p.d / 2) + g * 8;
+            scale = base + fp4_scale_offset(p.d) + (tok << g_shift) + g;
+        };
+        constexpr int U = READ ? 4 : 2;  // items in flight per thread
+        for (int e0 = tid; e0 < items; e0 += U * kThreads) {
+            bool ok[U];
+            int which[U];
+            __nv_bfloat16* rowp[U];
+            unsigned char *codes[U], *scale[U];
+            uint4 raw[U][READ ? 1 : 2];
+            unsigned char sb[U];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float2 f = __half22float2(as_half2(h4[k >> 2][k & 3]));  // f * s is exact: one rounding, by the product with `by`
-                    v[k] = __floats2bfloat162_rn(f.x * s * by, f.y * s * by);
+            for (int u = 0; u < U; ++u) {
+                const int e = min(e0 + u * kThreads, items - 1);  // (past the end: the last item again)
+                locate(e, ok[u], which[u], rowp[u], codes[u], scale[u]);
+                if (READ) {
+                    raw[u][0] = make_uint4(0, 0, 0, 0);
+                    sb[u] = 0;
+                    if (ok[u]) {
+                        const uint2 c = *reinterpret_cast<const uint2*>(codes[u]);
+                        raw[u][0].x = c.x; raw[u][0].y = c.y;
+                        sb[u] = *scale[u];
+                    }
+                } else if (ok[u]) {
+                    raw[u][0] = reinterpret_cast<const uint4*>(rowp[u])[0];
+                    raw[u][READ ? 0 : 1] = reinterpret_cast<const uint4*>(rowp[u])[1];
                 }
-                reinterpret_cast<uint4*>(rowp)[0] = reinterpret_cast<const uint4*>(v)[0];
-                reinterpret_cast<uint4*>(rowp)[1] = reinterpret_cast<const uint4*>(v)[1];
-            } else {
-                float x[kFp4Group], amax = 0.f;
-                load_group(rowp, by, x);
+            }
 #pragma unroll
-                for (int k = 0; k < kFp4Group; ++k) amax = fmaxf(amax, fabsf(x[k]));  // (fmaxf drops a NaN)
-                const uint8_t sb = e4m3_scale(amax);
-                const Fp4Thresholds th(e4m3_to_float(sb));
-                *codes = make_uint2(e2m1_code8(x, th), e2m1_code8(x + 8, th));
-                *scale = sb;
+            for (int u = 0; u < U; ++u) {
+                if (e0 + u * kThreads >= items) break;
+                if (READ) {  // (no page: codes and scale of zero)
+                    const float m = which[u] ? by_v.by : by_k.by;
+                    const __half2 f = __half2half2(__low2half(as_half2(e4m3x2_to_half(sb[u]))));
+                    uint32_t h4[2][4];
+                    e2m1x8_to_half(raw[u][0].x, h4[0]);
+                    e2m1x8_to_half(raw[u][0].y, h4[1]);
+                    __align__(16) __nv_bfloat162 v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float2 c = __half22float2(__hmul2(as_half2(h4[k >> 2][k & 3]), f));  // code * scale is exact in fp16
+                        v[k] = __floats2bfloat162_rn(c.x * m, c.y * m);
+                    }
+                    reinterpret_cast<uint4*>(rowp[u])[0] = reinterpret_cast<const uint4*>(v)[0];
+                    reinterpret_cast<uint4*>(rowp[u])[1] = reinterpret_cast<const uint4*>(v)[1];
+                } else if (ok[u]) {
+                    float x[kFp4Group], amax = 0.f;
+                    const __nv_bfloat162* e2 = reinterpret_cast<const __nv_bfloat162*>(raw[u]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float2 f = __bfloat1622float2(e2[k]);
+                        x[2 * k] = f.x;
+                        x[2 * k + 1] = f.y;
+                    }
+                    Fp4Quantiser by = by_k;
+                    if (which[u]) by = by_v;
+#pragma unroll
+                    for (int k = 0; k < kFp4Group; ++k) amax = max_nan(amax, fabsf(x[k]));
+                    Fp4Scale g;
+                    uint2 w;
+                    if (!by.odd(amax)) {
+                        g = by.scale(amax);
+                        w = make_uint2(by.codes<8>(x, g), by.codes<8>(x + 8, g));
+                    } else {
+                        amax = 0.f;
+#pragma unroll
+                        for (int k = 0; k < kFp4Group; ++k) amax = fmaxf(amax, fabsf(x[k]));  // (drops a NaN)
+                        g = by.scale_long(amax);
+                        w = make_uint2(by.codes_long<8>(x, g), by.codes_long<8>(x + 8, g));
+                    }
+                    *reinterpret_cast<uint2*>(codes[u]) = w;
+                    *scale[u] = g.byte;
+                }
             }
         }
     }
-    if (bad_page) atomicOr(p.status, FD_DEV_BAD_PAGE);
 }
 
-static int rows_grid(const Fp4RowsParams& p) { return std::max(1, std::min((p.total_rows + kWarps - 1) / kWarps, 8 * p.n_sms)); }
+// A run is short enough for every SM to have some, and long enough for its look-ups to be few.
+template <bool READ>
+static void launch_rows(const Fp4RowsParams& p, cudaStream_t s) {
+    const int resident = 4 * p.n_sms, run = std::max(1, std::min(kRun, (p.total_rows + resident - 1) / resident));
+    const int grid = std::max(1, std::min((p.total_rows + run - 1) / run, resident));
+    // floor(e / (groups of a row)) as the high half of a product: exact, as e < 64 rows and 64 rows of groups squared stay below 2^32
+    const unsigned per_row = 2u * p.Hkv * (p.d / kFp4Group);
+    kv_rows_fp4_kernel<READ><<<grid, kThreads, 0, s>>>(p, run, 0xffffffffu / per_row + 1);
+}
 
-void launch_kv_append_fp4(const Fp4RowsParams& p, cudaStream_t s) { kv_rows_fp4_kernel<false><<<rows_grid(p), kThreads, 0, s>>>(p); }
+void launch_kv_append_fp4(const Fp4RowsParams& p, cudaStream_t s) { launch_rows<false>(p, s); }
 
-void launch_kv_read_fp4(const Fp4RowsParams& p, cudaStream_t s) { kv_rows_fp4_kernel<true><<<rows_grid(p), kThreads, 0, s>>>(p); }
+void launch_kv_read_fp4(const Fp4RowsParams& p, cudaStream_t s) { launch_rows<true>(p, s); }
 
 }  // namespace fd

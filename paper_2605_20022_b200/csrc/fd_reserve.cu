@@ -75,35 +75,60 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(ReserveParams p) {
     auto list_at = [&](int i) { return i < n_free ? p.free_pages[i] : p.freed[i - n_free]; };
     bool bad_page = false;
 
-    // ---- rows
+    // ---- rows, four in a row per thread: one search, 16-byte stores
     const long long stride = (long long)gridDim.x * kThreads;
-    for (long long row = (long long)blockIdx.x * kThreads + tid; row < p.total_rows; row += stride) {
-        int slot = -1, position = -1;
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.slot_map) | reinterpret_cast<uintptr_t>(p.positions)) & 15) == 0;
+    for (long long row0 = 4 * ((long long)blockIdx.x * kThreads + tid); row0 < p.total_rows; row0 += 4 * stride) {
+        int slot[4] = {-1, -1, -1, -1}, position[4] = {-1, -1, -1, -1};
+        const int count = (int)min(4LL, p.total_rows - row0);
         if (!bad) {
-            int lo = 0, hi = B;  // the sequence that owns the row: the last one that starts at or before it
+            int lo = 0, hi = B;  // the sequence that owns the first row: the last one that starts at or before it
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (sc.rows[mid] <= row) lo = mid; else hi = mid;
+                if (sc.rows[mid] <= row0) lo = mid; else hi = mid;
             }
-            const int b = lo, i = (int)(row - sc.rows[b]);
-            const int n = p.prefix_lens[b], L = p.q_lens[b], M = p.n_mask[b], C = L - M;
-            const int pos = n + i, page = pos >> 4, first = (n + 15) >> 4;
-            position = pos;
-            if (i >= C) {
-                const int nb = p.n_blocks ? max(p.n_blocks[b], 1) : 1, each = M / nb;
-                const int g = (i - C) / each, u = (i - C) % each;
-                position = n + (C - nb + g) + 1 + u;
-            }
-            if (!shorted) {
-                int32_t* entry = p.page_table + (long long)b * p.max_pages + page;
-                int id = page >= first ? list_at(top - 1 - (sc.need[b] + page - first)) : *entry;
-                if ((unsigned)id >= (unsigned)p.num_pages) { bad_page = true; id = -1; }
-                if (page >= first && (pos & 15) == 0) *entry = id;
-                if (id >= 0) slot = id * 16 + (pos & 15);
+            int b = lo - 1, n = 0, C = 0, M = 0, first = 0, last_page = -1, id = -1, end = 0, start = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= count) break;
+                const int row = (int)(row0 + k);
+                if (k == 0 || row >= end) {  // on to the sequence of this row (past empty ones)
+                    do ++b; while (sc.rows[b + 1] <= row);
+                    start = sc.rows[b];
+                    end = sc.rows[b + 1];
+                    n = p.prefix_lens[b];
+                    M = p.n_mask[b];
+                    C = end - start - M;
+                    first = (n + 15) >> 4;
+                    last_page = -1;
+                }
+                const int i = row - start, pos = n + i, page = pos >> 4;
+                position[k] = pos;
+                if (i >= C) {
+                    const int nb = p.n_blocks ? max(p.n_blocks[b], 1) : 1, each = M / nb;
+                    const int g = (i - C) / each, u = (i - C) - g * each;
+                    position[k] = n + (C - nb + g) + 1 + u;
+                }
+                if (!shorted) {
+                    int32_t* entry = p.page_table + (long long)b * p.max_pages + page;
+                    if (page != last_page) {
+                        last_page = page;
+                        id = page >= first ? list_at(top - 1 - (sc.need[b] + page - first)) : *entry;
+                        if ((unsigned)id >= (unsigned)p.num_pages) { bad_page = true; id = -1; }
+                    }
+                    if (page >= first && (pos & 15) == 0) *entry = id;
+                    if (id >= 0) slot[k] = id * 16 + (pos & 15);
+                }
             }
         }
-        p.slot_map[row] = slot;
-        p.positions[row] = position;
+        if (wide && count == 4) {
+            *reinterpret_cast<int4*>(p.slot_map + row0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+            *reinterpret_cast<int4*>(p.positions + row0) = make_int4(position[0], position[1], position[2], position[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < count) { p.slot_map[row0 + k] = slot[k]; p.positions[row0 + k] = position[k]; }
+        }
     }
     // ---- released ids that stay on the list (the others have been handed out from where the commit wrote them)
     if (!bad)
@@ -129,8 +154,8 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(ReserveParams p) {
 }
 
 void launch_reserve(const ReserveParams& p, cudaStream_t s) {
-    const long long work = (p.total_rows + kThreads - 1) / kThreads;
-    const int grid = (int)std::max<long long>(1, std::min<long long>(work, 2LL * p.n_sms));
+    const long long work = (p.total_rows + 4 * kThreads - 1) / (4 * kThreads);
+    const int grid = (int)std::max<long long>(1, std::min<long long>(work, 4LL * p.n_sms));
     reserve_kernel<<<grid, kThreads, sizeof(ReserveSmem), s>>>(p);
 }
 
