@@ -109,7 +109,7 @@ struct Cfg {
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
     static constexpr int kFp4Offset = kBarOffset + 3072;         // FP4: Fp4Shared
-    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 2304 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 3328 : 0);  // the dynamic shared memory is declared 1024-byte aligned
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
     // A K or V tile in shared memory: [8-token group][half of d][8 rows][128 B] -- what one TMA box per page
@@ -139,11 +139,15 @@ static_assert(sizeof(Bars) <= 320, "Bars must fit in front of the range-start wi
 struct Fp4Shared {
     uint64_t raw_full[6], raw_empty[6];  // a tile of codes and scales has landed / has been widened
     uint64_t q_ready;                    // the Q tile of a piece has been turned into fp16
+    // Three S / P buffers and one O (columns 0, 128, 256; 384): tile g uses buffer g % 3, the groups take turns.
+    uint64_t s_full[3], p_full[3], pv_done[3];
+    uint64_t decided[4][2];              // [warp of a group][tile & 1]: the tile has settled its rows' references
     // Per query row: what its scores are multiplied by (slot = piece & 3; a slot is written again three pieces later,
     // when the epilogue of the piece it served is over: the P V of a piece waits for the epilogue before it).
     float row_scale[4][kMaxRows];
+    float ref[2][kMaxRows];              // [piece & 1] the reference of each row, -inf while it has none
 };
-static_assert(sizeof(Fp4Shared) <= 2304, "Fp4Shared must fit behind the row blocks");
+static_assert(sizeof(Fp4Shared) <= 3328, "Fp4Shared must fit behind the row blocks");
 
 
 // K (which = 0) or V (which = 1) load warp.
@@ -449,9 +453,9 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     using C = Cfg<D, MODE, FP4>;
     const int lane = threadIdx.x & 31;
     constexpr uint32_t idesc_qk = FP4 ? make_idesc_f16(128, kTileTokens, false) : make_idesc_bf16(128, kTileTokens, false);
-    constexpr uint32_t idesc_pv = FP4 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
+    constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
     const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
-    const bool group_pv = pv_by_group<MODE>(rg.e_c - rg.s_c);
+    const bool group_pv = FP4 || pv_by_group<MODE>(rg.e_c - rg.s_c);  // FP4: pv_role_fp4
     if (p.early == 1) wait_prior_launch();  // (this role touches shared and tensor memory only; p.early >= 2 lets it run ahead)
     const uint64_t qd0 = make_smem_desc(smem_u32(sq), 16, 1024);
     const int s_c = rg.s_c, e_c = rg.e_c;
@@ -465,7 +469,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
             const int gg = w.g0 + jj, s = jj & 1, st = gg % C::kStages, u = w.u_base[s] + (jj >> 1);
             if (!wait_all(&bars->v_full[st], (gg / C::kStages) & 1, abort)) { ok = false; return; }
             unsigned char* vt = sv + st * C::kKBytes;
-            if (!FP4) zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + jj) * kTileTokens, lane);  // (FP4: widened as zeros)
+            zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + jj) * kTileTokens, lane);
             // the first P V of a stream in a piece overwrites O: the previous piece's epilogue must have read it
             if (jj < 2 && w.piece > 0 && !wait_all(&bars->o_free, (w.piece - 1) & 1, abort)) { ok = false; return; }
             // (descriptors are made before the last wait: what follows it is the MMA instructions alone.  The address
@@ -497,18 +501,20 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
             [[maybe_unused]] const int u_prev = w.u_base[s] + (j >> 1) - 1;  // the stream's previous tile, over all pieces
             const uint64_t kd0 = make_smem_desc(smem_u32(sk + st * C::kKBytes), 16, C::kGroupBytes);
 #if FD_QK_MODE != 0
-            if (u_prev >= 0 && !wait_all(&bars->pv_done[s], u_prev & 1, abort)) { ok = false; break; }
+            if (!FP4 && u_prev >= 0 && !wait_all(&bars->pv_done[s], u_prev & 1, abort)) { ok = false; break; }
 #endif
+            if (FP4 && g >= 3 && !wait_all(&f4->pv_done[g % 3], ((g - 3) / 3) & 1, abort)) { ok = false; break; }
+            const uint32_t s_col = FP4 ? (uint32_t)(g % 3) * 128u : col_s[s];
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
                 for (int kk = 0; kk < C::kKSteps; ++kk) {
                     constexpr int kQHalf = kMaxRows * 128;
-                    umma_ss(tmem + col_s[s], qd0 + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
+                    umma_ss(tmem + s_col, qd0 + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
                             kd0 + (uint64_t)(((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
                 }
                 umma_commit(&bars->k_empty[st]);
-                umma_commit(&bars->s_full[s]);
+                umma_commit(FP4 ? &f4->s_full[g % 3] : &bars->s_full[s]);
                 if (j == pc.nt - 1) umma_commit(&bars->q_free);  // the next piece's Q may come in
             }
             __syncwarp();
@@ -516,6 +522,40 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
         }
         if (!group_pv && ok) issue_pv(pc.nt - 1);
         w.advance(pc);
+    }
+}
+
+// FP4: the warp that issues P V, in tile order.
+template <int D, int MODE>
+__device__ __forceinline__ void pv_role_fp4(unsigned char* sv, Bars* bars, Fp4Shared* f4, const Piece* ring, uint32_t tmem, const Range rg,
+                                            volatile int* abort) {
+    using C = Cfg<D, MODE, true>;
+    constexpr uint32_t idesc = make_idesc_f16(128, D, true);
+    Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
+    while (w.t < rg.e_c) {
+        if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
+        const int nt = ring[w.piece & (kDescSlots - 1)].nt, v = ring[w.piece & (kDescSlots - 1)].v;
+        for (int j = 0; j < nt; ++j) {
+            const int g = w.g0 + j, st = g % C::kStages, b = g % 3;
+            if (!wait_all(&bars->v_full[st], (g / C::kStages) & 1, abort)) return;
+            // the first P V of a piece overwrites O: the previous piece's epilogue must have read it
+            if (j == 0 && w.piece > 0 && !wait_all(&bars->o_free, (w.piece - 1) & 1, abort)) return;
+            const uint64_t vd0 = make_smem_desc(smem_u32(sv + st * C::kKBytes), 1024, C::kGroupBytes);
+            if (!wait_all(&f4->p_full[b], (g / 3) & 1, abort)) return;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kTileTokens / 16; ++kk)
+                    umma_ts(tmem + 384u, tmem + b * 128u + kk * 8, vd0 + (uint64_t)((kk * C::kPageBytes) >> 4), idesc, j > 0 || kk > 0);
+                umma_commit(&bars->v_empty[st]);
+                umma_commit(&f4->pv_done[b]);
+            }
+            __syncwarp();
+        }
+        w.g0 += nt;
+        w.t += nt;
+        w.b = v;
+        ++w.piece;
     }
 }
 
@@ -716,15 +756,21 @@ __device__ __forceinline__ uint32_t pack16(float2 v) {
     return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-// One row of a tile in the FP4 kernel, whose softmax warps have fewer registers than a whole row of S takes.  The common
-// case goes over S once, 32 columns at a time, and forms the weights against the running maximum as it stands; they
-// are kept -- packed, half the size of the scores -- if the tile's own maximum then turns out not to pass it by more than
-// the threshold.  Otherwise, and in the first tile of a piece (no maximum yet) and the tiles the mask cuts, S is gone
-// over twice: for the maximum, then for the weights, written as they are formed (a chunk's weights only ever land on
-// scores that have been read).
+// One row of a tile in the FP4 kernel.  Both groups add into one O (three S / P buffers instead of two and a second
+// accumulator: a group then finds its next S ready, where the chain softmax -> P V -> Q K^T of its own buffer used to stand
+// between two of its tiles), so a row's reference -- what its scores are taken against -- is shared by the two threads of
+// the row, and its changes have to follow the order of the tiles: a tile settles its reference after the tile before it
+// has (decided), and stores its weights only then.  The reference is raised when a score passes it by more than the
+// threshold, which is rare, so the weights are formed beforehand against the reference as it stands and only kept --
+// packed, half the size of the scores -- if nothing has changed.  Otherwise, and in the first tile of a piece (no
+// reference yet) and the tiles the mask cuts, S is gone over twice: for the maximum, then for the weights, written as
+// they are formed (a chunk's weights only ever land on scores that have been read).
+// m, l: the reference and the sum of this thread's weights so far.
 template <int D>
 __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_addr, float c, float head, bool masked, int lim, int blo, int bhi,
-                                                 bool first, float& m, float& l) {
+                                                 int j, volatile float* ref, uint64_t* decided_before, uint32_t before_parity, uint64_t* decided,
+                                                 uint64_t* pv_before, uint32_t pv_parity, volatile int* abort, float& m, float& l) {
+    const int lane = threadIdx.x & 31;
     auto take_max = [&](const uint32_t (&sv)[32], float& a, float& b) {
 #pragma unroll
         for (int k = 0; k < 32; k += 4) {
@@ -744,10 +790,17 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
             pk[(k >> 1) + 1] = pack16<true>(pb);
         }
     };
+    auto rebase = [&](float to) {  // this thread's sum, from the reference it was formed against
+        if (m != to) {
+            l *= m == -INFINITY ? 0.f : exp2f(m - to);
+            m = to;
+        }
+    };
     const float2 c2 = make_float2(c, c);
-    bool slow = masked || __any_sync(0xffffffffu, first || m == -INFINITY);  // (warp-uniform: masked is)
+    float now = *ref;
+    bool slow = masked || __any_sync(0xffffffffu, now == -INFINITY);  // (warp-uniform: masked is)
     if (!slow) {
-        const float2 nm2 = make_float2(-m, -m);
+        const float2 nm2 = make_float2(-now, -now);
         float a = -INFINITY, b = -INFINITY;
         float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
         uint32_t pk[2][32], sv[2][32];
@@ -759,14 +812,20 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
             take_max(sv[ch & 1], a, b);
             weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 1][(ch & 1) * 16]);
         }
-        slow = __any_sync(0xffffffffu, fmaxf(a, b) * c - head > m + kRescaleThreshold);
+        if (j > 0) (void)wait_all(decided_before, before_parity, abort);  // (an abort is acted upon by the caller's next wait)
+        slow = __any_sync(0xffffffffu, *ref != now || fmaxf(a, b) * c - head > now + kRescaleThreshold);
         if (!slow) {
+            if (lane == 0) mbar_arrive(decided);
             tmem_st32(s_addr, pk[0]);
             tmem_st32(s_addr + 32, pk[1]);
+            rebase(now);
             l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
         }
+    } else if (j > 0) {
+        (void)wait_all(decided_before, before_parity, abort);
     }
     if (slow) {
+        now = *ref;
         auto low_bits = [](int n) -> uint32_t { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
         auto load = [&](int ch, uint32_t (&sv)[32]) {
             tmem_ld32(s_addr + ch * 32, sv);
@@ -786,15 +845,17 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
             take_max(sv, a, b);
         }
         const float m_new = fmaxf(a, b) * c - head;
-        float alpha = 1.f;
-        if (first || m == -INFINITY) {
-            m = m_new;  // nothing accumulated yet (O is overwritten, or exactly zero)
-        } else if (m_new > m + kRescaleThreshold) {
-            alpha = exp2f(m - m_new);
-            m = m_new;
+        float alpha = 1.f, to = now;
+        if (now == -INFINITY) {
+            to = m_new;  // nothing accumulated yet (O is overwritten, or exactly zero)
+        } else if (m_new > now + kRescaleThreshold) {
+            alpha = exp2f(now - m_new);
+            to = m_new;
         }
-        if (__any_sync(0xffffffffu, alpha != 1.f)) {
-            // the previous P V of this stream has completed (the reuse of S and P orders it), so O is quiescent
+        if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+            // every P V before this tile's has completed once the last one has, and this tile's waits for its weights
+            (void)wait_all(pv_before, pv_parity, abort);
+            tc_fence_after();
 #pragma unroll 1
             for (int ch = 0; ch < D / 16; ++ch) {
                 uint32_t o[16];
@@ -804,9 +865,13 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
                 for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
                 tmem_st16(o_addr + ch * 16, o);
             }
-            l *= alpha;
+            tc_wait_st();
         }
-        const float mc = (m == -INFINITY) ? 0.f : m;
+        if (to != now) *ref = to;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(decided);
+        rebase(to);
+        const float mc = (to == -INFINITY) ? 0.f : to;
         const float2 nm2 = make_float2(-mc, -mc);
         float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
 #pragma unroll 1
@@ -825,15 +890,16 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
 template <int D, int MODE, bool FP4>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, float* ex, int* s_cs, const CtaStarts cs, const Piece* ring,
                                              uint32_t tmem, const Range rg, const Exchange<D> exch, int cl_rank, unsigned char* stage,
-                                             unsigned char* sv, const Fp4Shared* f4, volatile int* abort) {
+                                             unsigned char* sv, Fp4Shared* f4, volatile int* abort) {
     using C = Cfg<D, MODE, FP4>;
-    constexpr uint32_t idesc_pv = FP4 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
+    constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     const int s_c = rg.s_c, e_c = rg.e_c;
     const int s = warp >> 2;                  // stream
     const int r = (warp & 3) * 32 + lane;     // query row == TMEM lane
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
+    const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {FP4 ? 384u : 256u, 384u};
+    int chain = 0;                            // FP4: tiles this warp's rows have been through, both groups' (phase of decided)
     float c = p.scale_log2e;  // (FP4: of this row and piece, from the conversion of q)
     // FP4 holds P in fp16: everything is scaled by 2^7, so that weights between 2^-21 and, with the deferred rescaling, 2^15 keep
     // all of their bits; m carries the factor, so sums, partials and merges need not know
@@ -865,11 +931,28 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         // arrives on p_full for them, and they wait at the epilogue's hardware barrier, not by polling.
         const int n_idle_threads = 32 * (4 - min(4, (pc.rows + 31) >> 5));
 
-        for (int j = s; j < pc.nt && warp_active; j += 2) {
+        if constexpr (FP4) {
+            for (int j = s; j < pc.nt && warp_active; j += 2) {
+                const int g = w.g0 + j, b3 = g % 3, e = chain + j;
+                if (!wait_all(&f4->s_full[b3], (g / 3) & 1, abort)) { ok = false; break; }
+                tc_fence_after();
+                if (j < 2) c = f4->row_scale[w.piece & 3][r];
+                const int pos0 = (pc.tile0 + j) * kTileTokens;
+                // masked: the tile reaches into the query block (or past kv_len): the row's mask applies, in tile-local columns
+                softmax_tile_fp4<D>(tmem + lane_base + b3 * 128u, tmem + lane_base + 384u, c, kHead, pos0 + kTileTokens > pc.n, rm.limit - pos0,
+                                    rm.blk_lo - pos0, rm.blk_hi - pos0, j, &f4->ref[w.piece & 1][r], &f4->decided[warp & 3][(e - 1) & 1],
+                                    (uint32_t)((e - 1) >> 1) & 1u, &f4->decided[warp & 3][e & 1], &f4->pv_done[(g + 2) % 3], (uint32_t)((g - 1) / 3) & 1u,
+                                    abort, m, l);
+                tc_fence_before();
+                mbar_arrive(&f4->p_full[b3]);
+                if ((warp & 3) == 0 && lane == 0 && n_idle_threads) mbar_arrive_cnt(&f4->p_full[b3], n_idle_threads);
+            }
+            if (warp_active) chain += pc.nt;
+        }
+        for (int j = s; j < pc.nt && warp_active && !FP4; j += 2) {
             const int u = w.u_base[s] + (j >> 1);
             if (!wait_all(&bars->s_full[s], u & 1, abort)) { ok = false; break; }
             tc_fence_after();
-            if (FP4 && j < 2) c = f4->row_scale[w.piece & 3][r];
             {
                 const int pos0 = (pc.tile0 + j) * kTileTokens;
                 // tile reaches into the query block (or past kv_len): the row's mask applies, in tile-local columns
@@ -877,9 +960,6 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 const int lim = rm.limit - pos0, blo = rm.blk_lo - pos0, bhi = rm.blk_hi - pos0;
                 const uint32_t s_addr = tmem + lane_base + col_s[s];
 
-                if constexpr (FP4) {
-                    softmax_tile_fp4<D>(s_addr, tmem + lane_base + col_o[s], c, kHead, masked, lim, blo, bhi, j < 2, m, l);
-                } else {
                 // ---- the whole row of S in one round trip: TMEM loads queue behind the MMAs in flight,
                 //      so every ld -> wait pair costs up to one MMA tile; registers come from setmaxnreg
                 uint32_t sv[4][32];
@@ -903,7 +983,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         mx[2] = max3(mx[2], __uint_as_float(sv[ch][k + 4]), __uint_as_float(sv[ch][k + 5]));
                         mx[3] = max3(mx[3], __uint_as_float(sv[ch][k + 6]), __uint_as_float(sv[ch][k + 7]));
                     }
-                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c - kHead);
+                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
                 float alpha = 1.f;
                 if (j < 2 || m == -INFINITY) {
                     m = m_new;  // nothing accumulated yet (O is overwritten, or exactly zero)
@@ -940,14 +1020,13 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         const float2 pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
                         sum0 = __fadd2_rn(sum0, pa);
                         sum1 = __fadd2_rn(sum1, pb);
-                        pk[k >> 1] = pack16<FP4>(pa);
-                        pk[16 + (k >> 1)] = pack16<FP4>(pb);
+                        pk[k >> 1] = pack16<false>(pa);
+                        pk[16 + (k >> 1)] = pack16<false>(pb);
                     }
                     tmem_st32(s_addr + hp * 32, pk);  // overwrites S columns that are already in registers
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tc_wait_st();
-                }
             }
             tc_fence_before();
             mbar_arrive(&bars->p_full[s]);
@@ -958,7 +1037,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 const int gg = w.g0 + j, st = gg % C::kStages;
                 unsigned char* vt = sv + st * C::kKBytes;
                 if (!wait_all(&bars->v_full[st], (gg / C::kStages) & 1, abort)) { ok = false; break; }
-                if (!FP4) zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + j) * kTileTokens, lane);  // (FP4: widened as zeros)
+                zero_v_tail<C>(vt, pc.kv_len - (pc.tile0 + j) * kTileTokens, lane);
                 // the first P V of a stream in a piece overwrites O: the previous piece's epilogue (both groups) must have read it
                 if (j < 2 && w.piece > 0 && !wait_all(&bars->o_free, (w.piece - 1) & 1, abort)) { ok = false; break; }
                 // (the address field of a descriptor is its low 14 bits, in 16-byte units, so a K step is an addition)
@@ -998,12 +1077,16 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 ticket = atomicAdd(seg_cnt, 1);
             }
         }
-        if (warp_active) {  // every P V of the piece has completed: the last one of each stream
+        if (FP4 && warp_active) {  // P V are issued in tile order by one warp: the last one has completed
+            const int g_last = w.g0 + pc.nt - 1;
+            ok = ok && wait_all(&f4->pv_done[g_last % 3], (g_last / 3) & 1, abort);
+        }
+        if (!FP4 && warp_active) {  // every P V of the piece has completed: the last one of each stream
             ok = ok && wait_all(&bars->pv_done[0], (w.u_base[0] + ((pc.nt + 1) >> 1) - 1) & 1, abort);
             if (pc.nt >= 2) ok = ok && wait_all(&bars->pv_done[1], (w.u_base[1] + (pc.nt >> 1) - 1) & 1, abort);
         }
         tc_fence_after();
-        const bool two = pc.nt >= 2;
+        const bool two = pc.nt >= 2 && !FP4;
         // Stream exchange: group 1 hands its (m, l) to group 0, which answers with the two scale factors.
         // A thread only ever touches the two slots of its own row, so one barrier each way is enough.
         if (s == 1) { ex[r] = m; ex[kMaxRows + r] = l; }
@@ -1014,11 +1097,20 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         const bool stage_ok = merger && w.t + pc.nt == e_c && (bars->epi_flag >> 8) <= St::kMaxOthers;  // uniform: from shared memory
         float a0 = 0.f, a1 = 0.f, mm = -INFINITY, L = 0.f;
         if (s == 0) {
-            const float m1 = two ? ex[r] : -INFINITY, l1 = ex[kMaxRows + r];
-            mm = fmaxf(m, m1);
-            a0 = (m == -INFINITY) ? 0.f : exp2f(m - mm);
-            a1 = (m1 == -INFINITY) ? 0.f : exp2f(m1 - mm);
-            L = a0 * l + (two ? a1 * l1 : 0.f);
+            if constexpr (FP4) {
+                // one O, against the row's last reference; the two threads' sums are brought there
+                const float m1 = ex[r], l1 = ex[kMaxRows + r];
+                mm = f4->ref[w.piece & 1][r];
+                f4->ref[(w.piece + 1) & 1][r] = -INFINITY;  // (the next piece's: the one before this has long been read)
+                L = (m == -INFINITY ? 0.f : exp2f(m - mm) * l) + (pc.nt < 2 || m1 == -INFINITY ? 0.f : exp2f(m1 - mm) * l1);
+                a0 = 1.f;
+            } else {
+                const float m1 = two ? ex[r] : -INFINITY, l1 = ex[kMaxRows + r];
+                mm = fmaxf(m, m1);
+                a0 = (m == -INFINITY) ? 0.f : exp2f(m - mm);
+                a1 = (m1 == -INFINITY) ? 0.f : exp2f(m1 - mm);
+                L = a0 * l + (two ? a1 * l1 : 0.f);
+            }
             if (pc.complete) { const float inv = p.out_scale / L; a0 *= inv; a1 *= inv; }
             ex[r] = a0;
             ex[kMaxRows + r] = a1;
@@ -1219,6 +1311,8 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         if (FP4) {
             for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], C::kWidenWarps); }
             mbar_init(&f4->q_ready, C::kWidenWarps);
+            for (int i = 0; i < 3; ++i) { mbar_init(&f4->s_full[i], 1); mbar_init(&f4->p_full[i], 128); mbar_init(&f4->pv_done[i], 1); }
+            for (int i = 0; i < 4; ++i) { mbar_init(&f4->decided[i][0], 1); mbar_init(&f4->decided[i][1], 1); }
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
@@ -1237,6 +1331,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         mbar_fence_init();
     }
     if (warp == kMmaWarp) tmem_alloc(&bars->tmem_base, 512);
+    if (FP4 && tid < 2 * kMaxRows) f4->ref[tid / kMaxRows][tid % kMaxRows] = -INFINITY;
     if (warp == kKWarp && lane == 0) { prefetch_tmap(&tmap); prefetch_tmap(&qmap); }
     // a call that plans for itself: warp 0 does so meanwhile (it needs the earlier kernels' results -- the lengths --
     // and waits for them on its own; its global loads then overlap the set-up of the other warps)
@@ -1354,6 +1449,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         if constexpr (FP4) {
             unsigned char* raw = smem + C::kRawOffset;
             if (warp == kKWarp) load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
+            else if (warp == kVWarp) pv_role_fp4<D, MODE>(sv, bars, f4, ring, tmem, rg, abort);
             else if (warp >= 12) widen_role<D, MODE>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
         } else {
             if (warp == kKWarp) load_role<D, MODE>(tmap, p, n_rb, sk, bars->k_full, bars->k_empty, 0, rg, &bars->k_full[0], &bars->bad, abort);
