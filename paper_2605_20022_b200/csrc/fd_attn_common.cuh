@@ -11,8 +11,6 @@ namespace fd {
 
 using namespace sm100;
 
-constexpr int kDescSlots = 4;
-
 // The plan of a call that plans for itself (at most kSelfPlanMaxRb sequences, one row block each), in shared memory.
 struct SelfScans {
     int cu_q[kSelfPlanMaxRb + 1], cu_tiles[kSelfPlanMaxRb + 1], cu_ne[kSelfPlanMaxRb + 1];
@@ -91,11 +89,13 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
 // Piece descriptors.  The Q load warp walks the pieces ahead of everyone, decodes each one (a chain of
 // dependent global loads) and publishes it in a small ring in shared memory; the MMA warp and the softmax
 // groups pick it up from there, so the decode is off their critical path at a piece boundary.  Slot
-// reuse is safe: descriptor N + 1 is written after every QK^T of piece N - 1 has completed, when no
-// consumer is before piece N - 1 and every consumer copies its descriptor to registers at piece start.
-template <class Bars>
+// reuse is safe: descriptor N + 1 is written after every QK^T of piece N - 1 has completed, hence the P V of the tile B tiles
+// before its last (B: buffers of S).  Every consumer copies its descriptor to registers at piece start, so one that is not
+// past piece N - 1 - B yet has copied that piece's: descriptors N - B to N + 1 must not share a slot, and with two buffers
+// (bf16) four slots do, with three (FP4) eight.
+template <int SLOTS, class Bars>
 __device__ __forceinline__ void publish_piece(Bars* bars, Piece* ring, int n, const Piece& pc) {
-    ring[n & (kDescSlots - 1)] = pc;
+    ring[n & (SLOTS - 1)] = pc;
     asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_u32(&bars->desc_n)), "r"(n + 1) : "memory");
 }
 template <class Bars>
@@ -201,7 +201,7 @@ __device__ __forceinline__ void self_plan(const AttnParams& p, SelfScans* sc, Ro
 // lands as q_box_t * G consecutive 128-byte rows, row (i, g) at i * G + g: the order the MMA wants.  The
 // last box of a piece may reach past the block (rows of the next sequence, or zeros past T): each query
 // row only ever influences its own output row, and those rows are never stored.
-template <int D, class Bars>
+template <int D, int SLOTS, class Bars>
 __device__ __forceinline__ void q_role(const CUtensorMap& qmap, const AttnParams& p, int n_rb, unsigned char* sq, Bars* bars, Piece* ring,
                                        const Range rg, volatile int* abort) {
     constexpr int kHalves = D / 64;
@@ -211,7 +211,7 @@ __device__ __forceinline__ void q_role(const CUtensorMap& qmap, const AttnParams
     Walk w = {s_c, 0, {0, 0}, 0, rg.first};
     int issued = 0;
     Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
-    if (lane == 0) publish_piece(bars, ring, 0, pc);
+    if (lane == 0) publish_piece<SLOTS>(bars, ring, 0, pc);
     if (p.early == 1) wait_prior_launch();  // q may be written by it (p.early >= 2: it is known not to be)
     while (w.t < e_c) {
         if (w.piece > 0 && !wait_all(&bars->q_free, (w.piece - 1) & 1, abort)) break;
@@ -227,7 +227,7 @@ __device__ __forceinline__ void q_role(const CUtensorMap& qmap, const AttnParams
         if (w.t < e_c) {
             // the next piece: descriptor for the other roles, and its Q rows on their way into L2
             pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
-            if (lane == 0) publish_piece(bars, ring, w.piece, pc);
+            if (lane == 0) publish_piece<SLOTS>(bars, ring, w.piece, pc);
             const int nb2 = (pc.Lv + bt - 1) / bt;
             for (int e = lane; e < nb2 * kHalves; e += 32)
                 tma_prefetch_3d(&qmap, (e % kHalves) * 64, pc.kvh * p.G, pc.row0 + (e / kHalves) * bt);

@@ -56,9 +56,6 @@ using namespace sm100;
 namespace {
 
 // Warps that widen 4-bit tiles (4 or 8).
-#ifndef FD_WIDEN_WARPS
-#define FD_WIDEN_WARPS 8
-#endif
 // warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads (FP4: 8 loads both, 9 idle, 12-15 widen)
 constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10, kQWarp = 11;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
@@ -86,14 +83,14 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 
 template <int D, int MODE, bool FP4>
 struct Cfg {
-    static constexpr int kWidenWarps = FP4 ? FD_WIDEN_WARPS : 0;  // FP4: the warps behind warp 11 widen the tiles
+    static constexpr int kWidenWarps = FP4 ? 8 : 0;  // FP4: the warps behind warp 11 widen the tiles
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
-    // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps: the launch allocates 168 (no widening
-    // warps), 128 (four) or 96 (eight) to each, and what the groups take adds up to no more than that.
-    static constexpr int kRegSoftmax = !FP4 ? 224 : kWidenWarps == 4 ? 152 : 144;
-    static constexpr int kRegHelper = !FP4 || kWidenWarps == 4 ? 56 : 48;
-    static constexpr int kRegWiden = kWidenWarps == 4 ? 128 : 64;
-    static_assert(!FP4 || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * (kWidenWarps == 4 ? 128 : 96), "register split");
+    // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps: the launch allocates 168 (bf16) or
+    // 96 (FP4) to each, and what the groups take adds up to no more than that.
+    static constexpr int kRegSoftmax = FP4 ? 144 : 224;
+    static constexpr int kRegHelper = FP4 ? 48 : 56;
+    static constexpr int kRegWiden = 64;
+    static_assert(!FP4 || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * 96, "register split");
     // buffers in the K ring, and again in the V ring (FP4: of widened tiles, fed from the raw ring)
     static constexpr int kStages = FP4 ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
     static constexpr int kQBytes = kMaxRows * D * 2;
@@ -109,7 +106,8 @@ struct Cfg {
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
     static constexpr int kFp4Offset = kBarOffset + 3072;         // FP4: Fp4Shared
-    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 3328 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kDescSlots = FP4 ? 8 : 4;  // ring of piece descriptors: see publish_piece
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
     // A K or V tile in shared memory: [8-token group][half of d][8 rows][128 B] -- what one TMA box per page
@@ -146,8 +144,9 @@ struct Fp4Shared {
     // when the epilogue of the piece it served is over: the P V of a piece waits for the epilogue before it).
     float row_scale[4][kMaxRows];
     float ref[2][kMaxRows];              // [piece & 1] the reference of each row, -inf while it has none
+    Piece ring[8];                       // piece descriptors
 };
-static_assert(sizeof(Fp4Shared) <= 3328, "Fp4Shared must fit behind the row blocks");
+static_assert(sizeof(Fp4Shared) <= 4096, "Fp4Shared must fit behind the row blocks");
 
 
 // K (which = 0) or V (which = 1) load warp.
@@ -300,32 +299,40 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
 // share a token, so the reads are contiguous; of a 16-byte store's eight lanes -- two tokens, four chunks -- the
 // chunks of the upper half of d store their words in the order 2 3 0 1, which puts all eight on different banks.
 // ZERO_TAIL: tokens at or beyond `valid` become zeros (no token owns them: they may hold a NaN, and 0 * NaN is not 0).
-constexpr int kWidenThreads = 32 * FD_WIDEN_WARPS;
+constexpr int kWidenThreads = 256;
+
+template <int D>
+struct RawWords {  // a thread's part of a tile; all of it is read before anything is stored (a store orders the reads behind it)
+    static constexpr int kChunks = D / 32;  // 32-element chunks of a token
+    static constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
+    uint4 codes[kPasses];
+    uint32_t sc[kPasses];
+    __device__ __forceinline__ void load(const unsigned char* raw) {
+        constexpr int kRawPage = 2 * fp4_page_bytes(D);
+        const int t = (int)threadIdx.x - 384, c = t % kChunks;
+#pragma unroll
+        for (int it = 0; it < kPasses; ++it) {
+            const int tok = t / kChunks + it * (kWidenThreads / kChunks);
+            const unsigned char* page = raw + (tok >> 4) * kRawPage;
+            codes[it] = *reinterpret_cast<const uint4*>(page + (tok & 15) * (D / 2) + c * 16);
+            sc[it] = *reinterpret_cast<const uint16_t*>(page + fp4_scale_offset(D) + (tok & 15) * (D / 16) + c * 2);
+        }
+    }
+};
 
 template <int D, bool ZERO_TAIL>
-__device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned char* tile, int valid) {
-    constexpr int kChunks = D / 32;        // 32-element chunks of a token
-    constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
-    constexpr int kRawPage = 2 * fp4_page_bytes(D);
+__device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char* tile, int valid) {
+    constexpr int kChunks = RawWords<D>::kChunks;
     constexpr int kHalves = D / 64;
     const int t = (int)threadIdx.x - 384, c = t % kChunks;
     const bool swap = kHalves == 2 && (c & 2);
-    uint4 codes[kPasses];                  // all reads go out first: a store orders the reads behind it
-    uint32_t sc[kPasses];
 #pragma unroll
-    for (int it = 0; it < kPasses; ++it) {
+    for (int it = 0; it < RawWords<D>::kPasses; ++it) {
         const int tok = t / kChunks + it * (kWidenThreads / kChunks);
-        const unsigned char* page = raw + (tok >> 4) * kRawPage;
-        codes[it] = *reinterpret_cast<const uint4*>(page + (tok & 15) * (D / 2) + c * 16);
-        sc[it] = *reinterpret_cast<const uint16_t*>(page + fp4_scale_offset(D) + (tok & 15) * (D / 16) + c * 2);
-    }
-#pragma unroll
-    for (int it = 0; it < kPasses; ++it) {
-        const int tok = t / kChunks + it * (kWidenThreads / kChunks);
-        const __half2 s2 = as_half2(e4m3x2_to_half((uint16_t)sc[it]));
+        const __half2 s2 = as_half2(e4m3x2_to_half((uint16_t)in.sc[it]));
         const __half2 s_lo = __half2half2(__low2half(s2)), s_hi = __half2half2(__high2half(s2));
         const bool dead = ZERO_TAIL && tok >= valid;
-        const uint4 cd = codes[it];
+        const uint4 cd = in.codes[it];
         const uint32_t wd[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
         const __half2 s01 = swap ? s_hi : s_lo, s23 = swap ? s_lo : s_hi;
         unsigned char* row = tile + (tok >> 3) * (kHalves * 1024) + (c >> 1) * 1024 + (tok & 7) * 128;
@@ -348,7 +355,7 @@ __device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned ch
 template <int D>
 __device__ __forceinline__ void q_to_half(unsigned char* sq, float* row_scale, float scale_log2e) {
     constexpr int kPer = kWidenThreads / kMaxRows, kUnits = D / 8 / kPer;  // 16-byte units of a row, per thread
-    static_assert(kPer == 1 || kPer == 2, "128 or 256 widening threads");
+    static_assert(kPer == 2, "two threads a row");
     const int t = (int)threadIdx.x - 384, r = t / kPer, part = t % kPer;
     auto at = [&](int i) -> uint4* {  // the thread's i-th unit
         const int u = part * kUnits + (kPer == 2 && part && kUnits >= 8 ? i ^ 4 : i);
@@ -392,12 +399,14 @@ __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* s
     Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
     while (w.t < rg.e_c) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
-        const Piece pc = ring[w.piece & (kDescSlots - 1)];
+        const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
         auto do_k = [&](int j) -> bool {
             const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
             if (!wait_all(&f4->raw_full[rs], (g / C::kRawStages) & 1, abort)) return false;
+            RawWords<D> in;
+            in.load(raw + rs * C::kRawBytes);
             if (!wait_all(&bars->k_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
-            widen_tile<D, false>(raw + rs * C::kRawBytes, sk + st * C::kKBytes, 0);
+            widen_tile<D, false>(in, sk + st * C::kKBytes, 0);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->k_full[st]);
@@ -405,17 +414,17 @@ __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* s
         };
         auto do_v = [&](int j) -> bool {
             const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            RawWords<D> in;  // (the tile has landed: do_k has waited for it)
+            in.load(raw + rs * C::kRawBytes + fp4_page_bytes(D));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&f4->raw_empty[rs]);
             if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
-            const unsigned char* rv = raw + rs * C::kRawBytes + fp4_page_bytes(D);
-            if (valid >= kTileTokens) widen_tile<D, false>(rv, sv + st * C::kKBytes, 0);
-            else widen_tile<D, true>(rv, sv + st * C::kKBytes, valid);
+            if (valid >= kTileTokens) widen_tile<D, false>(in, sv + st * C::kKBytes, 0);
+            else widen_tile<D, true>(in, sv + st * C::kKBytes, valid);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&bars->v_full[st]);
-                mbar_arrive(&f4->raw_empty[rs]);
-            }
+            if (lane == 0) mbar_arrive(&bars->v_full[st]);
             return true;
         };
         if (!do_k(0)) return;
@@ -463,7 +472,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     bool ok = true;
     while (w.t < e_c && ok) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) break;
-        const Piece pc = ring[w.piece & (kDescSlots - 1)];
+        const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
         if (!wait_all(FP4 ? &f4->q_ready : &bars->q_full, w.piece & 1, abort)) break;
         auto issue_pv = [&](int jj) {  // (ranges whose P V this warp issues: see kGroupPvMinTiles)
             const int gg = w.g0 + jj, s = jj & 1, st = gg % C::kStages, u = w.u_base[s] + (jj >> 1);
@@ -534,7 +543,7 @@ __device__ __forceinline__ void pv_role_fp4(unsigned char* sv, Bars* bars, Fp4Sh
     Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
     while (w.t < rg.e_c) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
-        const int nt = ring[w.piece & (kDescSlots - 1)].nt, v = ring[w.piece & (kDescSlots - 1)].v;
+        const int nt = ring[w.piece & (C::kDescSlots - 1)].nt, v = ring[w.piece & (C::kDescSlots - 1)].v;
         for (int j = 0; j < nt; ++j) {
             const int g = w.g0 + j, st = g % C::kStages, b = g % 3;
             if (!wait_all(&bars->v_full[st], (g / C::kStages) & 1, abort)) return;
@@ -771,16 +780,16 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
                                                  int j, volatile float* ref, uint64_t* decided_before, uint32_t before_parity, uint64_t* decided,
                                                  uint64_t* pv_before, uint32_t pv_parity, volatile int* abort, float& m, float& l) {
     const int lane = threadIdx.x & 31;
-    auto take_max = [&](const uint32_t (&sv)[32], float& a, float& b) {
+    auto take_max = [&](const auto& sv, float& a, float& b) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4) {
+        for (int k = 0; k < (int)(sizeof(sv) / 4); k += 4) {
             a = max3(a, __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
             b = max3(b, __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
         }
     };
-    auto weights = [&](const uint32_t (&x)[32], float2 c2, float2 nm2, float2& sum0, float2& sum1, uint32_t* pk) {
+    auto weights = [&](const auto& x, float2 c2, float2 nm2, float2& sum0, float2& sum1, uint32_t* pk) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4) {
+        for (int k = 0; k < (int)(sizeof(x) / 4); k += 4) {
             const float2 xa = __ffma2_rn(make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, nm2);
             const float2 xb = __ffma2_rn(make_float2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), c2, nm2);
             const float2 pa = make_float2(ex2_approx(xa.x), ex2_approx(xa.y)), pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
@@ -803,14 +812,14 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
         const float2 nm2 = make_float2(-now, -now);
         float a = -INFINITY, b = -INFINITY;
         float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
-        uint32_t pk[2][32], sv[2][32];
-        tmem_ld32(s_addr, sv[0]);
+        uint32_t pk[2][32], sv[2][16];
+        tmem_ld16(s_addr, sv[0]);
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
+        for (int ch = 0; ch < 8; ++ch) {
             tc_wait_ld();
-            if (ch < 3) tmem_ld32(s_addr + (ch + 1) * 32, sv[(ch + 1) & 1]);
+            if (ch < 7) tmem_ld16(s_addr + (ch + 1) * 16, sv[(ch + 1) & 1]);
             take_max(sv[ch & 1], a, b);
-            weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 1][(ch & 1) * 16]);
+            weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 2][(ch & 3) * 8]);
         }
         if (j > 0) (void)wait_all(decided_before, before_parity, abort);  // (an abort is acted upon by the caller's next wait)
         slow = __any_sync(0xffffffffu, *ref != now || fmaxf(a, b) * c - head > now + kRescaleThreshold);
@@ -921,7 +930,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         if (tid == 0) bars->piece_ok = wait_piece(bars, w.piece, abort);
         named_bar_sync(1, 256);
         if (!bars->piece_ok) break;
-        const Piece pc = ring[w.piece & (kDescSlots - 1)];
+        const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
         const bool warp_active = (warp & 3) * 32 < pc.rows;
         const int i = r / p.G;
         const RowMask rm = row_mask(pc.i0 + i, pc.n, pc.Lq, pc.M, pc.nb, r < pc.rows);
@@ -1288,10 +1297,10 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
     Bars* bars = reinterpret_cast<Bars*>(smem + C::kBarOffset);
     float* ex = reinterpret_cast<float*>(smem + C::kExOffset);
     int* s_cs = reinterpret_cast<int*>(smem + C::kCsOffset);
-    Piece* ring = reinterpret_cast<Piece*>(smem + C::kDescOffset);
     SelfScans* scans = reinterpret_cast<SelfScans*>(smem + C::kScanOffset);
     RowBlock* rbs = reinterpret_cast<RowBlock*>(smem + C::kRbOffset);
     Fp4Shared* f4 = reinterpret_cast<Fp4Shared*>(smem + C::kFp4Offset);  // FP4 only
+    Piece* ring = FP4 ? f4->ring : reinterpret_cast<Piece*>(smem + C::kDescOffset);
     volatile int* abort = &bars->abort;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -1456,7 +1465,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
             else if (warp == kVWarp) load_role<D, MODE>(tmap, p, n_rb, sv, bars->v_full, bars->v_empty, 1, rg, &bars->k_full[0], &bars->bad, abort);
         }
         if (warp == kMmaWarp) mma_role<D, MODE, FP4>(p, sq, sk, sv, bars, f4, ring, tmem, rg, abort);
-        else if (warp == kQWarp) q_role<D>(qmap, p, n_rb, sq, bars, ring, rg, abort);
+        else if (warp == kQWarp) q_role<D, C::kDescSlots>(qmap, p, n_rb, sq, bars, ring, rg, abort);
         if (MODE == kTcCluster) cluster_sync_all();  // the cluster barrier of the merge counts every thread
     }
     // ---- common tail: everything of this CTA has completed, or it is giving up

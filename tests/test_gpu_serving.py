@@ -518,6 +518,23 @@ def test_attention_random_shapes(seed):
         check(got, want, f"{step.name} path {path}")
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,batch,longest", [(32, 8, 128, 330, 120), (16, 2, 64, 700, 100), (8, 8, 128, 290, 300)])
+def test_attention_many_short_sequences(Hq, Hkv, d, batch, longest):
+    """A CTA works through a dozen segments of one to three tiles: the roles run pieces ahead of one another."""
+    rng = np.random.default_rng(batch)
+    pl = rng.integers(0, longest + 1, batch)
+    nm = rng.integers(0, 3, batch) * (rng.random(batch) < 0.5)
+    ql = rng.integers(0, 6, batch) + nm + (rng.random(batch) < 0.9)
+    step = wl.make_step("short sequences", wl.Shape(Hq, Hkv, d, 1000), pl.tolist(), ql.tolist(), nm.tolist(), seed=batch)
+    q, cache = wl.make_q(step), ref.make_cache(wl.make_kv(step), rng_seed=batch)
+    want = attn_ref(step, q, cache)
+    with Ctx(step, 0, max_batch=batch) as ctx:
+        for _ in range(5):
+            got, status = attn_gpu(ctx, step, q, cache)
+            assert status == 0
+            check(got, want, "short sequences")
+
+
 @pytest.mark.parametrize("path", PATHS)
 @pytest.mark.parametrize("size,scale", [(3.0e5, 1e-7), (1e-6, 1e4), (8.0, 0.0), (1e30, 1e-32)])
 def test_attention_queries_of_any_size(path, size, scale):
