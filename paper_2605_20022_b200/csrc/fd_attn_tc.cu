@@ -39,6 +39,26 @@
 //
 // Every wait is bounded.  A wait that runs out raises a CTA-wide abort flag: all roles leave
 // their loops, in-flight TMA copies are drained, TMEM is released and FD_DEV_TIMEOUT is set.
+//
+// 4-bit pages (FP4).  Same walk, same epilogue and merges; a tile differs in three places.
+//     loads    : codes and scales of K and V of a page lie side by side in the cache: one untiled bulk copy a page into a raw
+//                ring, 3.6 times fewer bytes than bf16;
+//     widening : eight warps turn a raw tile into fp16 K and V tiles in the layout the MMAs read.  code * scale has at most
+//                6 significant bits and e4m3's range, so fp16 holds it exactly; k_scale goes into the scale of the scores,
+//                v_scale into the output.  Q is converted to fp16 by the same warps, a row against a power of two of its own;
+//     softmax  : P is fp16.  Three S / P buffers and one O; the groups take turns and share the reference of a row.
+// TMEM columns: S / P buffers [0,128) [128,256) [256,384), O [384,384+d).
+//
+// What bounds it: the tensor pipe needs 1024 clocks a tile (d = 128, 128 rows), the exponentials as many, shared memory
+// about 1550 (Q K^T reads 128 bytes a clock, widening writes what P V reads); measured are 2400 with full rows: 283 us for a
+// batch of 16 on a 32k prefix, 971 TFLOP/s, 59 % of the measured cuBLAS rate, 2.1 TB/s of cache.  What is missing is
+// latency: each of softmax, P V, Q K^T and widening hands over through a barrier (150 to 300 clocks a hand-over) with five
+// warps to a scheduler.  A piece costs 6.8 us more than its tiles (first and last tile in two passes, O drained before the
+// next piece's first P V, code that is not in the instruction cache: unrolling the two-pass form made a batch of 64 go from
+// 141 to 163 us), which is what calls on many short sequences spend their time on.
+// Measured and dropped, batch 16 on 32k / batch 64, one token each: S^T = K Q^T with K widened into TMEM, no K tile in shared
+// memory, 394 / 95-115 us, but 155-183 us at up to 16 rows; two S buffers and two accumulators, as in the bf16 form, 344 / 159;
+// four widening warps 472 / 190; four for K and four for V, 431 / 187.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -55,8 +75,8 @@ using namespace sm100;
 
 namespace {
 
-// Warps that widen 4-bit tiles (4 or 8).
-// warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads (FP4: 8 loads both, 9 idle, 12-15 widen)
+// warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads
+// (FP4: 8 loads both, 9 issues P V, 10 issues Q K^T, 12-19 widen)
 constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10, kQWarp = 11;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kEarlyLoadMaxTiles = 96;     // longest range of a CTA that starts on its KV before the previous launch has completed
@@ -140,8 +160,8 @@ struct Fp4Shared {
     // Three S / P buffers and one O (columns 0, 128, 256; 384): tile g uses buffer g % 3, the groups take turns.
     uint64_t s_full[3], p_full[3], pv_done[3];
     uint64_t decided[4][2];              // [warp of a group][tile & 1]: the tile has settled its rows' references
-    // Per query row: what its scores are multiplied by (slot = piece & 3; a slot is written again three pieces later,
-    // when the epilogue of the piece it served is over: the P V of a piece waits for the epilogue before it).
+    // Per query row: what its scores are multiplied by.  Slot = piece & 3: the Q of piece n is converted when every Q K^T of
+    // piece n - 1 has completed, hence every P V up to three tiles before that, and those of piece n - 4 among them.
     float row_scale[4][kMaxRows];
     float ref[2][kMaxRows];              // [piece & 1] the reference of each row, -inf while it has none
     Piece ring[8];                       // piece descriptors
@@ -303,6 +323,8 @@ constexpr int kWidenThreads = 256;
 
 template <int D>
 struct RawWords {  // a thread's part of a tile; all of it is read before anything is stored (a store orders the reads behind it)
+    // (The raw tile is given back only when these words have been widened and stored.  Given back as soon as the reads had been
+    // issued, with nothing yet depending on them, one call in twelve on many short sequences found words of the next tile.)
     static constexpr int kChunks = D / 32;  // 32-element chunks of a token
     static constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
     uint4 codes[kPasses];
@@ -416,15 +438,16 @@ __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* s
             const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
             RawWords<D> in;  // (the tile has landed: do_k has waited for it)
             in.load(raw + rs * C::kRawBytes + fp4_page_bytes(D));
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&f4->raw_empty[rs]);
             if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
             if (valid >= kTileTokens) widen_tile<D, false>(in, sv + st * C::kKBytes, 0);
             else widen_tile<D, true>(in, sv + st * C::kKBytes, valid);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->v_full[st]);
+            if (lane == 0) {
+                mbar_arrive(&bars->v_full[st]);
+                mbar_arrive(&f4->raw_empty[rs]);  // here, where every word read has been used, and not behind the reads: see RawWords
+            }
             return true;
         };
         if (!do_k(0)) return;
@@ -534,7 +557,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     }
 }
 
-// FP4: the warp that issues P V, in tile order.
+// FP4: the warp that issues P V, in tile order (they add into one O; and Q K^T of the tiles ahead does not stand behind them).
 template <int D, int MODE>
 __device__ __forceinline__ void pv_role_fp4(unsigned char* sv, Bars* bars, Fp4Shared* f4, const Piece* ring, uint32_t tmem, const Range rg,
                                             volatile int* abort) {
