@@ -4,6 +4,9 @@
 // Neighbouring threads own neighbouring groups of a row, so both sides are contiguous across a warp.  A CTA takes a run of
 // rows: first a thread per row finds the row's sequence and page (a search and a dependent load), then all threads stream
 // the run's groups with nothing but loads and stores between them.
+// Bound by issue: 24 prompts of 8 heads of 64 (20 k rows, 41 MB in) take 23 us to append and 19 us to read back (floor of
+// both 15.4), half of the issue slots used.  With the look-up made for every group the two took 53 us, now 38 (34 from a graph).
+// A few rows (64 sequences, 1-16 each) are launch latency and the look-up: 9.9 us for both.
 #include <algorithm>
 
 #include "fd_fp4.cuh"

@@ -7,8 +7,9 @@
 //   kHalves   the whole head is rotated and halves are paired: elements 4 l .. 4 l + 3 and the same of the upper half, so that a
 //             pair lies in one lane;
 //   kGeneral  8 consecutive elements: the partner lies in the same lane (adjacent pairs) or rot_dim / 16 lanes away.
-// In 4 bits a scale group is four lanes (kHalves) or two.  Bound by HBM for many rows: 12 KB in, 8 KB + the cache out per row of
-// 32 + 8 + 8 heads of 128.
+// In 4 bits a scale group is four lanes (kHalves) or two.  12 KB in, 8 KB and the cache out per row of 32 + 8 + 8 heads of 128:
+// 9600 rows take 69 us (33 us of bytes), bound by issue -- half of the slots used with a quarter of the warps resident, the
+// registers holding the loads in flight.  With a CTA a row, and the read back of the cache behind it, 128 us; now 91.  One sequence's 32 rows: 2.9 us.
 #include <algorithm>
 
 #include "fd_fp4.cuh"
