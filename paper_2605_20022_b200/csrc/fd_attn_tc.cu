@@ -125,8 +125,8 @@ struct Cfg {
     static constexpr int kScanOffset = kBarOffset + 720;         // SelfScans: the scans of a call that plans for itself
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
-    static constexpr int kFp4Offset = kBarOffset + 3072;         // FP4: Fp4Shared
-    static constexpr int kSmemBytes = kBarOffset + 3072 + (FP4 ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kFp4Offset = kRbOffset + 1024;          // FP4: Fp4Shared
+    static constexpr int kSmemBytes = kRbOffset + 1024 + (FP4 ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
     static constexpr int kDescSlots = FP4 ? 8 : 4;  // ring of piece descriptors: see publish_piece
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
@@ -824,7 +824,7 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
     };
     auto rebase = [&](float to) {  // this thread's sum, from the reference it was formed against
         if (m != to) {
-            l *= m == -INFINITY ? 0.f : exp2f(m - to);
+            l = __fmul_rn(l, m == -INFINITY ? 0.f : exp2f(m - to));  // (rounded by itself: both passes below then add to the same)
             m = to;
         }
     };

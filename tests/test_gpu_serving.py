@@ -539,6 +539,27 @@ def test_attention_many_short_sequences(Hq, Hkv, d, batch, longest):
 
 
 @pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("Hq,Hkv,d,by", [(32, 8, 128, 4.0), (16, 2, 64, 4.0), (32, 8, 128, 12.0)])
+def test_attention_scores_that_rise_and_fall_along_the_sequence(Hq, Hkv, d, by, path):
+    """K drifts from tile to tile, so that half of the rows meet a new maximum in every tile (what was summed so far is
+    rescaled, again and again) and the other half never after the first."""
+    pl, ql, nm = [5000, 2100, 700, 90, 1], [32, 17, 32, 5, 1], [16, 0, 16, 0, 0]
+    step = wl.make_step("drift", wl.Shape(Hq, Hkv, d, 1000), pl, ql, nm, seed=int(by) + d)
+    kv = wl.make_kv(step)
+    for b in range(len(pl)):
+        for page in range(-(-(pl[b] + ql[b]) // 16)):
+            kv[step.page_table[b, page], 0] += by * (page // 8)
+    q, cache = wl.make_q(step), ref.make_cache(kv, rng_seed=5)
+    with Ctx(step, path, max_q_len=32) as ctx:
+        got, status = attn_gpu(ctx, step, q, cache)
+        assert status == 0
+        check(got, attn_ref(step, q, cache), "drift")
+        for _ in range(20):
+            again, _ = attn_gpu(ctx, step, q, cache)
+            assert np.array_equal(got, again), "two runs on the same inputs differ bitwise"
+
+
+@pytest.mark.parametrize("path", PATHS)
 @pytest.mark.parametrize("size,scale", [(3.0e5, 1e-7), (1e-6, 1e4), (8.0, 0.0), (1e30, 1e-32)])
 def test_attention_queries_of_any_size(path, size, scale):
     """Queries far outside and far inside fp16's range (the kernels may hold them in 16 bits, but not lose them): rows of one
