@@ -726,6 +726,7 @@ static fd_status fp4_rows(fd_ctx* c, int batch, int total_q_rows, const void* k,
     if (total_q_rows > 0 && (!k || !v)) return FD_ERR_INVALID_ARG;
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(kv_cache, 16)) return FD_ERR_INVALID_ARG;
     if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    if (2LL * c->cfg.n_kv_heads * fd::fp4_page_bytes(c->cfg.head_dim) > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;  // (places within a page are 32-bit)
     p->total_rows = total_q_rows; p->num_pages = num_pages; p->Hkv = c->cfg.n_kv_heads; p->d = c->cfg.head_dim;
     p->max_pages = c->cfg.max_pages_per_seq; p->max_q_len = c->cfg.max_q_len;
     p->k = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->v = static_cast<__nv_bfloat16*>(const_cast<void*>(v));

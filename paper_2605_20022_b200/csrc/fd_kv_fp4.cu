@@ -181,11 +181,15 @@ __global__ void __launch_bounds__(kThreads, READ ? 4 : 3) kv_rows_fp4_kernel(Fp4
 // A run is short enough for every SM to have some, and long enough for its look-ups to be few.
 template <bool READ>
 static void launch_rows(const Fp4RowsParams& p, cudaStream_t s) {
-    const int resident = 4 * p.n_sms, run = std::max(1, std::min(kRun, (p.total_rows + resident - 1) / resident));
-    const int grid = std::max(1, std::min((p.total_rows + run - 1) / run, resident));
-    // floor(e / (groups of a row)) as the high half of a product: exact, as e < 64 rows and 64 rows of groups squared stay below 2^32
-    const unsigned per_row = 2u * p.Hkv * (p.d / kFp4Group);
-    kv_rows_fp4_kernel<READ><<<grid, kThreads, 0, s>>>(p, run, 0xffffffffu / per_row + 1);
+    // The kernel takes floor(e / per_row), e < run * per_row, as the high half of a product with the reciprocal rounded up.  Before
+    // it is cut off that is too large by at most e / 2^32, and e / per_row is at least 1 / per_row below the next whole number: exact
+    // while run * per_row^2 < 2^32.  Longer rows (from 512 kv-heads of 128 on) get shorter runs; where a run is one row the quotient
+    // is 0, and so is the product with a reciprocal of 0.
+    const long long per_row = 2LL * p.Hkv * (p.d / kFp4Group), exact = 0xffffffffLL / (per_row * per_row);
+    const long long resident = 4LL * p.n_sms, wanted = std::min<long long>(kRun, (p.total_rows + resident - 1) / resident);
+    const int run = (int)std::max(1LL, std::min(wanted, exact));
+    const int grid = (int)std::max(1LL, std::min((p.total_rows + run - 1LL) / run, resident));
+    kv_rows_fp4_kernel<READ><<<grid, kThreads, 0, s>>>(p, run, run == 1 ? 0u : (unsigned)(0xffffffffLL / per_row + 1));
 }
 
 void launch_kv_append_fp4(const Fp4RowsParams& p, cudaStream_t s) { launch_rows<false>(p, s); }
