@@ -1,4 +1,5 @@
-"""GPU tests of the 4-bit cache: rows of a tile that no query owns, head counts far above the usual ones."""
+"""GPU tests of the 4-bit cache: consecutive attention calls under a pinned plan, rows of a tile that no query owns, head counts far
+above the usual ones."""
 import numpy as np
 import pytest
 import torch
@@ -7,12 +8,135 @@ import fp4_ref as ref
 import paper_2605_20022_b200 as fd
 from helpers import Ctx
 from paper_2605_20022_b200 import workload as wl
+from test_gpu_parity import PATHS, _random_step
+from test_gpu_serving import attn_ref, check
 
 pytestmark = pytest.mark.gpu
 
 
 def _bits(t):
     return t.view(torch.int16)
+
+
+# ---------------------------------------------------------------------------------------------- consecutive calls under a pin
+def _chain(ctx, step, n_blocks, layers, q0, pools, kv_pool, k_new, v_new, table, wait_between):
+    """Attention calls under one pinned plan.  A layer is (format, query, append): on 4-bit ("4") or bf16 ("b") pages, from q0 (0)
+    or the output k layers back (k), behind an append to the bf16 pool or not."""
+    T = step.total_q_rows
+    ints = [table, step.prefix_lens.cuda(), step.q_lens.cuda()]
+    nm, nb = step.n_mask.cuda(), n_blocks.cuda()
+    outs = [torch.full(q0.shape, float("nan"), dtype=torch.bfloat16, device="cuda") for _ in layers]
+    kv_pool = kv_pool.clone()
+    torch.cuda.synchronize()
+    fd.fd_plan_pin(ctx.h, step.batch, T, ints[1], ints[2], nm, nb)
+    for l, (fmt, back, append) in enumerate(layers):
+        x = outs[l - back] if back else q0
+        if append:
+            fd.fd_kv_append(ctx.h, step.batch, T, k_new, v_new, kv_pool, step.num_pages, *ints)
+        if fmt == "4":
+            fd.fd_attn_draft_verify_fp4(ctx.h, step.batch, T, x, pools[l % len(pools)], step.num_pages, *ints, nm, nb, 1.0, 1.0, outs[l])
+        else:
+            fd.fd_attn_draft_verify_blocks(ctx.h, step.batch, T, x, kv_pool, step.num_pages, *ints, nm, nb, outs[l])
+        if wait_between:
+            torch.cuda.synchronize()
+    fd.fd_plan_unpin(ctx.h)
+    return outs, fd.fd_last_device_status(ctx.h)
+
+
+# every start that a 4-bit call can make: behind a call that does not write its query (reading ahead), behind one that does, behind
+# an append to the other cache, behind a bf16 call; in runs, so that several calls may be under way at once
+LAYERS = [("4", 0, False), ("4", 0, False), ("4", 1, False), ("4", 0, False), ("4", 2, False), ("4", 0, True), ("4", 1, True),
+          ("b", 0, True), ("4", 0, False), ("4", 1, False), ("b", 1, False), ("4", 0, True)]
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("seed", list(range(400, 412)))
+def test_chain_of_attention_calls_under_a_pinned_plan(seed, path):
+    """With the promise that lets consecutive calls overlap, without it, and with the device idle between any two calls: the same
+    bits; and the 4-bit layers match the 64-bit reference on the queries they were given."""
+    step, nb = _random_step(seed)
+    if step.total_q_rows == 0:
+        pytest.skip("all blocks empty")
+    s, T = step.shape, step.total_q_rows
+    g = torch.Generator().manual_seed(seed)
+    q0 = wl.make_q(step).cuda()
+    caches = [ref.make_cache(wl.make_kv(step, l), rng_seed=seed) for l in range(2)]
+    pools = [torch.from_numpy(c).cuda() for c in caches]
+    kv_pool = wl.make_kv(step, 2).cuda()
+    k_new, v_new = (torch.randn((T, s.n_kv_heads, s.head_dim), generator=g).bfloat16().cuda() for _ in range(2))
+    args = (step, nb, LAYERS, q0, pools, kv_pool, k_new, v_new, step.page_table.cuda())
+    with Ctx(step, path) as ctx:
+        alone, status = _chain(ctx, *args, wait_between=True)
+        assert status == 0
+        for l, (fmt, back, _) in enumerate(LAYERS):
+            if fmt == "4":
+                fed = alone[l - back].cpu() if back else q0.cpu()
+                check(alone[l].double().cpu().numpy(), attn_ref(step, fed, caches[l % 2], nb), f"layer {l}")
+        for promise in (False, True):
+            fd.fd_calls_back_to_back(ctx.h, promise)
+            for _ in range(4):
+                outs, status = _chain(ctx, *args, wait_between=False)
+                assert status == 0
+                for l in range(len(LAYERS)):
+                    assert torch.equal(_bits(outs[l]), _bits(alone[l])), f"layer {l}, promise {promise}"
+
+
+@pytest.mark.parametrize("path", PATHS)
+def test_chain_with_page_ids_outside_the_pool(path):
+    """The sequences that need such a page get zeros in every layer, the others what they get without it."""
+    step = wl.make_step("bad", wl.Shape(8, 2, 128, 10), [700, 40, 2000, 300, 9], [8, 16, 9, 1, 30], [4, 0, 3, 0, 16], seed=8)
+    nb = torch.ones_like(step.n_mask)
+    s, T = step.shape, step.total_q_rows
+    g = torch.Generator().manual_seed(8)
+    pools = [torch.from_numpy(ref.make_cache(wl.make_kv(step, l))).cuda() for l in range(2)]
+    k_new, v_new = (torch.randn((T, s.n_kv_heads, s.head_dim), generator=g).bfloat16().cuda() for _ in range(2))
+    layers = [layer for layer in LAYERS if not layer[2]]  # (an append would find the bad ids too)
+    args = (step, nb, layers, wl.make_q(step).cuda(), pools, wl.make_kv(step, 2).cuda(), k_new, v_new)
+    table = step.page_table.clone()
+    table[1, 0], table[2, 100], table[2, 3] = step.num_pages, -1, 2 ** 31 - 1
+    row0 = np.concatenate([[0], np.cumsum(step.q_lens.numpy())])
+    with Ctx(step, path) as ctx:
+        good, status = _chain(ctx, *args, step.page_table.cuda(), wait_between=True)
+        assert status == 0
+        for promise in (False, True):
+            fd.fd_calls_back_to_back(ctx.h, promise)
+            for _ in range(3):
+                outs, status = _chain(ctx, *args, table.cuda(), wait_between=False)
+                assert status == fd.FD_DEV_BAD_PAGE
+                for l, out in enumerate(outs):
+                    for b in range(step.batch):
+                        rows = slice(int(row0[b]), int(row0[b + 1]))
+                        assert (out[rows] == 0).all() if b in (1, 2) else torch.equal(_bits(out[rows]), _bits(good[l][rows])), (l, b)
+
+
+def test_chain_whose_cache_is_the_output_before():
+    """The pages of every second call are the bytes that the call before it writes: nothing of them may be read ahead."""
+    step = wl.make_step("alias", wl.Shape(32, 1, 128, 10), [60, 10, 130], [9, 9, 9], [0, 0, 0], seed=12)
+    s, T = step.shape, step.total_q_rows
+    size = step.num_pages * 2 * ref.page_bytes(128)
+    q = wl.make_q(step).cuda()
+    assert size <= q.numel() * 2
+    pool = torch.from_numpy(ref.make_cache(wl.make_kv(step))).cuda()
+    ints = [step.page_table.cuda(), step.prefix_lens.cuda(), step.q_lens.cuda(), step.n_mask.cuda()]
+    with Ctx(step, fd.FD_ATTN_TCGEN05_PLANNED, max_q_len=9) as ctx:
+        def run(wait):
+            outs = [torch.zeros_like(q) for _ in range(8)]
+            torch.cuda.synchronize()
+            fd.fd_plan_pin(ctx.h, step.batch, T, *ints[1:])
+            for l, out in enumerate(outs):
+                cache = outs[l - 1].view(torch.uint8).view(-1)[:size] if l % 2 else pool
+                fd.fd_attn_draft_verify_fp4(ctx.h, step.batch, T, q, cache, step.num_pages, *ints, None, 1.0, 1.0, out)
+                if wait:
+                    torch.cuda.synchronize()
+            fd.fd_plan_unpin(ctx.h)
+            assert fd.fd_last_device_status(ctx.h) == 0
+            return outs
+
+        alone = run(True)
+        assert any((o[T - 1] != 0).any() for o in alone[1::2])
+        fd.fd_calls_back_to_back(ctx.h, True)
+        for _ in range(10):
+            assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(run(False), alone))
 
 
 # ---------------------------------------------------------------------------------------------- rows that no query owns
