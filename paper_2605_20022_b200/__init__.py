@@ -3,7 +3,7 @@
 Every function has the name and the argument order of its C entry point in
 ``include/flexdraft.h``; tensors are torch CUDA tensors whose ``data_ptr()`` is
 handed through unchanged (by ctypes, or for the calls made several times per layer by the
-native ``_marshal``).  All arithmetic runs inside the library's CUDA kernels.
+native ``_marshal`` where that has been built).  All arithmetic runs inside the library's CUDA kernels.
 If the library has not been built, or no CUDA device is present, the calls raise:
 there is no fallback path.
 """
@@ -31,6 +31,7 @@ EXPORTS = ["fd_create", "fd_destroy", "fd_attn_draft_verify", "fd_verify_accept"
            "fd_last_device_status", "fd_attn_path", "fd_attn_last_mode", "fd_launch_count", "fd_status_string",
            "fd_verify_accept_static", "fd_host_reserve", "fd_step_host", "fd_step_host_append", "fd_step_device", "fd_selftest_wait_timeout", "fd_attn_draft_verify_blocks", "fd_select_branch", "fd_draft_select", "fd_kv_append", "fd_plan_pin", "fd_plan_unpin", "fd_calls_back_to_back", "fd_verify_accept_sample", "fd_plan_ranges_host",
            "fd_kv_reserve", "fd_qk_norm_rope_append", "fd_kv_append_fp4", "fd_kv_read_fp4", "fd_attn_draft_verify_fp4"]
+_MARSHALLED = EXPORTS[-5:]  # the calls made several times per layer
 
 
 class fd_config(ctypes.Structure):
@@ -47,7 +48,7 @@ class FlexDraftError(RuntimeError):
 
 
 _lib = None
-_native = None  # the _marshal extension, bound to the loaded library
+_native = None  # the _marshal extension, bound to the loaded library, or what stands in for it
 
 
 def library_path() -> str:
@@ -61,7 +62,7 @@ def load() -> ctypes.CDLL:
         if not os.path.exists(_build.SO):
             raise FileNotFoundError(f"{_build.SO} is not built: run `python -m paper_2605_20022_b200._build`")
         lib = ctypes.CDLL(_build.SO)
-        vp, ci = ctypes.c_void_p, ctypes.c_int
+        vp, ci, cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_float
         lib.fd_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(fd_config)]
         lib.fd_destroy.argtypes = [vp]
         lib.fd_attn_draft_verify.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, vp]
@@ -89,13 +90,33 @@ def load() -> ctypes.CDLL:
         lib.fd_launch_count.restype = ctypes.c_int64
         lib.fd_status_string.argtypes = [ci]
         lib.fd_status_string.restype = ctypes.c_char_p
-        if not os.path.exists(_build.MARSHAL):
-            raise FileNotFoundError(f"{_build.MARSHAL} is not built: run `python -m paper_2605_20022_b200._build`")
-        from . import _marshal
-        _marshal.bind(_build.SO)
-        _native = _marshal
+        lib.fd_kv_reserve.argtypes = [vp, ci, ci] + [vp] * 10 + [ci, vp, vp, vp]
+        lib.fd_qk_norm_rope_append.argtypes = [vp, ci, vp, ctypes.c_int64, vp, vp, cf, vp, ci, ci, ci, vp, vp, vp, vp, ci, ci, cf, cf, vp]
+        lib.fd_kv_append_fp4.argtypes = [vp, ci, ci, vp, vp, vp, ci, vp, vp, vp, cf, cf, vp]
+        lib.fd_kv_read_fp4.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, cf, cf, vp, vp, vp]
+        lib.fd_attn_draft_verify_fp4.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, cf, cf, vp, vp]
+        try:
+            from . import _marshal
+        except ImportError:  # not built for this interpreter: the same calls, a few microseconds slower on the host
+            _native = _CtypesMarshal(lib)
+        else:
+            _marshal.bind(_build.SO)
+            _native = _marshal
         _lib = lib
     return _lib
+
+
+class _CtypesMarshal:
+    """The calls of ``_marshal`` through ctypes."""
+
+    def __init__(self, lib):
+        for name in _MARSHALLED:
+            setattr(self, name, self._call(getattr(lib, name)))
+
+    @staticmethod
+    def _call(function):
+        kinds = function.argtypes
+        return lambda *args: function(*[_ptr(a) if kind is ctypes.c_void_p else a for kind, a in zip(kinds, args, strict=True)])
 
 
 def _load_native():

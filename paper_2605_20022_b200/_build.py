@@ -1,11 +1,12 @@
 """Compile libflexdraft.so (all CUDA kernels + the C ABI) for sm_100a with nvcc, and the binding's native argument
-marshalling with gcc, in-tree."""
+marshalling with gcc (where there are gcc and Python's headers), in-tree."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sysconfig
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -39,7 +40,6 @@ def build_marshal(force: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Build if the library is missing or older than a source.  Returns its path."""
-    build_marshal(force)
     if force or _stale():
         nvcc = os.environ.get("NVCC", "nvcc")
         tmp = SO + f".tmp{os.getpid()}"
@@ -47,6 +47,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
               ["-I", os.path.join(ROOT, "include"), "-o", tmp] + sources()
         subprocess.run(cmd, check=True)
         os.replace(tmp, SO)
+    try:
+        build_marshal(force)
+    except (OSError, subprocess.CalledProcessError) as e:
+        warnings.warn(f"no native argument marshalling ({e}): the binding marshals through ctypes")
     return SO
 
 
