@@ -16,7 +16,6 @@ struct fd_ctx {
     int attn_path;     // resolved FD_ATTN_SIMT or FD_ATTN_TCGEN05
     int tc_choice;     // FD_ATTN_TCGEN05 (per call), FD_ATTN_TCGEN05_PLANNED or FD_ATTN_TCGEN05_SELF_PLANNED
     int last_mode;     // FD_TC_* of the last tensor-core call
-    int epoch;         // number of the last attention call (never 0 once a call was made)
     float scale_log2e;
     // scratch (device)
     unsigned char* pool;
@@ -162,7 +161,6 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->chain_append = false;
     c->after_attn = false;
     c->back_to_back = false;
-    c->epoch = 0;
     c->attn_path = (cfg->attn_path == FD_ATTN_SIMT || !tc_ok) ? FD_ATTN_SIMT : FD_ATTN_TCGEN05;
     // SIMT kernel: two 74 KB CTAs fit an SM; tensor-core kernel: one persistent CTA per SM
     c->n_ctas = c->attn_path == FD_ATTN_SIMT ? 2 * c->n_sms : c->n_sms;
@@ -181,7 +179,6 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     const size_t o_rb = take(NR * sizeof(fd::RowBlock));
     const size_t o_cuq = take((NR + 1) * sizeof(int));
     const size_t o_cut = take((NR + 1) * sizeof(int));
-    const size_t o_ok = take(B * sizeof(int));
     const size_t o_sc = take(2 * NR * cfg->n_kv_heads * sizeof(int));
     const size_t o_cf = take((size_t)c->n_ctas * sizeof(int));
     const size_t o_cs = take(((size_t)c->n_ctas + 1) * sizeof(int));
@@ -212,7 +209,6 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->plan.rb = reinterpret_cast<fd::RowBlock*>(c->pool + o_rb);
     c->plan.cu_q = reinterpret_cast<int*>(c->pool + o_cuq);
     c->plan.cu_tiles = reinterpret_cast<int*>(c->pool + o_cut);
-    c->plan.seq_bad = reinterpret_cast<int*>(c->pool + o_ok);
     c->plan.seg_count = reinterpret_cast<int*>(c->pool + o_sc);
     c->plan.cta_first = reinterpret_cast<int*>(c->pool + o_cf);
     c->plan.cta_start = reinterpret_cast<int*>(c->pool + o_cs);
@@ -865,8 +861,6 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
     if (tc) {
         if (fd::attn_tc_prepare(&c->tc_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
     }
-    c->epoch = c->epoch == 0x7fffffff ? 1 : c->epoch + 1;
-    p.epoch = c->epoch;
     // a pinned plan serves this call if it was made for exactly these lengths; anything else replaces it
     const bool reuse = c->pinned && batch == c->pin_batch && total_q_rows == c->pin_rows && prefix_lens == c->pin_pl &&
                        q_lens == c->pin_ql && n_mask == c->pin_nm && n_blocks == c->pin_nb;

@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
             for (int c = 0; c < D; ++c) qT[c * kMaxRows + r] = 0.f;
         }
 
+        bool bad = false;  // a page id outside the pool (the same in every thread)
         float m = -INFINITY, l = 0.f, acc[D];
 #pragma unroll
         for (int c = 0; c < D; ++c) acc[c] = 0.f;
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
                 if (pos0 >= kv_len) break;
                 int phys = p.page_table[(long long)b * p.max_pages + pos0 / 16];
                 if ((unsigned)phys >= (unsigned)p.num_pages) {  // never form an address from a bad id
-                    if (r == 0) flag_sequence(p, b);
+                    bad = true;
                     phys = 0;
                 }
                 __syncthreads();  // everyone is done with the previous page
@@ -169,13 +170,20 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
         }
 
         const bool complete = (t == seg_start) && (t_end == seg_end);
+        if (bad && r == 0) atomicOr(p.status, FD_DEV_BAD_PAGE);
         if (r < rows) {
             if (complete) {
-                store_out_row<D>(p.out + ((long long)(row0 + i) * p.Hq + kvh * p.G + g) * D, acc, p.out_scale / l);
+                float inv = p.out_scale / l;
+                if (bad) {  // defined output, zeros: by assignment, what came from a stand-in page may be inf or NaN
+                    inv = 0.f;
+#pragma unroll
+                    for (int c = 0; c < D; ++c) acc[c] = 0.f;
+                }
+                store_out_row<D>(p.out + ((long long)(row0 + i) * p.Hq + kvh * p.G + g) * D, acc, inv);
             } else {
                 const int slot = 2 * cta + (t == s_c ? 0 : 1);
                 p.part.m[slot * kMaxRows + r] = m;
-                p.part.l[slot * kMaxRows + r] = l;
+                p.part.l[slot * kMaxRows + r] = bad ? -1.f : l;  // (the merge kernel looks for it)
                 float4* o = partial_o4(p.part, D, slot, 0, r);
 #pragma unroll
                 for (int c = 0; c < D; c += 4) o[(c >> 2) * kMaxRows] = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);

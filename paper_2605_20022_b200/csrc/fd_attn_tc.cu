@@ -149,7 +149,8 @@ struct Bars {
     int desc_n;                // piece descriptors published so far (written by the Q load warp)
     int piece_ok;              // thread 0 of the softmax groups: the descriptor of the next piece is there
     int first;                 // a call that plans for itself: the row block that owns the first tile of this CTA's range
-    int bad;                   // a load warp of this CTA met a page id outside the pool
+    int bad;                   // bit (piece & 31): a load warp met a page id outside the pool in that piece (they run at most
+                               // as many pieces ahead as there are tile buffers, 14; the softmax groups clear the bit once past it)
 };
 static_assert(sizeof(Bars) <= 320, "Bars must fit in front of the range-start window");
 
@@ -172,7 +173,7 @@ static_assert(sizeof(Fp4Shared) <= 4096, "Fp4Shared must fit behind the row bloc
 // K (which = 0) or V (which = 1) load warp.
 template <int D, int MODE>
 __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnParams& p, int n_rb, unsigned char* ring, uint64_t* full,
-                                          uint64_t* empty, int which, const Range rg, uint64_t* k0_full, volatile int* bad, volatile int* abort) {
+                                          uint64_t* empty, int which, const Range rg, uint64_t* k0_full, int* bad, volatile int* abort) {
     using C = Cfg<D, MODE, false>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     constexpr int kOps = 8;  // pages of a tile: one box each
@@ -190,7 +191,7 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
     // writes the query block's own slots and nothing else: tiles of the prefix are read ahead, the wait comes before
     // the first tile that reaches into the block (pages are 16 tokens, tiles 128: no page lies in both kinds)
     bool waited = !p.early;
-    int bad_early = -1;
+    bool bad_early = false;
     while (w.t < e_c && ok) {
         const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
         const int32_t* table = p.page_table + (long long)pc.b * p.max_pages;
@@ -204,8 +205,8 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
             int id = table[pos >> 4];
             if ((unsigned)id >= (unsigned)p.num_pages) {  // never form an address from a bad id
                 if (!waited && p.early >= 2) { wait_prior_launch(); waited = true; }
-                if (waited) flag_sequence(p, pc.b); else bad_early = pc.b;  // (no global write ahead of the prior launch)
-                *bad = 1;
+                if (waited) atomicOr(p.status, FD_DEV_BAD_PAGE); else bad_early = true;  // (no global write ahead of the prior launch)
+                atomicOr(bad, 1 << (w.piece & 31));
                 id = 0;
             }
             return id;
@@ -218,7 +219,7 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
             if (!waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n))) {  // the launch before this one may write what this tile holds
                 wait_prior_launch();
                 waited = true;
-                if (bad_early >= 0) flag_sequence(p, bad_early);
+                if (bad_early) atomicOr(p.status, FD_DEV_BAD_PAGE);
             }
             if (!wait_all(&empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
 #if FD_STAGGER
@@ -259,7 +260,7 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
 // brings both (2304 bytes at d = 128).  Otherwise the K load warp's walk: see load_role.
 template <int D, int MODE>
 __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, unsigned char* raw, Fp4Shared* f4, const Range rg,
-                                              volatile int* bad, volatile int* abort) {
+                                              int* bad, volatile int* abort) {
     using C = Cfg<D, MODE, true>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     int issued = 0;
@@ -267,7 +268,7 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
     const int s_c = rg.s_c, e_c = rg.e_c;
     Walk w = {s_c, 0, {0, 0}, 0, rg.first};
     bool ok = true, waited = !p.early;
-    int bad_early = -1;
+    bool bad_early = false;
     while (w.t < e_c && ok) {
         const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
         const int32_t* table = p.page_table + (long long)pc.b * p.max_pages;
@@ -278,8 +279,8 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
             int id = table[pos >> 4];
             if ((unsigned)id >= (unsigned)p.num_pages) {  // never form an address from a bad id
                 if (!waited && p.early >= 2) { wait_prior_launch(); waited = true; }
-                if (waited) flag_sequence(p, pc.b); else bad_early = pc.b;
-                *bad = 1;
+                if (waited) atomicOr(p.status, FD_DEV_BAD_PAGE); else bad_early = true;
+                atomicOr(bad, 1 << (w.piece & 31));
                 id = 0;
             }
             return id;
@@ -292,7 +293,7 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
             if (!waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n))) {
                 wait_prior_launch();
                 waited = true;
-                if (bad_early >= 0) flag_sequence(p, bad_early);
+                if (bad_early) atomicOr(p.status, FD_DEV_BAD_PAGE);
             }
             if (!wait_all(&f4->raw_empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
             const int npg = min(8, (pc.kv_len - (pc.tile0 + j) * kTileTokens + 15) >> 4);
@@ -728,7 +729,7 @@ struct Stage {
 
 template <int D, int MODE, bool FP4, class IssueRound>
 __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, const unsigned char* stage, int n_other, int own_pos,
-                                             const float* own, int r, int cg, bool active, bool flagged, int kvh, int row0,
+                                             const float* own, int r, int cg, bool active, bool bad, int kvh, int row0,
                                              volatile int* abort, IssueRound issue_round) {
     using S = Stage<D, MODE, FP4>;
     constexpr int CW = D / 2;
@@ -775,7 +776,7 @@ __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, co
     if (!active) return;
     if (own_pos == n_other) add_own();
     __nv_bfloat16* dst = p.out + ((long long)(row0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * D + cg * CW;
-    if (flagged) {  // a page id of this sequence was bad: defined output, zeros (by assignment)
+    if (bad) {  // a page id of this sequence was bad: defined output, zeros (by assignment)
 #pragma unroll
         for (int c = 0; c < CW; ++c) acc[c] = 0.f;
         store_cols_bf16<CW>(dst, acc, 0.f);
@@ -957,6 +958,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         if (tid == 0) bars->piece_ok = wait_piece(bars, w.piece, abort);
         named_bar_sync(1, 256);
         if (!bars->piece_ok) break;
+        if (tid == 0 && bars->bad && w.piece > 0) atomicAnd(&bars->bad, ~(1 << ((w.piece - 1) & 31)));  // (all 256 threads are past that piece)
         const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
         const bool warp_active = (warp & 3) * 32 < pc.rows;
         const int i = r / p.G;
@@ -1155,8 +1157,9 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         if (s == 1) { a0 = ex[r]; a1 = ex[kMaxRows + r]; }
         constexpr int kChunks = D / 64;  // 32-column chunks per softmax group
         const bool do_read = !leave && warp_active;
-        // the load warps of this CTA have seen every page id of the segment by now
-        const bool zero_rows = pc.complete && sequence_flagged(p, pc.b);
+        // the load warps of this CTA have seen every page id of the piece by now (read where it is used: no register is held for it)
+        auto bad_piece = [&]() { return (*static_cast<volatile int*>(&bars->bad) >> (w.piece & 31)) & 1; };
+        const bool zero_rows = bad_piece();
         float o[kChunks][32];  // this thread's row, its group's half of the columns
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
@@ -1212,7 +1215,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
             // could not compute (it is giving up) counts as "saw no key"; a CTA whose load warps met a page id outside
             // the pool says so with a negative l
             if (r < pc.rows && s == 0) {
-                const float2 ml = !do_read ? make_float2(-INFINITY, 0.f) : make_float2(mm, bars->bad ? -1.f : L);
+                const float2 ml = !do_read ? make_float2(-INFINITY, 0.f) : make_float2(mm, bad_piece() ? -1.f : L);
                 unsigned char* blk = dest != cl_rank ? exch.g_block(dest) : exch.land + (size_t)cl_rank * exch.block;
                 *reinterpret_cast<float2*>(blk + exch.ml_off(rl)) = ml;
             }
@@ -1239,23 +1242,26 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 named_bar_sync(1, 256);
                 if (tid == 0 && !leave && !*abort) {
                     __threadfence();
-                    atomicAdd(seg_cnt + 1, 1);
+                    atomicAdd(seg_cnt + 1, bad_piece() ? 0x10001 : 1);  // (the upper half: pieces that met a page id outside the pool)
                 }
             } else {
                 if (tid == 0) {
                     // the n - 1 other pieces: all drawn before ours, so their CTAs are past their last tile
                     const unsigned long long t_start = global_ns();
                     bool there = false;
+                    int bad = 0;
                     for (uint32_t it = 0; !there; ++it) {
                         int v;
                         asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(seg_cnt + 1) : "memory");
-                        there = v >= n_pieces - 1;
+                        there = (v & 0xffff) >= n_pieces - 1;
+                        bad = v >> 16;
                         if (!there && (it & 15u) == 15u && (*abort || global_ns() - t_start > kWaitLimitNs)) break;
                     }
                     if (there) {
                         seg_cnt[0] = 0;  // everyone has drawn and delivered: ready for the next call
                         seg_cnt[1] = 0;
-                        bars->epi_flag |= 4;  // go: read after the barrier below, so that all 256 threads decide alike
+                        // go (8: zeros); read after the barrier below, so that all 256 threads decide alike
+                        bars->epi_flag |= 4 | ((bad | bad_piece()) != 0) << 3;
                     } else {
                         *abort = 1;
                     }
@@ -1289,8 +1295,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                     issue_round(0);
                     int own_pos = 0;
                     for (int c = c_first; c < cta; ++c) own_pos += max(cs.at(c), seg_t0) < min(cs.at(c + 1), seg_t1);
-                    // (after the acquire: every CTA of the segment has looked up its page ids by now)
-                    bars->epi_flag |= (own_pos << 16) | (sequence_flagged(p, pc.b) ? 8 : 0);
+                    bars->epi_flag |= own_pos << 16;
                 }
                 named_bar_sync(1, 256);  // orders the acquire before every thread's loads of the partials
                 const int rr = tid & (kMaxRows - 1), cg = tid >> 7;
@@ -1298,7 +1303,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 if ((bars->epi_flag & 4) && !leave) {
                     if (!stage_ok) {
                         if (rr < pc.rows)
-                            merge_row<D, D / 2>(p, cs, c_first, c_last, pc.b, pc.kvh, pc.row0, seg_t0, seg_t1, rr, cg, &o[0][0], cta);
+                            merge_row<D, D / 2>(p, cs, c_first, c_last, (bars->epi_flag & 8) != 0, pc.kvh, pc.row0, seg_t0, seg_t1, rr, cg, &o[0][0], cta);
                     } else {
                         merge_staged<D, MODE, FP4>(p, bars, stage, (int)((bars->epi_flag >> 8) & 0xff), (int)(bars->epi_flag >> 16), &o[0][0], rr, cg,
                                               rr < pc.rows, (bars->epi_flag & 8) != 0, pc.kvh, pc.row0, abort, issue_round);

@@ -40,9 +40,8 @@ struct Plan {
     int* cu_q;      // [n_rb+1] first query row of each row block
     int* cu_tiles;  // [n_rb+1] exclusive scan of the row blocks' tiles (per kv-head)
     int* cu_ne;     // [n_rb+1] exclusive scan of (tiles > 0)
-    int* seq_bad;   // [B]   number (AttnParams::epoch) of the last call that met a page id outside the pool in the sequence:
-                    //       equal to the running call's number = flagged, the sequence's rows are zeroed
-    int* seg_count; // [n_rb * Hkv][2] per segment: merge tickets drawn, partial pieces delivered (zero between calls)
+    int* seg_count; // [n_rb * Hkv][2] per segment: merge tickets drawn, partial pieces delivered (zero between calls); the upper half
+                    //       of the second counts the delivered pieces that met a page id outside the pool
     int* cta_first; // [n_ctas] row block that owns the first tile of each attention CTA's range
     int* cta_start; // [n_ctas + 1] first tile of each attention CTA's range (non-decreasing; [n_ctas] = total)
 };
@@ -85,7 +84,6 @@ struct AttnParams {
     int q_box_t;      // block rows per Q load box of the tensor-core kernel (see q_box_rows)
     int min_range_tiles;  // least tiles worth giving a CTA a range of its own
     int piece_cost;   // fixed cost of starting a segment in a range, in tiles (balances ranges with many short segments)
-    int epoch;        // number of this attention call on its context, never 0 (see Plan::seq_bad)
     int cluster;      // CTAs per cluster when every segment is split over one cluster, else 0
     int early;        // 1: the launch before this one on the stream is an attention or append call served by the same pinned
                       //    plan, which writes neither the plan nor the lengths nor the page table: they may be read
@@ -98,14 +96,6 @@ struct AttnParams {
     const unsigned char* kv4;  // the 4-bit cache (fd_fp4.cuh), nullptr in a call on bf16 pages
     float out_scale;           // what the merged output is multiplied by: 1, or v_scale of a 4-bit cache
 };
-
-// A sequence in which this call met a page id outside the pool: its rows are written as zeros.  The flag is the
-// call's own number, so nothing has to be cleared between calls.
-__device__ __forceinline__ void flag_sequence(const AttnParams& p, int b) {
-    p.plan.seq_bad[b] = p.epoch;
-    atomicOr(p.status, FD_DEV_BAD_PAGE);
-}
-__device__ __forceinline__ bool sequence_flagged(const AttnParams& p, int b) { return __ldcg(p.plan.seq_bad + b) == p.epoch; }
 
 // Hybrid mask of one query row, never materialised: key position j is visible iff
 //     j < limit  ||  (blk_lo <= j && j < blk_hi).
@@ -243,17 +233,18 @@ __device__ inline void store_cols_bf16(__nv_bfloat16* dst, const float* o, float
 // Combine the partial pieces of segment (b, kvh) = tiles [t0, t1), held by CTAs c_first..c_last, for query
 // row r (output row row0 + r / G), columns [cg * CW, (cg + 1) * CW), in CTA order (fixed, so the result does
 // not depend on timing), and write the bf16 output.  The caller guarantees that every piece has been
-// written and is visible.  A piece that saw no visible key for the row holds m = -inf, l = 0, O = 0.
+// written and is visible.  A piece that saw no visible key for the row holds m = -inf, l = 0, O = 0.  bad: a piece met a page id
+// outside the pool, the row's output is zeros (and every row's of the sequence: its segments all need the same pages).
 // `own` (or nullptr): the O values of CTA own_cta's piece for exactly this row and these columns, still in
 // the caller's registers -- the same numbers it stored, so using them instead of loading changes nothing.
 template <int D, int CW>
-__device__ inline void merge_row(const AttnParams& p, const CtaStarts& cs, int c_first, int c_last, int b, int kvh, int row0,
+__device__ inline void merge_row(const AttnParams& p, const CtaStarts& cs, int c_first, int c_last, bool bad, int kvh, int row0,
                                  int t0, int t1, int r, int cg, const float* own = nullptr, int own_cta = -1) {
     __nv_bfloat16* dst = p.out + ((long long)(row0 + r / p.G) * p.Hq + kvh * p.G + r % p.G) * D + cg * CW;
     float acc[CW];
 #pragma unroll
     for (int c = 0; c < CW; ++c) acc[c] = 0.f;
-    if (sequence_flagged(p, b)) {  // a page id of this sequence was bad: defined output, zeros
+    if (bad) {  // defined output, zeros
         store_cols_bf16<CW>(dst, acc, 0.f);
         return;
     }

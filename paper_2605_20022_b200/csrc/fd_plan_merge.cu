@@ -12,8 +12,8 @@
 // many short segments gets fewer tiles.
 //
 // The plan kernel checks the lengths (O(B) work, one CTA).  Page ids are checked where they are
-// used, by the attention kernels: a sequence with an id outside the pool is flagged in seq_bad,
-// read from page 0 instead, and has its output rows zeroed by the merge kernel.
+// used, by the attention kernels: page 0 is read in place of an id outside the pool, and the output rows are zeroed by
+// whoever writes them: the CTA that holds the whole segment, or the merge, which the piece's CTA tells.
 #include <algorithm>
 
 #include "fd_internal.cuh"
@@ -175,14 +175,18 @@ __global__ void __launch_bounds__(kMergeThreads) merge_kernel(AttnParams p) {
     if (r >= rows) return;
     const int ntiles = p.plan.cu_tiles[v + 1] - p.plan.cu_tiles[v];
     if (ntiles == 0) return;
-    const int b = p.plan.rb[v].b;
     const int t0 = p.Hkv * p.plan.cu_tiles[v] + kvh * ntiles, t1 = t0 + ntiles;
     CtaStarts cs = {};
     cs.g = p.plan.cta_start;
     const int c_first = range_owner(cs.g, p.n_ctas, t0), c_last = range_owner(cs.g, p.n_ctas, t1 - 1);
-    // an unsplit segment was written by the attention kernel itself; it is revisited only to zero it
-    if (segment_pieces(cs, c_first, c_last, t0, t1) <= 1 && !sequence_flagged(p, b)) return;
-    merge_row<D, D / 4>(p, cs, c_first, c_last, b, kvh, p.plan.cu_q[v], t0, t1, r, cg);
+    // an unsplit segment was written by the attention kernel itself
+    if (segment_pieces(cs, c_first, c_last, t0, t1) <= 1) return;
+    bool bad = false;  // a piece that met a page id outside the pool has left l < 0
+    for (int c = c_first; c <= c_last; ++c) {
+        const int sc = cs.at(c);
+        if (max(sc, t0) < min(cs.at(c + 1), t1)) bad = bad || p.part.l[(2 * c + (sc >= t0 ? 0 : 1)) * kMaxRows + r] < 0.f;
+    }
+    merge_row<D, D / 4>(p, cs, c_first, c_last, bad, kvh, p.plan.cu_q[v], t0, t1, r, cg);
 }
 
 void launch_merge(const AttnParams& p, cudaStream_t s) {

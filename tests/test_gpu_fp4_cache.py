@@ -1,4 +1,4 @@
-"""GPU tests of the 4-bit cache: consecutive attention calls under a pinned plan, rows of a tile that no query owns, head counts far
+"""GPU tests of the 4-bit cache: consecutive and captured attention calls, rows of a tile that no query owns, head counts far
 above the usual ones."""
 import numpy as np
 import pytest
@@ -109,6 +109,37 @@ def test_chain_with_page_ids_outside_the_pool(path):
                         assert (out[rows] == 0).all() if b in (1, 2) else torch.equal(_bits(out[rows]), _bits(good[l][rows])), (l, b)
 
 
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("Hq,Hkv,d,fp4", [(8, 4, 128, True), (8, 4, 64, True), (8, 4, 128, False), (8, 4, 64, False)])
+def test_page_ids_outside_the_pool_in_some_of_many_short_sequences(Hq, Hkv, d, fp4, path):
+    """Forty pieces of a tile for every CTA, a bad page in some: zeros in exactly those sequences."""
+    B = 1600
+    step = wl.make_step("many", wl.Shape(Hq, Hkv, d, 10), [(37 * b) % 50 for b in range(B)], [1 + b % 3 for b in range(B)], [0] * B, seed=3)
+    T, q, kv = step.total_q_rows, wl.make_q(step).cuda(), wl.make_kv(step)
+    cache = torch.from_numpy(ref.make_cache(kv)).cuda() if fp4 else kv.cuda()
+    ints = [step.prefix_lens.cuda(), step.q_lens.cuda(), step.n_mask.cuda()]
+    good = step.page_table.cuda()
+    seq = torch.repeat_interleave(torch.arange(B), step.q_lens).cuda()
+    with Ctx(step, path) as ctx:
+        def attend(table):
+            out = torch.full_like(q, float("nan"))
+            if fp4:
+                fd.fd_attn_draft_verify_fp4(ctx.h, B, T, q, cache, step.num_pages, table, *ints, None, 1.0, 1.0, out)
+            else:
+                fd.fd_attn_draft_verify(ctx.h, B, T, q, cache, step.num_pages, table, *ints, out)
+            return out, fd.fd_last_device_status(ctx.h)
+
+        want, status = attend(good)
+        assert status == 0 and torch.isfinite(want.float()).all()
+        for k in range(6):
+            bad = torch.rand(B, generator=torch.Generator().manual_seed(k)) < (0.01, 0.3, 0.9)[k % 3]
+            table = good.clone()
+            table[bad.cuda(), 0] = -5
+            out, status = attend(table)
+            hit = bad.cuda()[seq]
+            assert status == fd.FD_DEV_BAD_PAGE and (out[hit] == 0).all() and torch.equal(_bits(out[~hit]), _bits(want[~hit]))
+
+
 def test_chain_whose_cache_is_the_output_before():
     """The pages of every second call are the bytes that the call before it writes: nothing of them may be read ahead."""
     step = wl.make_step("alias", wl.Shape(32, 1, 128, 10), [60, 10, 130], [9, 9, 9], [0, 0, 0], seed=12)
@@ -137,6 +168,53 @@ def test_chain_whose_cache_is_the_output_before():
         fd.fd_calls_back_to_back(ctx.h, True)
         for _ in range(10):
             assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(run(False), alone))
+
+
+# ---------------------------------------------------------------------------------------------- captured calls
+@pytest.mark.parametrize("pin", [False, True])
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("fp4", [True, False])
+def test_captured_call_forgets_the_bad_page_of_an_earlier_replay(fp4, path, pin):
+    """Two calls in a graph, replayed with page ids outside the pool in some sequences, then in others, then in none: zeros where this
+    replay met one, and nowhere else."""
+    step = wl.make_step("replay", wl.Shape(8, 2, 128, 10), [700, 40, 2000, 300], [8, 16, 9, 1], [4, 0, 3, 0], seed=9)
+    T, q = step.total_q_rows, wl.make_q(step).cuda()
+    kv = wl.make_kv(step)
+    cache = torch.from_numpy(ref.make_cache(kv)).cuda() if fp4 else kv.cuda()
+    good = step.page_table.cuda()
+    ints = [good.clone(), step.prefix_lens.cuda(), step.q_lens.cuda(), step.n_mask.cuda()]
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    row0 = np.concatenate([[0], np.cumsum(step.q_lens.numpy())])
+    with Ctx(step, path) as ctx:
+        def body():
+            if pin:
+                fd.fd_plan_pin(ctx.h, step.batch, T, *ints[1:])
+            for out in outs:
+                if fp4:
+                    fd.fd_attn_draft_verify_fp4(ctx.h, step.batch, T, q, cache, step.num_pages, *ints, None, 1.0, 1.0, out)
+                else:
+                    fd.fd_attn_draft_verify(ctx.h, step.batch, T, q, cache, step.num_pages, *ints, out)
+            if pin:
+                fd.fd_plan_unpin(ctx.h)
+
+        body()
+        torch.cuda.synchronize()
+        want = outs[0].clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            body()
+        for bad in ((1,), (), (0, 2), (3,), (), (1, 2, 3), ()):
+            ints[0].copy_(good)
+            for b in bad:
+                ints[0][b, 1 if b < 3 else 18] = step.num_pages + b
+            for out in outs:
+                out.fill_(float("nan"))
+            graph.replay()
+            assert fd.fd_last_device_status(ctx.h) == (fd.FD_DEV_BAD_PAGE if bad else 0)
+            for out in outs:
+                for b in range(step.batch):
+                    rows = slice(int(row0[b]), int(row0[b + 1]))
+                    assert (out[rows] == 0).all() if b in bad else torch.equal(_bits(out[rows]), _bits(want[rows])), (bad, b)
 
 
 # ---------------------------------------------------------------------------------------------- rows that no query owns
