@@ -50,12 +50,15 @@
 // TMEM columns: S / P buffers [0,128) [128,256) [256,384), O [384,384+d).
 //
 // What bounds it: the tensor pipe needs 1024 clocks a tile (d = 128, 128 rows), the exponentials as many, shared memory
-// about 1550 (Q K^T reads 128 bytes a clock, widening writes what P V reads); measured are 2400 with full rows: 283 us for a
-// batch of 16 on a 32k prefix, 971 TFLOP/s, 59 % of the measured cuBLAS rate, 2.1 TB/s of cache.  What is missing is
-// latency: each of softmax, P V, Q K^T and widening hands over through a barrier (150 to 300 clocks a hand-over) with five
+// about 1550 (Q K^T reads 128 bytes a clock, widening writes what P V reads); measured are 2400 with full rows: a batch of
+// 16 on a 32k prefix takes 330 us call after call, 834 TFLOP/s, 51 % of the measured cuBLAS burst rate, 1.9 TB/s of cache
+// (283 us and 971 TFLOP/s in short runs, before the power cap lowers the clock).  What is missing is latency: each of softmax, P V, Q K^T and widening hands over through a barrier (150 to 300 clocks a hand-over) with five
 // warps to a scheduler.  A piece costs 6.8 us more than its tiles (first and last tile in two passes, O drained before the
 // next piece's first P V, code that is not in the instruction cache: unrolling the two-pass form made a batch of 64 go from
-// 141 to 163 us), which is what calls on many short sequences spend their time on.
+// 141 to 163 us).  By that fit a batch of 64 with 1-16 rows (133 us) spends 72 us on 68 tiles a CTA and 31 us on 4.5 pieces.  The
+// merges' live accumulators spill (536 bytes stored in the planned form, 680 in the self-planned one), and builds that differ
+// in a few instructions of the epilogue took from 132 to 151 us at batch 64.  Registers of the softmax warps 152 (all that the
+// launch has): fewer spills, but 371 us on the 32k prefix.
 // Measured and dropped, batch 16 on 32k / batch 64, one token each: S^T = K Q^T with K widened into TMEM, no K tile in shared
 // memory, 394 / 95-115 us, but 155-183 us at up to 16 rows; two S buffers and two accumulators, as in the bf16 form, 344 / 159;
 // four widening warps 472 / 190; four for K and four for V, 431 / 187.
@@ -325,7 +328,8 @@ constexpr int kWidenThreads = 256;
 template <int D>
 struct RawWords {  // a thread's part of a tile; all of it is read before anything is stored (a store orders the reads behind it)
     // (The raw tile is given back only when these words have been widened and stored.  Given back as soon as the reads had been
-    // issued, with nothing yet depending on them, one call in twelve on many short sequences found words of the next tile.)
+    // issued, with nothing yet depending on them, one call in twelve on many short sequences found words of the next tile.  Why is
+    // not established; the order as it is needs no more than that a store waits for the words it stores.)
     static constexpr int kChunks = D / 32;  // 32-element chunks of a token
     static constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
     uint4 codes[kPasses];

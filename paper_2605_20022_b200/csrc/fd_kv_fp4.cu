@@ -4,9 +4,10 @@
 // Neighbouring threads own neighbouring groups of a row, so both sides are contiguous across a warp.  A CTA takes a run of
 // rows: first a thread per row finds the row's sequence and page (a search and a dependent load), then all threads stream
 // the run's groups with nothing but loads and stores between them.
-// Bound by issue: 24 prompts of 8 heads of 64 (20 k rows, 41 MB in) take 23 us to append and 19 us to read back (floor of
-// both 15.4), half of the issue slots used.  With the look-up made for every group the two took 53 us, now 38 (34 from a graph).
-// A few rows (64 sequences, 1-16 each) are launch latency and the look-up: 9.9 us for both.
+// 24 prompts of 8 heads of 64 (20 k rows, 41 MB in) take 21 us to append and 17 us to read back, calls replayed from a graph (7.7 us
+// of bytes each).  The warps wait for their loads: half of the issue slots are used in the append, two fifths in the read.  One
+// behind the other through the Python entry points the two take 42 us; with the look-up made for every group they took 53.
+// A few rows (64 sequences, 1-16 each) are launch latency and the look-up: 5.8 and 4.2 us.
 #include <algorithm>
 
 #include "fd_fp4.cuh"

@@ -8,8 +8,10 @@
 //             pair lies in one lane;
 //   kGeneral  8 consecutive elements: the partner lies in the same lane (adjacent pairs) or rot_dim / 16 lanes away.
 // In 4 bits a scale group is four lanes (kHalves) or two.  12 KB in, 8 KB and the cache out per row of 32 + 8 + 8 heads of 128:
-// 9600 rows take 69 us (33 us of bytes), bound by issue -- half of the slots used with a quarter of the warps resident, the
-// registers holding the loads in flight.  With a CTA a row, and the read back of the cache behind it, 128 us; now 91.  One sequence's 32 rows: 2.9 us.
+// 9785 rows take 69 us into 4-bit pages and 66 into bf16 pages (33 and 37 us of bytes), calls replayed from a graph; adjacent
+// pairs 66 and 57, half of the head rotated 69 and 61.  The warps wait for their loads: a quarter of them is resident, as registers
+// hold the loads in flight, and half of the issue slots are used.  A CTA a row, and the read back of the cache behind it, took
+// 128 us, a warp a row 91.  One sequence's 32 rows: 2.9 us.
 #include <algorithm>
 
 #include "fd_fp4.cuh"
