@@ -362,7 +362,8 @@ fd_status fd_kv_reserve(fd_ctx* ctx, int batch, int total_q_rows, int32_t* page_
  *
  * A row whose slot is negative is padding: nothing is written for it.  A slot beyond the pool: k and v of the row are
  * not written (FD_DEV_BAD_PAGE).  A position outside [0, max_positions): nothing is written for the row
- * (FD_DEV_BAD_LENGTHS).  Two rows with the same slot leave one of the two there.
+ * (FD_DEV_BAD_LENGTHS).  Two rows of a call with the same slot leave a mixture of the two there (codes and scales are stored
+ * apart): give each row a slot of its own, as fd_kv_reserve does.
  * Arithmetic: fp32 throughout, each result rounded once, to bf16 or to 4 bits.
  */
 fd_status fd_qk_norm_rope_append(fd_ctx* ctx, int total_q_rows, const void* qkv, int64_t row_stride,
@@ -390,8 +391,8 @@ fd_status fd_qk_norm_rope_append(fd_ctx* ctx, int total_q_rows, const void* qkv,
  *                   bytes of scales
  *
  * When to choose it: it holds 3.6 times the tokens in the same memory.  Its attention is faster than the bf16 cache's on long
- * prefixes (32k: 330 to 380 us against 400 to 440 for a batch of 16), about as fast for a batch of 64 on 1k to 4k, and slower on small batches
- * (8 sequences: 44 us against 38; one: 14 against 12).
+ * prefixes (32k: 330 to 380 us against 400 to 440 for a batch of 16), about as fast for a batch of 64 on 1k to 4k, and slower
+ * on small batches (8 sequences: 44 us against 38; one: 14 against 12).
  *
  * fd_kv_append_fp4 is fd_kv_append for it, fd_kv_read_fp4 the reverse: k_out / v_out [T, Hkv, d] bf16 get the values held
  * at positions n_b .. n_b + Lq_b - 1 (any range of the sequence: pass the range's start as prefix_lens), rounded to bf16.
