@@ -17,7 +17,10 @@
  * append, and a whole step from host buffers.  Around them stand what a serving loop needs
  * next: pages out of a free list (fd_kv_reserve), norm, rotation and append in one pass
  * (fd_qk_norm_rope_append), and a cache held in 4 bits with the attention that reads it
- * (fd_kv_append_fp4, fd_kv_read_fp4, fd_attn_draft_verify_fp4).  Everything runs in
+ * (fd_kv_append_fp4, fd_kv_read_fp4, fd_attn_draft_verify_fp4).  Further out: the attention of
+ * the prompts a sequence begins with (fd_attn_prompt), a cache held in 8 bits (fd_kv_append_fp8,
+ * fd_kv_read_fp8, fd_attn_draft_verify_fp8), and the pages of sequences that branch and end
+ * (fd_kv_fork, fd_kv_free, fd_kv_compact, fd_kv_copy_pages).  Everything runs in
  * hand-written CUDA kernels; there is no CPU fallback.
  *
  * Conventions (all entry points)
@@ -70,13 +73,16 @@ enum {
     FD_DEV_BAD_PAGE = 2,      /* a page id needed by a sequence is outside [0, num_pages) */
     FD_DEV_TIMEOUT = 4,       /* a bounded device-side wait ran out; the kernel returned early */
     FD_DEV_BAD_ACCEPT = 8,    /* fd_kv_commit: accepted_len[b] >= q_lens[b] */
-    FD_DEV_NO_PAGES = 16      /* fd_kv_reserve: the free list holds fewer pages than the query blocks need */
+    FD_DEV_NO_PAGES = 16      /* fd_kv_reserve, fd_kv_fork: the free list holds fewer pages than the call needs */
 };
 
-/* How a paged KV cache holds its values (fd_qk_norm_rope_append). */
+/* How a paged KV cache holds its values (fd_qk_norm_rope_append, fd_kv_copy_pages). */
 enum {
     FD_KV_BF16 = 0,           /* [num_pages, 2, Hkv, P, d] bf16, the cache of fd_attn_draft_verify */
-    FD_KV_FP4 = 1             /* 4-bit pages, the cache of fd_attn_draft_verify_fp4 (see there) */
+    FD_KV_FP4 = 1,            /* 4-bit pages, the cache of fd_attn_draft_verify_fp4 (see there) */
+    FD_KV_FP8 = 2,            /* 8-bit pages, the cache of fd_attn_draft_verify_fp8 (see there; fd_kv_copy_pages only) */
+    FD_KV_ROWS = 3            /* no cache: [2, num_pages * P, Hkv, d] bf16, K rows then V rows, row = slot; what fd_attn_prompt and
+                                 fd_kv_append_fp8 take (fd_qk_norm_rope_append only) */
 };
 
 /* Which two elements of a head fd_qk_norm_rope_append rotates together (R = rot_dim). */
@@ -356,9 +362,9 @@ fd_status fd_kv_reserve(fd_ctx* ctx, int batch, int total_q_rows, int32_t* page_
  *   rope_style      FD_ROPE_HALVES or FD_ROPE_ADJACENT
  *   positions, slot_map   device, [T] int32 (fd_kv_reserve writes both)
  *   q_out           device, [T, Hq, d] bf16, 16-byte aligned, does not overlap qkv
- *   kv_cache        device, the cache of kv_format: bf16 pages (128-byte aligned) or 4-bit pages (16-byte aligned)
- *   kv_format       FD_KV_BF16 or FD_KV_FP4
- *   k_scale, v_scale   FD_KV_FP4: as in fd_kv_append_fp4; FD_KV_BF16: not used
+ *   kv_cache        device, the cache of kv_format: bf16 pages (128-byte aligned), 4-bit pages or rows (16-byte aligned)
+ *   kv_format       FD_KV_BF16, FD_KV_FP4 or FD_KV_ROWS
+ *   k_scale, v_scale   FD_KV_FP4: as in fd_kv_append_fp4; otherwise not used
  *
  * A row whose slot is negative is padding: nothing is written for it.  A slot beyond the pool: k and v of the row are
  * not written (FD_DEV_BAD_PAGE).  A position outside [0, max_positions): nothing is written for the row
@@ -417,6 +423,142 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, con
                                    int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
                                    const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks,
                                    float k_scale, float v_scale, void* out, void* stream);
+
+/*
+ * A KV cache held in 8 bits: attention over it, and the ways into and out of it.  Half the size of bf16 pages (0.504 of it at
+ * d = 128), four significant bits an element where the 4-bit cache has two.  (The paper keeps its cache in bf16; this is the
+ * library's own.)  The P tokens of a page share, for each kv-head and for K and V apart, one scale; every element is an e4m3 code:
+ *
+ *     value = code * scale
+ *     scale = the smallest power of two, from 2^-15 to 2^7, for which the largest magnitude among the block's tokens is at most
+ *             448 * scale (2^7 where none is: then larger elements, infinities too, are held as 57344)
+ *     code  = the e4m3 number nearest to x / scale                                     (nearest, ties to even; a NaN stays one)
+ *
+ *   cache layout    [num_pages, Hkv, 2, P * d + 16] bytes, 16-byte aligned: for each page and kv-head K then V, each as [P][d]
+ *                   codes followed by the scale as a 32-bit float and 12 bytes of zeros
+ *
+ * The block's tokens are those of its sequence at positions below n_b + Lq_b.  When tokens join a block that is begun, those at
+ * positions below n_b keep their values, expressed in the new scale: exactly, unless the scale has grown so far that a code
+ * falls among e4m3's subnormals, where it is rounded again (nearest, ties to even).  Bytes of positions no token owns are
+ * left as they are, and do not count for the scale.  So what a block holds depends on its tokens and, within those subnormals,
+ * on the order in which they came.
+ *
+ * fd_kv_append_fp8 is fd_kv_append for it, fd_kv_read_fp8 the reverse: k_out / v_out [T, Hkv, d] bf16 get the values held
+ * at positions n_b .. n_b + Lq_b - 1 (any range of the sequence: pass the range's start as prefix_lens), exactly.  Lq_b is not
+ * bounded by max_q_len in either.  A sequence that is skipped, or a slot whose page id is outside the pool, leaves its rows of
+ * k_out / v_out as zeros.  Arguments and device-detected errors are fd_kv_append's.  A page that two sequences of a call name is
+ * written by both: let each append to pages of its own, as fd_kv_reserve and fd_kv_fork hand out.  Neither call overlaps the
+ * calls around it: under a pinned plan the attention call behind one starts when it has completed.
+ *
+ * fd_attn_draft_verify_fp8 is fd_attn_draft_verify_blocks for it: same arguments (n_blocks may be NULL), same mask, same
+ * errors, same forms (FD_TC_*), pinned plans and overlap of consecutive attention calls included.  Slots no valid token owns may
+ * hold any bit pattern.  Arithmetic: the values of the cache enter exactly, q and the softmax weights as in
+ * fd_attn_draft_verify_fp4, sums in fp32; bf16 output.
+ */
+fd_status fd_kv_append_fp8(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
+                           void* kv_cache, int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
+                           const int32_t* q_lens, void* stream);
+fd_status fd_kv_read_fp8(fd_ctx* ctx, int batch, int total_q_rows, const void* kv_cache, int num_pages,
+                         const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens, void* k_out,
+                         void* v_out, void* stream);
+fd_status fd_attn_draft_verify_fp8(fd_ctx* ctx, int batch, int total_q_rows, const void* q, const void* kv_cache,
+                                   int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
+                                   const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks, void* out,
+                                   void* stream);
+
+/*
+ * Attention of whole prompts, or of chunks of them, over their own keys (what a sequence goes through before its first decode
+ * step; the paper starts behind it).  Sequences are packed one behind the other, rows [T, Hq, d] of q and [Tk, Hkv, d] of k and v;
+ * sequence b has Lq_b query rows and Lk_b keys, and its last row is the position of its last key.  Row i, q-head h:
+ *
+ *     out[row0_b + i, h, :] = sum_{j <= i + Lk_b - Lq_b} softmax_j( scale * <q[row0_b + i, h], k_b[j, h/G]> ) v_b[j, h/G]
+ *
+ * A row that sees no key (Lk_b < Lq_b has such rows, in front) becomes zeros.  Lengths are not bounded by max_q_len or by
+ * max_pages_per_seq; scale is the context's.
+ *
+ *   batch           B, 0 <= B <= max_batch (B = 0 is a no-op)
+ *   total_q_rows    T; must equal sum_b q_lens[b]          total_kv_rows   Tk; must equal sum_b kv_lens[b]
+ *   q, k, v         device, bf16, 16-byte aligned; row t of q starts at element t * q_stride, of k and v at t * kv_stride (multiples
+ *                   of 8, at least Hq * d and Hkv * d: slices of one projection's output will do); k and v NULL only with Tk = 0
+ *   q_lens          device, [B] int32
+ *   kv_lens         device, [B] int32, or NULL: the same as q_lens
+ *   out             device, [T, Hq, d] bf16, 16-byte aligned; fully overwritten; shares no bytes with q, k or v
+ *
+ * Inconsistent lengths zero all T rows (FD_DEV_BAD_LENGTHS).  Keys and values of a sequence never reach another one.  Within a
+ * sequence the elements of v are taken to be finite: an infinity or a NaN in v_b[j] reaches the rows in front of j whose last key
+ * lies in the same 128 keys.
+ * Arithmetic: bf16 inputs, fp32 scores / softmax / accumulation, softmax weights rounded to bf16 in front of the product with v,
+ * bf16 output.
+ */
+fd_status fd_attn_prompt(fd_ctx* ctx, int batch, int total_q_rows, int total_kv_rows, const void* q, int64_t q_stride,
+                         const void* k, const void* v, int64_t kv_stride, const int32_t* q_lens, const int32_t* kv_lens,
+                         void* out, void* stream);
+
+/*
+ * The pages of sequences that branch (several samples of one prompt), of sequences that end, and of a pool that is to be
+ * compacted.  Tables and lists are the same for all layers; each layer's cache then takes the copies (fd_kv_copy_pages).  (The paper
+ * describes no page management.)
+ *
+ *   shared   device, [num_pages] int32: owners of each page beyond its first; 0 for a free page and for one that has never been
+ *            forked.  fd_kv_reserve and fd_kv_commit hand out and release only pages behind a sequence's whole prefix pages,
+ *            which are never shared, and need not know of it.
+ *   page_table, prefix_lens   device, [batch, max_pages_per_seq] and [batch] int32, in/out
+ *   free_pages, n_free, n_free_out   the free list, as in fd_kv_reserve (n_free_out may be n_free itself)
+ *   num_pages * P < 2^31
+ *
+ * Call them between steps (behind fd_kv_commit): pages reserved for a query block that has not been committed are not looked at.
+ *
+ * fd_kv_fork: child children[i] becomes a copy of parents[i], for i ascending.  With n = prefix_lens[parent], f = floor(n / P):
+ *
+ *     page_table[child][p] = page_table[parent][p],  shared[that page] += 1                            for p < f
+ *     n % P > 0:  page_table[child][f] = the id popped from the free list;  copy_src[i], copy_dst[i] = page_table[parent][f], that id
+ *     otherwise copy_src[i] = copy_dst[i] = -1;  entries of the child's row behind these = -1;  prefix_lens[child] = n
+ *
+ * (what was in the child's row is not looked at: free it first).  copy_src, copy_dst: device, [n_forks] int32, written.  Too few
+ * ids on the list: nothing is done, the copies are -1 (FD_DEV_NO_PAGES).  An index outside [0, batch), a child named twice or named as
+ * a parent too, a length that is negative or beyond the table: nothing is done, the copies are -1 (FD_DEV_BAD_LENGTHS).  A page
+ * id outside the pool: not shared (its entry in the child's row is -1), or not copied (FD_DEV_BAD_PAGE).
+ *
+ * fd_kv_free: the sequences seqs[i] give their pages back, for i descending, from the last page of the prefix to the first:
+ *
+ *     shared[id] > 0:  shared[id] -= 1;      otherwise id is pushed onto the free list
+ *
+ * and page_table[seq][p] = -1, prefix_lens[seq] = 0.  (Freeing in the order of forking, or of reserving, leaves the list as it
+ * was before.)  An index outside [0, batch), a sequence listed twice, a length negative or beyond the table, a sequence of 2^21
+ * pages or more, 2^29 of them in all: nothing is done (FD_DEV_BAD_LENGTHS).  An id outside the pool, or held by more sequences than shared says: dropped, or pushed once
+ * (FD_DEV_BAD_PAGE).
+ *
+ * fd_kv_compact: the m = num_pages - n_free pages that are not on the free list move to ids 0 .. m - 1.  Pages below m stay; the
+ * i-th page in use at or above m (ascending) moves to the i-th free id below m:  copy_src[i], copy_dst[i].  Then
+ *
+ *     page_map[id] = where page id is now, -1 for a page that was free;  every id in the table is replaced by its page_map
+ *     shared moves with its pages (shared may be NULL);  free_pages[k] = num_pages - 1 - k for k < n_free (m on top)
+ *
+ *   page_map   device, [num_pages] int32, written          n_copies   device, [1] int32, written: moves
+ *   copy_src, copy_dst   device, [max_copies] int32, written, -1 behind the moves;  min(m, n_free) are enough
+ *
+ * An id listed twice or outside the pool (FD_DEV_BAD_PAGE), a list longer than the pool, more moves than max_copies
+ * (FD_DEV_BAD_LENGTHS): tables, list and shared stay, page_map is the identity, n_copies = 0, the copies are unspecified
+ * pairs of which none counts.
+ *
+ * fd_kv_copy_pages: page copy_dst[i] of one layer's cache becomes a copy of page copy_src[i], for i < *n_copies (NULL: for
+ * i < max_copies).  A pair with a negative id is skipped; one with an id beyond the pool too (FD_DEV_BAD_PAGE).  The copies of a call
+ * are made in no particular order: no page may be the target of two of them, or the target of one and the source of another.
+ *
+ *   kv_cache   device, the cache of kv_format (FD_KV_BF16, FD_KV_FP4, FD_KV_FP8), 16-byte aligned
+ */
+fd_status fd_kv_fork(fd_ctx* ctx, int n_forks, const int32_t* parents, const int32_t* children, int batch,
+                     int32_t* page_table, int32_t* prefix_lens, int32_t* shared, const int32_t* free_pages,
+                     const int32_t* n_free, int32_t* n_free_out, int num_pages, int32_t* copy_src, int32_t* copy_dst,
+                     void* stream);
+fd_status fd_kv_free(fd_ctx* ctx, int n_seqs, const int32_t* seqs, int batch, int32_t* page_table, int32_t* prefix_lens,
+                     int32_t* shared, int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int num_pages,
+                     void* stream);
+fd_status fd_kv_compact(fd_ctx* ctx, int batch, int32_t* page_table, int32_t* shared, int32_t* free_pages,
+                        const int32_t* n_free, int num_pages, int32_t* page_map, int max_copies, int32_t* copy_src,
+                        int32_t* copy_dst, int32_t* n_copies, void* stream);
+fd_status fd_kv_copy_pages(fd_ctx* ctx, int max_copies, const int32_t* n_copies, const int32_t* copy_src,
+                           const int32_t* copy_dst, void* kv_cache, int num_pages, int kv_format, void* stream);
 
 /*
  * Draft-side tail of the step (Sec. 4.2, Eq. 4; Sec. 4.3 "Selective verification", Eq. 5).  One row of

@@ -24,14 +24,16 @@ FD_ATTN_AUTO, FD_ATTN_SIMT, FD_ATTN_TCGEN05 = 0, 1, 2
 FD_ATTN_TCGEN05_PLANNED, FD_ATTN_TCGEN05_SELF_PLANNED = 3, 4
 FD_TC_PLANNED, FD_TC_SELF_PLANNED, FD_TC_CLUSTER = 0, 1, 2
 FD_DEV_NO_PAGES = 16
-FD_KV_BF16, FD_KV_FP4 = 0, 1
+FD_KV_BF16, FD_KV_FP4, FD_KV_FP8, FD_KV_ROWS = 0, 1, 2, 3
 FD_ROPE_HALVES, FD_ROPE_ADJACENT = 0, 1
 
 EXPORTS = ["fd_create", "fd_destroy", "fd_attn_draft_verify", "fd_verify_accept", "fd_kv_commit",
            "fd_last_device_status", "fd_attn_path", "fd_attn_last_mode", "fd_launch_count", "fd_status_string",
            "fd_verify_accept_static", "fd_host_reserve", "fd_step_host", "fd_step_host_append", "fd_step_device", "fd_selftest_wait_timeout", "fd_attn_draft_verify_blocks", "fd_select_branch", "fd_draft_select", "fd_kv_append", "fd_plan_pin", "fd_plan_unpin", "fd_calls_back_to_back", "fd_verify_accept_sample", "fd_plan_ranges_host",
-           "fd_kv_reserve", "fd_qk_norm_rope_append", "fd_kv_append_fp4", "fd_kv_read_fp4", "fd_attn_draft_verify_fp4"]
-_MARSHALLED = EXPORTS[-5:]  # the calls made several times per layer
+           "fd_kv_reserve", "fd_qk_norm_rope_append", "fd_kv_append_fp4", "fd_kv_read_fp4", "fd_attn_draft_verify_fp4",
+           "fd_kv_append_fp8", "fd_kv_read_fp8", "fd_attn_draft_verify_fp8", "fd_attn_prompt", "fd_kv_fork", "fd_kv_free",
+           "fd_kv_compact", "fd_kv_copy_pages"]
+_MARSHALLED = EXPORTS[-13:]  # the calls made several times per layer
 
 
 class fd_config(ctypes.Structure):
@@ -95,6 +97,15 @@ def load() -> ctypes.CDLL:
         lib.fd_kv_append_fp4.argtypes = [vp, ci, ci, vp, vp, vp, ci, vp, vp, vp, cf, cf, vp]
         lib.fd_kv_read_fp4.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, cf, cf, vp, vp, vp]
         lib.fd_attn_draft_verify_fp4.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, cf, cf, vp, vp]
+        i64 = ctypes.c_int64
+        lib.fd_kv_append_fp8.argtypes = [vp, ci, ci, vp, vp, vp, ci, vp, vp, vp, vp]
+        lib.fd_kv_read_fp8.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp]
+        lib.fd_attn_draft_verify_fp8.argtypes = [vp, ci, ci, vp, vp, ci, vp, vp, vp, vp, vp, vp, vp]
+        lib.fd_attn_prompt.argtypes = [vp, ci, ci, ci, vp, i64, vp, vp, i64, vp, vp, vp, vp]
+        lib.fd_kv_fork.argtypes = [vp, ci, vp, vp, ci, vp, vp, vp, vp, vp, vp, ci, vp, vp, vp]
+        lib.fd_kv_free.argtypes = [vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, ci, vp]
+        lib.fd_kv_compact.argtypes = [vp, ci, vp, vp, vp, vp, ci, vp, ci, vp, vp, vp, vp]
+        lib.fd_kv_copy_pages.argtypes = [vp, ci, vp, vp, vp, vp, ci, ci, vp]
         try:
             from . import _marshal
         except ImportError:  # not built for this interpreter: the same calls, a few microseconds slower on the host
@@ -272,6 +283,67 @@ def fd_attn_draft_verify_fp4(ctx, batch, total_q_rows, q, kv_cache, num_pages, p
 def fd_kv_fp4_page_bytes(head_dim: int, page_size: int = 16) -> int:
     """Bytes that one page of one kv-head takes in a 4-bit cache, for K or for V: codes, then scales."""
     return page_size * (head_dim // 2 + head_dim // 16)
+
+
+def fd_kv_append_fp8(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table, prefix_lens, q_lens, stream=None,
+                     raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_append_fp8(ctx, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table,
+                                                        prefix_lens, q_lens, _stream(stream))
+    return _check("fd_kv_append_fp8", code, raise_on_error) if code else code
+
+
+def fd_kv_read_fp8(ctx, batch, total_q_rows, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_out, v_out, stream=None,
+                   raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_read_fp8(ctx, batch, total_q_rows, kv_cache, num_pages, page_table, prefix_lens, q_lens,
+                                                      k_out, v_out, _stream(stream))
+    return _check("fd_kv_read_fp8", code, raise_on_error) if code else code
+
+
+def fd_attn_draft_verify_fp8(ctx, batch, total_q_rows, q, kv_cache, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks, out,
+                             stream=None, raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_attn_draft_verify_fp8(ctx, batch, total_q_rows, q, kv_cache, num_pages, page_table, prefix_lens,
+                                                                q_lens, n_mask, n_blocks, out, _stream(stream))
+    return _check("fd_attn_draft_verify_fp8", code, raise_on_error) if code else code
+
+
+def fd_kv_fp8_block_bytes(head_dim: int, page_size: int = 16) -> int:
+    """Bytes that one page of one kv-head takes in an 8-bit cache, for K or for V: codes, then the scale and zeros."""
+    return page_size * head_dim + 16
+
+
+def fd_attn_prompt(ctx, batch, total_q_rows, total_kv_rows, q, q_stride, k, v, kv_stride, q_lens, kv_lens, out, stream=None,
+                   raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_attn_prompt(ctx, batch, total_q_rows, total_kv_rows, q, q_stride, k, v, kv_stride, q_lens,
+                                                      kv_lens, out, _stream(stream))
+    return _check("fd_attn_prompt", code, raise_on_error) if code else code
+
+
+def fd_kv_fork(ctx, n_forks, parents, children, batch, page_table, prefix_lens, shared, free_pages, n_free, n_free_out, num_pages,
+               copy_src, copy_dst, stream=None, raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_fork(ctx, n_forks, parents, children, batch, page_table, prefix_lens, shared, free_pages,
+                                                  n_free, n_free_out, num_pages, copy_src, copy_dst, _stream(stream))
+    return _check("fd_kv_fork", code, raise_on_error) if code else code
+
+
+def fd_kv_free(ctx, n_seqs, seqs, batch, page_table, prefix_lens, shared, free_pages, n_free, n_free_out, num_pages, stream=None,
+               raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_free(ctx, n_seqs, seqs, batch, page_table, prefix_lens, shared, free_pages, n_free,
+                                                  n_free_out, num_pages, _stream(stream))
+    return _check("fd_kv_free", code, raise_on_error) if code else code
+
+
+def fd_kv_compact(ctx, batch, page_table, shared, free_pages, n_free, num_pages, page_map, max_copies, copy_src, copy_dst, n_copies,
+                  stream=None, raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_compact(ctx, batch, page_table, shared, free_pages, n_free, num_pages, page_map, max_copies,
+                                                     copy_src, copy_dst, n_copies, _stream(stream))
+    return _check("fd_kv_compact", code, raise_on_error) if code else code
+
+
+def fd_kv_copy_pages(ctx, max_copies, n_copies, copy_src, copy_dst, kv_cache, num_pages, kv_format=FD_KV_BF16, stream=None,
+                     raise_on_error=True) -> int:
+    code = (_native or _load_native()).fd_kv_copy_pages(ctx, max_copies, n_copies, copy_src, copy_dst, kv_cache, num_pages, kv_format,
+                                                        _stream(stream))
+    return _check("fd_kv_copy_pages", code, raise_on_error) if code else code
 
 
 def fd_draft_select(ctx, batch, total_mask_rows, max_blocks, draft_logits, bias, n_mask, n_blocks, threshold, mask_tokens,

@@ -6,7 +6,9 @@
 #include <new>
 
 #include "fd_fp4.cuh"
+#include "fd_fp8.cuh"
 #include "fd_internal.cuh"
+#include "fd_prompt.cuh"
 
 struct fd_ctx {
     fd_config cfg;
@@ -34,10 +36,14 @@ struct fd_ctx {
     float* sv_chunk_w;
     unsigned char* sv_flags;
     unsigned int* rs_ticket;     // page reservation
+    unsigned int* fk_ticket;     // fork
+    int* cp_failed;              // compaction
+    fd::PromptPlan prompt;       // work list of the prompt attention
     int* status;
     int max_rows;      // capacity of keys
     int max_rb;        // capacity of the row-block arrays of the plan
     void* tc_state;
+    void* prompt_state;
     long long launches;
     // a pinned plan: the work list of one step, reused by every attention call with these lengths
     bool pinned;
@@ -101,10 +107,21 @@ static fd::AttnParams attn_params(fd_ctx* c, int batch, int total_q_rows, const 
     return p;
 }
 
+// Bytes of one page of K, or of V, of one kv-head.
+static long long block_bytes(int fmt, int d) {
+    return fmt == FD_KV_FP8 ? fd::fp8_block_bytes(d) : fmt == FD_KV_FP4 ? fd::fp4_page_bytes(d) : 16 * d * 2;
+}
+
+// Do [a, a + na) and [b, b + nb) share bytes?
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
 // A scale of a 4-bit cache: positive and finite.
 static bool good_scale(float s) { return s > 0.f && s <= 3.4028234e38f; }
 
-static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, bool fp4, float k_scale, float v_scale,
+static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, int fmt, float k_scale, float v_scale,
                            int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
                            const int32_t* n_mask, const int32_t* n_blocks, void* out, void* stream);
 
@@ -143,6 +160,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->cfg = *cfg;
     c->launches = 0;
     c->tc_state = nullptr;
+    c->prompt_state = nullptr;
     c->host = nullptr;
     c->pinned = false;
     c->pin_chain = false;
@@ -164,7 +182,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->attn_path = (cfg->attn_path == FD_ATTN_SIMT || !tc_ok) ? FD_ATTN_SIMT : FD_ATTN_TCGEN05;
     // SIMT kernel: two 74 KB CTAs fit an SM; tensor-core kernel: one persistent CTA per SM
     c->n_ctas = c->attn_path == FD_ATTN_SIMT ? 2 * c->n_sms : c->n_sms;
-    if (c->attn_path == FD_ATTN_SIMT && fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
+    if (c->attn_path == FD_ATTN_SIMT && (fd::attn_simt_prepare(cfg->head_dim) != cudaSuccess || fd::prompt_simt_prepare(cfg->head_dim) != cudaSuccess)) { cudaGetLastError(); delete c; return FD_ERR_CUDA; }
 
     const int B = cfg->max_batch, d = cfg->head_dim;
     const size_t slots = 2 * (size_t)c->n_ctas;
@@ -202,6 +220,9 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     const size_t o_svw = take((size_t)B * ds_chunks * sizeof(float));
     const size_t o_svf = take((size_t)c->max_rows);
     const size_t o_rst = take(sizeof(unsigned int));
+    const size_t o_fkt = take(sizeof(unsigned int));
+    const size_t o_cpf = take(sizeof(int));
+    const size_t o_pp = take((5 * (size_t)B + 4) * sizeof(int));
     const size_t o_stat = take(sizeof(int));
     if (cudaMalloc(&c->pool, off) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_WORKSPACE; }
     if (cudaMemset(c->pool, 0, off) != cudaSuccess) { cudaFree(c->pool); delete c; return FD_ERR_CUDA; }
@@ -231,6 +252,10 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->sv_chunk_w = reinterpret_cast<float*>(c->pool + o_svw);
     c->sv_flags = c->pool + o_svf;
     c->rs_ticket = reinterpret_cast<unsigned int*>(c->pool + o_rst);
+    c->fk_ticket = reinterpret_cast<unsigned int*>(c->pool + o_fkt);
+    c->cp_failed = reinterpret_cast<int*>(c->pool + o_cpf);
+    int* pp = reinterpret_cast<int*>(c->pool + o_pp);
+    c->prompt = {pp, pp + B + 1, pp + 2 * B + 2, pp + 3 * B + 2, pp + 4 * B + 2, pp + 5 * B + 3};
     c->status = reinterpret_cast<int*>(c->pool + o_stat);
     *out = c;
     return FD_OK;
@@ -240,6 +265,7 @@ fd_status fd_destroy(fd_ctx* c) {
     if (!c) return FD_OK;
     cudaDeviceSynchronize();
     fd::attn_tc_free(c->tc_state);
+    fd::prompt_tc_free(c->prompt_state);
     if (c->host) {
         HostStage* h = c->host;
         cudaStreamDestroy(h->h2d); cudaStreamDestroy(h->d2h);
@@ -443,7 +469,7 @@ fd_status fd_attn_draft_verify_blocks(fd_ctx* c, int batch, int total_q_rows, co
                                       int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
                                       const int32_t* q_lens, const int32_t* n_mask, const int32_t* n_blocks,
                                       void* out, void* stream) {
-    return attn_call(c, batch, total_q_rows, q, kv_cache, false, 1.f, 1.f, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
+    return attn_call(c, batch, total_q_rows, q, kv_cache, FD_KV_BF16, 1.f, 1.f, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
                      out, stream);
 }
 
@@ -452,8 +478,15 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* c, int batch, int total_q_rows, const
                                    const int32_t* n_mask, const int32_t* n_blocks, float k_scale, float v_scale, void* out,
                                    void* stream) {
     if (!good_scale(k_scale) || !good_scale(v_scale)) return FD_ERR_INVALID_ARG;
-    return attn_call(c, batch, total_q_rows, q, kv_cache, true, k_scale, v_scale, num_pages, page_table, prefix_lens, q_lens, n_mask,
+    return attn_call(c, batch, total_q_rows, q, kv_cache, FD_KV_FP4, k_scale, v_scale, num_pages, page_table, prefix_lens, q_lens, n_mask,
                      n_blocks, out, stream);
+}
+
+fd_status fd_attn_draft_verify_fp8(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, int num_pages,
+                                   const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
+                                   const int32_t* n_mask, const int32_t* n_blocks, void* out, void* stream) {
+    return attn_call(c, batch, total_q_rows, q, kv_cache, FD_KV_FP8, 1.f, 1.f, num_pages, page_table, prefix_lens, q_lens, n_mask, n_blocks,
+                     out, stream);
 }
 
 fd_status fd_plan_pin(fd_ctx* c, int batch, int total_q_rows, const int32_t* prefix_lens, const int32_t* q_lens,
@@ -678,7 +711,7 @@ fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, i
                                  void* kv_cache, int num_pages, int kv_format, float k_scale, float v_scale, void* stream) {
     if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
     if (!c || total_q_rows < 0 || total_q_rows > c->max_rows || num_pages < 0 || !(eps >= 0.f)) return FD_ERR_INVALID_ARG;
-    if (kv_format != FD_KV_BF16 && kv_format != FD_KV_FP4) return FD_ERR_INVALID_ARG;
+    if (kv_format != FD_KV_BF16 && kv_format != FD_KV_FP4 && kv_format != FD_KV_ROWS) return FD_ERR_INVALID_ARG;
     if (rope_style != FD_ROPE_HALVES && rope_style != FD_ROPE_ADJACENT) return FD_ERR_INVALID_ARG;
     const int d = c->cfg.head_dim, heads = c->cfg.n_q_heads + 2 * c->cfg.n_kv_heads;
     if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return FD_ERR_INVALID_ARG;
@@ -688,7 +721,7 @@ fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, i
     if (total_q_rows == 0) return FD_OK;
     if (!qkv || !slot_map || !q_out || !kv_cache) return FD_ERR_INVALID_ARG;
     if (!aligned(qkv, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(cos_sin, 16) || !aligned(q_out, 16) ||
-        !aligned(kv_cache, kv_format == FD_KV_FP4 ? 16 : 128))
+        !aligned(kv_cache, kv_format == FD_KV_BF16 ? 128 : 16))
         return FD_ERR_INVALID_ARG;
     if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
     // every row reads all of its heads before another thread's q could land there only if the two do not share bytes
@@ -704,6 +737,12 @@ fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, i
     p.q_out = static_cast<__nv_bfloat16*>(q_out);
     if (kv_format == FD_KV_FP4) p.kv4 = static_cast<unsigned char*>(kv_cache);
     else p.kv = static_cast<__nv_bfloat16*>(kv_cache);
+    const long long row = (long long)c->cfg.n_kv_heads * d;
+    if (kv_format == FD_KV_ROWS) {
+        p.page_step = 16 * row; p.tok_step = row; p.head_step = d; p.v_step = num_pages * 16LL * row;
+    } else {
+        p.page_step = 32 * row; p.tok_step = d; p.head_step = 16 * d; p.v_step = 16 * row;
+    }
     p.k_scale = k_scale; p.v_scale = v_scale; p.n_sms = c->n_sms; p.status = c->status;
     fd::launch_norm_rope(p, static_cast<cudaStream_t>(stream));
     c->launches += 1;
@@ -752,6 +791,155 @@ fd_status fd_kv_read_fp4(fd_ctx* c, int batch, int total_q_rows, const void* kv_
     const fd_status st = fp4_rows(c, batch, total_q_rows, k_out, v_out, kv_cache, num_pages, page_table, prefix_lens, q_lens, k_scale, v_scale, &p);
     if (st != FD_OK || batch == 0) return st;
     fd::launch_kv_read_fp4(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+// Rows into (append) or out of (read) an 8-bit cache: the checks and parameters the two share.
+static fd_status fp8_rows(fd_ctx* c, int batch, int total_q_rows, const void* k, const void* v, const void* kv_cache, int num_pages,
+                          const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens, fd::Fp8RowsParams* p) {
+    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
+    if (batch == 0) return total_q_rows == 0 ? FD_OK : FD_ERR_INVALID_ARG;
+    if (!page_table || !prefix_lens || !q_lens || !kv_cache) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && (!k || !v)) return FD_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(kv_cache, 16)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    if (2LL * c->cfg.n_kv_heads * block_bytes(FD_KV_FP8, c->cfg.head_dim) > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;  // (places within a page are 32-bit)
+    p->batch = batch; p->total_rows = total_q_rows; p->num_pages = num_pages; p->Hkv = c->cfg.n_kv_heads; p->d = c->cfg.head_dim;
+    p->max_pages = c->cfg.max_pages_per_seq;
+    p->k = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->v = static_cast<__nv_bfloat16*>(const_cast<void*>(v));
+    p->kv8 = static_cast<unsigned char*>(const_cast<void*>(kv_cache));
+    p->page_table = page_table; p->prefix_lens = prefix_lens; p->q_lens = q_lens; p->n_sms = c->n_sms; p->status = c->status;
+    return FD_OK;
+}
+
+fd_status fd_kv_append_fp8(fd_ctx* c, int batch, int total_q_rows, const void* k_new, const void* v_new, void* kv_cache,
+                           int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (the next attention call waits for this launch)
+    fd::Fp8RowsParams p;
+    const fd_status st = fp8_rows(c, batch, total_q_rows, k_new, v_new, kv_cache, num_pages, page_table, prefix_lens, q_lens, &p);
+    if (st != FD_OK || batch == 0) return st;
+    fd::launch_kv_append_fp8(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_read_fp8(fd_ctx* c, int batch, int total_q_rows, const void* kv_cache, int num_pages, const int32_t* page_table,
+                         const int32_t* prefix_lens, const int32_t* q_lens, void* k_out, void* v_out, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
+    fd::Fp8RowsParams p;
+    const fd_status st = fp8_rows(c, batch, total_q_rows, k_out, v_out, kv_cache, num_pages, page_table, prefix_lens, q_lens, &p);
+    if (st != FD_OK || batch == 0) return st;
+    fd::launch_kv_read_fp8(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_attn_prompt(fd_ctx* c, int batch, int total_q_rows, int total_kv_rows, const void* q, int64_t q_stride, const void* k,
+                         const void* v, int64_t kv_stride, const int32_t* q_lens, const int32_t* kv_lens, void* out, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (not a call on the paged cache)
+    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || total_kv_rows < 0) return FD_ERR_INVALID_ARG;
+    if (batch == 0) return total_q_rows == 0 && total_kv_rows == 0 ? FD_OK : FD_ERR_INVALID_ARG;
+    if (!q_lens || (!kv_lens && total_kv_rows != total_q_rows)) return FD_ERR_INVALID_ARG;
+    const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, d = c->cfg.head_dim;
+    if (q_stride < (int64_t)Hq * d || q_stride % 8 != 0 || q_stride > 0x7fffffffLL) return FD_ERR_INVALID_ARG;
+    if (kv_stride < (int64_t)Hkv * d || kv_stride % 8 != 0 || kv_stride > 0x7fffffffLL) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && (!q || !out)) return FD_ERR_INVALID_ARG;
+    if (total_q_rows > 0 && total_kv_rows > 0 && (!k || !v)) return FD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return FD_ERR_INVALID_ARG;
+    // an item's output is written while others still read
+    const size_t nq = total_q_rows ? ((size_t)(total_q_rows - 1) * q_stride + (size_t)Hq * d) * 2 : 0, no = (size_t)total_q_rows * Hq * d * 2;
+    const size_t nk = total_kv_rows ? ((size_t)(total_kv_rows - 1) * kv_stride + (size_t)Hkv * d) * 2 : 0;
+    if (overlap(out, no, q, nq) || overlap(out, no, k, nk) || overlap(out, no, v, nk)) return FD_ERR_INVALID_ARG;
+    fd::PromptParams p = {};
+    p.batch = batch; p.total_q = total_q_rows; p.total_kv = total_kv_rows;
+    p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.d = d; p.tile_tokens = fd::kMaxRows / p.G;
+    p.scale_log2e = c->scale_log2e;
+    p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);
+    p.q_stride = q_stride; p.kv_stride = kv_stride;
+    p.q_lens = q_lens; p.kv_lens = kv_lens;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.plan = c->prompt; p.n_ctas = c->n_ctas; p.status = c->status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;
+    if (tc && fd::prompt_tc_prepare(&c->prompt_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
+    fd::launch_prompt_plan(p, s);
+    c->launches += 1;
+    if (tc) {
+        if (fd::launch_prompt_tc(c->prompt_state, p, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
+        c->launches += 1;
+    } else if (total_q_rows > 0) {  // (no rows: the plan alone checks the lengths)
+        fd::launch_prompt_simt(p, s);
+        c->launches += 1;
+    }
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_fork(fd_ctx* c, int n_forks, const int32_t* parents, const int32_t* children, int batch, int32_t* page_table,
+                     int32_t* prefix_lens, int32_t* shared, const int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out,
+                     int num_pages, int32_t* copy_src, int32_t* copy_dst, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; c->pinned = false; }  // (rewrites lengths and tables)
+    if (!c || batch < 0 || batch > c->cfg.max_batch || n_forks < 0 || n_forks > batch || num_pages < 1) return FD_ERR_INVALID_ARG;
+    if (!free_pages || !n_free || !n_free_out) return FD_ERR_INVALID_ARG;
+    if (n_forks > 0 && (!parents || !children || !page_table || !prefix_lens || !shared || !copy_src || !copy_dst)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    fd::ForkParams p;
+    p.n_forks = n_forks; p.batch = batch; p.num_pages = num_pages; p.max_pages = c->cfg.max_pages_per_seq;
+    p.parents = parents; p.children = children; p.page_table = page_table; p.prefix_lens = prefix_lens; p.shared = shared;
+    p.free_pages = free_pages; p.n_free = n_free; p.n_free_out = n_free_out; p.copy_src = copy_src; p.copy_dst = copy_dst;
+    p.ticket = c->fk_ticket; p.n_sms = c->n_sms; p.status = c->status;
+    fd::launch_kv_fork(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_free(fd_ctx* c, int n_seqs, const int32_t* seqs, int batch, int32_t* page_table, int32_t* prefix_lens, int32_t* shared,
+                     int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int num_pages, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; c->pinned = false; }  // (rewrites lengths and tables)
+    if (!c || batch < 0 || batch > c->cfg.max_batch || n_seqs < 0 || n_seqs > batch || num_pages < 1) return FD_ERR_INVALID_ARG;
+    if (!free_pages || !n_free || !n_free_out) return FD_ERR_INVALID_ARG;
+    if (n_seqs > 0 && (!seqs || !page_table || !prefix_lens || !shared)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    fd::FreeParams p;
+    p.n_seqs = n_seqs; p.batch = batch; p.num_pages = num_pages; p.max_pages = c->cfg.max_pages_per_seq;
+    p.seqs = seqs; p.page_table = page_table; p.prefix_lens = prefix_lens; p.shared = shared;
+    p.free_pages = free_pages; p.n_free = n_free; p.n_free_out = n_free_out; p.status = c->status;
+    fd::launch_kv_free(p, static_cast<cudaStream_t>(stream));
+    c->launches += 1;
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_compact(fd_ctx* c, int batch, int32_t* page_table, int32_t* shared, int32_t* free_pages, const int32_t* n_free,
+                        int num_pages, int32_t* page_map, int max_copies, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies,
+                        void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; c->pinned = false; }  // (rewrites the tables)
+    if (!c || batch < 0 || batch > c->cfg.max_batch || num_pages < 1 || max_copies < 0) return FD_ERR_INVALID_ARG;
+    if (!free_pages || !n_free || !page_map || !n_copies || (batch > 0 && !page_table)) return FD_ERR_INVALID_ARG;
+    if (max_copies > 0 && (!copy_src || !copy_dst)) return FD_ERR_INVALID_ARG;
+    if ((long long)num_pages * c->cfg.page_size > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    fd::CompactParams p;
+    p.batch = batch; p.num_pages = num_pages; p.max_pages = c->cfg.max_pages_per_seq; p.max_copies = max_copies;
+    p.page_table = page_table; p.shared = shared; p.free_pages = free_pages; p.n_free = n_free; p.page_map = page_map;
+    p.copy_src = copy_src; p.copy_dst = copy_dst; p.n_copies = n_copies;
+    p.failed = c->cp_failed; p.n_sms = c->n_sms; p.status = c->status;
+    c->launches += fd::launch_kv_compact(p, static_cast<cudaStream_t>(stream));
+    return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+fd_status fd_kv_copy_pages(fd_ctx* c, int max_copies, const int32_t* n_copies, const int32_t* copy_src, const int32_t* copy_dst,
+                           void* kv_cache, int num_pages, int kv_format, void* stream) {
+    if (c) { c->pin_chain = false; c->after_attn = false; }  // (writes a cache)
+    if (!c || max_copies < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
+    if (kv_format != FD_KV_BF16 && kv_format != FD_KV_FP4 && kv_format != FD_KV_FP8) return FD_ERR_INVALID_ARG;
+    if (max_copies == 0) return FD_OK;
+    if (!copy_src || !copy_dst || !kv_cache || !aligned(kv_cache, 16)) return FD_ERR_INVALID_ARG;
+    fd::CopyPagesParams p;
+    p.max_copies = max_copies; p.num_pages = num_pages; p.n_copies = n_copies; p.src = copy_src; p.dst = copy_dst;
+    p.cache = static_cast<unsigned char*>(kv_cache);
+    p.page_bytes = 2LL * c->cfg.n_kv_heads * block_bytes(kv_format, c->cfg.head_dim);
+    if (p.page_bytes > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
+    p.n_sms = c->n_sms; p.status = c->status;
+    fd::launch_kv_copy_pages(p, static_cast<cudaStream_t>(stream));
     c->launches += 1;
     return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
 }
@@ -830,7 +1018,7 @@ fd_status fd_last_device_status(fd_ctx* c, int32_t* code, void* stream) {
 }  // extern "C"
 
 // The attention call on either cache.
-static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, bool fp4, float k_scale, float v_scale,
+static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q, const void* kv_cache, int fmt, float k_scale, float v_scale,
                            int num_pages, const int32_t* page_table, const int32_t* prefix_lens, const int32_t* q_lens,
                            const int32_t* n_mask, const int32_t* n_blocks, void* out, void* stream) {
     if (!c || batch < 0 || total_q_rows < 0 || num_pages < 0) return FD_ERR_INVALID_ARG;
@@ -840,15 +1028,16 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
     if (!page_table || !prefix_lens || !q_lens || !n_mask) return FD_ERR_INVALID_ARG;
     if (total_q_rows > 0 && (!q || !out)) return FD_ERR_INVALID_ARG;
     if (!kv_cache || num_pages == 0) return FD_ERR_INVALID_ARG;
-    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(kv_cache, fp4 ? 16 : 128) || !aligned(page_table, 4)) return FD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(kv_cache, fmt != FD_KV_BF16 ? 16 : 128) || !aligned(page_table, 4)) return FD_ERR_INVALID_ARG;
     if ((long long)num_pages * 2 * c->cfg.n_kv_heads * 16 > 0x7fffffffLL) return FD_ERR_UNSUPPORTED;
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     fd::AttnParams p = attn_params(c, batch, total_q_rows, prefix_lens, q_lens, n_mask, n_blocks);
     p.num_pages = num_pages;
     p.q = static_cast<const __nv_bfloat16*>(q);
-    if (fp4) {
-        p.kv4 = static_cast<const unsigned char*>(kv_cache);
+    p.fmt = fmt;
+    if (fmt != FD_KV_BF16) {
+        p.kvq = static_cast<const unsigned char*>(kv_cache);
         p.scale_log2e *= k_scale;
         p.out_scale = v_scale;
     } else {
@@ -872,7 +1061,7 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
         // (a table too narrow for four tiles per sequence leaves a cluster nothing to split)
         const bool splittable = (long long)p.max_pages * 16 >= 4 * fd::kTileTokens;
         const int cl = (c->tc_choice == FD_ATTN_TCGEN05 && batch <= fd::kSelfPlanMaxRb && n_seg <= fd::kClusterMaxSegments && splittable)
-                           ? fd::attn_tc_cluster_size(c->tc_state, fp4, n_seg, c->n_sms) : 0;
+                           ? fd::attn_tc_cluster_size(c->tc_state, fmt, n_seg, c->n_sms) : 0;
         if (cl >= 2) { mode = fd::kTcCluster; p.cluster = cl; }
         else if (batch <= fd::kSelfPlanMaxRb && !reuse) mode = fd::kTcSelfPlanned;
     }
@@ -890,7 +1079,7 @@ static fd_status attn_call(fd_ctx* c, int batch, int total_q_rows, const void* q
     // it only before its own first write), the append writes the cache
     if (p.early && tc && c->back_to_back) {
         const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), q1 = q0 + (size_t)total_q_rows * p.Hq * p.d * 2;
-        const size_t page = fp4 ? (size_t)fd::fp4_page_bytes(p.d) : (size_t)16 * p.d * 2;  // bytes of one head's K, or V
+        const size_t page = (size_t)block_bytes(fmt, p.d);  // bytes of one head's K, or V
         const uintptr_t k0 = reinterpret_cast<uintptr_t>(kv_cache), k1 = k0 + (size_t)num_pages * 2 * p.Hkv * page;
         bool clash = c->chain_out.size() >= 1024;  // (a chain that long is not a step of a model: stop keeping track)
         for (const auto& w : c->chain_out) clash = clash || (w.first < q1 && q0 < w.second) || (w.first < k1 && k0 < w.second);

@@ -7,9 +7,10 @@
 // n + i + 1 for a candidate row (causal, no mask token) and kv_len for a mask row (prefix,
 // candidates, whole mask block).  Softmax is the online form in the log2 domain.
 //
-// FP4: the same over 4-bit pages.  A page is widened to bf16 as it enters shared memory, which is exact (fd_fp4.cuh);
-// everything behind that is the same code.
+// FMT: the same over 4-bit or 8-bit pages.  A page is widened to bf16 as it enters shared memory, which is exact (fd_fp4.cuh,
+// fd_fp8.cuh); everything behind that is the same code.
 #include "fd_fp4.cuh"
+#include "fd_fp8.cuh"
 #include "fd_internal.cuh"
 
 namespace fd {
@@ -36,6 +37,25 @@ __device__ inline void widen_page(const unsigned char* src, __nv_bfloat16* dst) 
     }
 }
 
+// The same from 8 bits.
+template <int D>
+__device__ inline void widen_page8(const unsigned char* src, __nv_bfloat16* dst) {
+    const float s = *reinterpret_cast<const float*>(src + 16 * D);
+    for (int e = threadIdx.x; e < 16 * D / 8; e += kMaxRows) {
+        const uint2 codes = *reinterpret_cast<const uint2*>(src + e * 8);
+        uint32_t h[4];
+        e4m3x4_to_half(codes.x, h[0], h[1]);
+        e4m3x4_to_half(codes.y, h[2], h[3]);
+        __align__(16) __nv_bfloat162 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(as_half2(h[k]));
+            v[k] = __floats2bfloat162_rn(f.x * s, f.y * s);
+        }
+        reinterpret_cast<uint4*>(dst)[e] = *reinterpret_cast<const uint4*>(v);
+    }
+}
+
 template <int D>
 __device__ inline void store_out_row(__nv_bfloat16* dst, const float* o, float inv) {
 #pragma unroll
@@ -47,7 +67,7 @@ __device__ inline void store_out_row(__nv_bfloat16* dst, const float* o, float i
     }
 }
 
-template <int D, bool FP4>
+template <int D, int FMT>
 __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     float* qT = reinterpret_cast<float*>(smem_raw);                                   // [D][128], pre-scaled
@@ -110,9 +130,12 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
                     phys = 0;
                 }
                 __syncthreads();  // everyone is done with the previous page
-                if (FP4) {
-                    widen_page<D>(p.kv4 + fp4_page_offset(phys, p.Hkv, kvh, 0, D), ks);
-                    widen_page<D>(p.kv4 + fp4_page_offset(phys, p.Hkv, kvh, 1, D), vs);
+                if (FMT == FD_KV_FP4) {
+                    widen_page<D>(p.kvq + fp4_page_offset(phys, p.Hkv, kvh, 0, D), ks);
+                    widen_page<D>(p.kvq + fp4_page_offset(phys, p.Hkv, kvh, 1, D), vs);
+                } else if (FMT == FD_KV_FP8) {
+                    widen_page8<D>(p.kvq + fp8_block_offset(phys, p.Hkv, kvh, 0, D), ks);
+                    widen_page8<D>(p.kvq + fp8_block_offset(phys, p.Hkv, kvh, 1, D), vs);
                 } else {
                     const __nv_bfloat16* kp = p.kv + (((long long)phys * 2 + 0) * p.Hkv + kvh) * 16 * D;
                     const __nv_bfloat16* vp = p.kv + (((long long)phys * 2 + 1) * p.Hkv + kvh) * 16 * D;
@@ -197,21 +220,17 @@ __global__ void __launch_bounds__(kMaxRows) attn_simt_kernel(AttnParams p) {
 cudaError_t attn_simt_prepare(int d) {
     if (d != 128) return cudaSuccess;
     const int smem = 128 * kMaxRows * 4 + 2 * 16 * 128 * 2;
-    const cudaError_t e = cudaFuncSetAttribute(attn_simt_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(attn_simt_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(attn_simt_kernel<128, FD_KV_BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_simt_kernel<128, FD_KV_FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(attn_simt_kernel<128, FD_KV_FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
 
 void launch_attn_simt(const AttnParams& p, cudaStream_t s) {
     if (p.batch == 0) return;
     const int smem = p.d * kMaxRows * 4 + 2 * 16 * p.d * 2;
-    const bool fp4 = p.kv4 != nullptr;
-    if (p.d == 64) {
-        if (fp4) attn_simt_kernel<64, true><<<p.n_ctas, kMaxRows, smem, s>>>(p);
-        else attn_simt_kernel<64, false><<<p.n_ctas, kMaxRows, smem, s>>>(p);
-    } else {
-        if (fp4) attn_simt_kernel<128, true><<<p.n_ctas, kMaxRows, smem, s>>>(p);
-        else attn_simt_kernel<128, false><<<p.n_ctas, kMaxRows, smem, s>>>(p);
-    }
+    auto launch = [&](auto kernel) { kernel<<<p.n_ctas, kMaxRows, smem, s>>>(p); };
+    if (p.d == 64) launch(p.fmt == FD_KV_FP8 ? attn_simt_kernel<64, FD_KV_FP8> : p.fmt == FD_KV_FP4 ? attn_simt_kernel<64, FD_KV_FP4> : attn_simt_kernel<64, FD_KV_BF16>);
+    else launch(p.fmt == FD_KV_FP8 ? attn_simt_kernel<128, FD_KV_FP8> : p.fmt == FD_KV_FP4 ? attn_simt_kernel<128, FD_KV_FP4> : attn_simt_kernel<128, FD_KV_BF16>);
 }
 
 }  // namespace fd

@@ -40,16 +40,17 @@
 // Every wait is bounded.  A wait that runs out raises a CTA-wide abort flag: all roles leave
 // their loops, in-flight TMA copies are drained, TMEM is released and FD_DEV_TIMEOUT is set.
 //
-// 4-bit pages (FP4).  Same walk, same epilogue and merges; a tile differs in three places.
-//     loads    : codes and scales of K and V of a page lie side by side in the cache: one untiled bulk copy a page into a raw
-//                ring, 3.6 times fewer bytes than bf16;
-//     widening : eight warps turn a raw tile into fp16 K and V tiles in the layout the MMAs read.  code * scale has at most
-//                6 significant bits and e4m3's range, so fp16 holds it exactly; k_scale goes into the scale of the scores,
+// 4-bit and 8-bit pages (wide formats).  Same walk, same epilogue and merges; a tile differs in three places.
+//     loads    : codes and scales of a page come by untiled bulk copies into a raw ring: in 4 bits K and V of a page, which lie side
+//                by side, in one copy, 3.6 times fewer bytes than bf16; in 8 bits a tile's K and its V are stages of their own,
+//                half a tile's bytes each, in the order in which they are widened;
+//     widening : eight warps turn a raw tile into fp16 K and V tiles in the layout the MMAs read.  code * scale is exact in
+//                fp16 in both formats (fd_fp4.cuh, fd_fp8.cuh); k_scale goes into the scale of the scores,
 //                v_scale into the output.  Q is converted to fp16 by the same warps, a row against a power of two of its own;
 //     softmax  : P is fp16.  Three S / P buffers and one O; the groups take turns and share the reference of a row.
 // TMEM columns: S / P buffers [0,128) [128,256) [256,384), O [384,384+d).
 //
-// What bounds it: the tensor pipe needs 1024 clocks a tile (d = 128, 128 rows), the exponentials as many, shared memory
+// What bounds the 4-bit form: the tensor pipe needs 1024 clocks a tile (d = 128, 128 rows), the exponentials as many, shared memory
 // about 1550 (Q K^T reads 128 bytes a clock, widening writes what P V reads); measured are 2400 with full rows: a batch of
 // 16 on a 32k prefix takes 330 us call after call, 834 TFLOP/s, 51 % of the measured cuBLAS burst rate, 1.9 TB/s of cache
 // (283 us and 971 TFLOP/s in short runs, before the power cap lowers the clock).  What is missing is latency: each of softmax, P V, Q K^T and widening hands over through a barrier (150 to 300 clocks a hand-over) with five
@@ -65,10 +66,12 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <type_traits>
 #include <vector>
 
 #include "fd_attn_common.cuh"
 #include "fd_fp4.cuh"
+#include "fd_fp8.cuh"
 #include "fd_internal.cuh"
 #include "fd_sm100.cuh"
 
@@ -78,8 +81,11 @@ using namespace sm100;
 
 namespace {
 
+// A format whose pages are widened on their way to the MMAs (FMT: FD_KV_*).
+__host__ __device__ constexpr bool wide(int fmt) { return fmt != FD_KV_BF16; }
+
 // warps 0-3 softmax group 0, 4-7 softmax group 1, 8 K loads, 9 V loads, 10 MMA, 11 Q loads
-// (FP4: 8 loads both, 9 issues P V, 10 issues Q K^T, 12-19 widen)
+// (wide formats: 8 loads both, 9 issues P V, 10 issues Q K^T, 12-19 widen)
 constexpr int kKWarp = 8, kVWarp = 9, kMmaWarp = 10, kQWarp = 11;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kEarlyLoadMaxTiles = 96;     // longest range of a CTA that starts on its KV before the previous launch has completed
@@ -104,22 +110,23 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 #define FD_STAGGER 1
 #endif
 
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 struct Cfg {
-    static constexpr int kWidenWarps = FP4 ? 8 : 0;  // FP4: the warps behind warp 11 widen the tiles
+    static constexpr int kWidenWarps = wide(FMT) ? 8 : 0;  // the warps behind warp 11 widen the tiles
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
     // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps: the launch allocates 168 (bf16) or
-    // 96 (FP4) to each, and what the groups take adds up to no more than that.
-    static constexpr int kRegSoftmax = FP4 ? 144 : 224;
-    static constexpr int kRegHelper = FP4 ? 48 : 56;
+    // 96 (wide formats) to each, and what the groups take adds up to no more than that.
+    static constexpr int kRegSoftmax = wide(FMT) ? 144 : 224;
+    static constexpr int kRegHelper = wide(FMT) ? 48 : 56;
     static constexpr int kRegWiden = 64;
-    static_assert(!FP4 || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * 96, "register split");
-    // buffers in the K ring, and again in the V ring (FP4: of widened tiles, fed from the raw ring)
-    static constexpr int kStages = FP4 ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
+    static_assert(!wide(FMT) || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * 96, "register split");
+    // buffers in the K ring, and again in the V ring (wide formats: of widened tiles, fed from the raw ring)
+    static constexpr int kStages = wide(FMT) ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
     static constexpr int kQBytes = kMaxRows * D * 2;
     static constexpr int kKBytes = kTileTokens * D * 2;  // one K (or V) tile
-    static constexpr int kRawStages = FP4 ? (D == 128 ? 3 : 6) : 0;
-    static constexpr int kRawPage = 2 * fp4_page_bytes(D);   // K and V of one page of the kv-head lie side by side in the cache
+    static constexpr int kRawStages = wide(FMT) ? (D == 128 ? 3 : 6) : 0;
+    // one page of the kv-head in a stage: K and V, which lie side by side in the cache (FP4), or one of the two (FP8)
+    static constexpr int kRawPage = FMT == FD_KV_FP8 ? fp8_block_bytes(D) : 2 * fp4_page_bytes(D);
     static constexpr int kRawBytes = 8 * kRawPage;           // ... of a tile
     static constexpr int kRawOffset = kQBytes + 2 * kStages * kKBytes;
     static constexpr int kBarOffset = kRawOffset + kRawStages * kRawBytes;
@@ -128,9 +135,9 @@ struct Cfg {
     static constexpr int kScanOffset = kBarOffset + 720;         // SelfScans: the scans of a call that plans for itself
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
-    static constexpr int kFp4Offset = kRbOffset + 1024;          // FP4: Fp4Shared
-    static constexpr int kSmemBytes = kRbOffset + 1024 + (FP4 ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
-    static constexpr int kDescSlots = FP4 ? 8 : 4;  // ring of piece descriptors: see publish_piece
+    static constexpr int kWideOffset = kRbOffset + 1024;          // wide formats: WideShared
+    static constexpr int kSmemBytes = kRbOffset + 1024 + (wide(FMT) ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kDescSlots = wide(FMT) ? 8 : 4;  // ring of piece descriptors: see publish_piece
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
     // A K or V tile in shared memory: [8-token group][half of d][8 rows][128 B] -- what one TMA box per page
@@ -157,9 +164,9 @@ struct Bars {
 };
 static_assert(sizeof(Bars) <= 320, "Bars must fit in front of the range-start window");
 
-// What a call on 4-bit pages keeps beside Bars.
-struct Fp4Shared {
-    uint64_t raw_full[6], raw_empty[6];  // a tile of codes and scales has landed / has been widened
+// What a call on pages of a wide format keeps beside Bars.
+struct WideShared {
+    uint64_t raw_full[6], raw_empty[6];  // a stage of codes and scales has landed / has been widened
     uint64_t q_ready;                    // the Q tile of a piece has been turned into fp16
     // Three S / P buffers and one O (columns 0, 128, 256; 384): tile g uses buffer g % 3, the groups take turns.
     uint64_t s_full[3], p_full[3], pv_done[3];
@@ -170,7 +177,7 @@ struct Fp4Shared {
     float ref[2][kMaxRows];              // [piece & 1] the reference of each row, -inf while it has none
     Piece ring[8];                       // piece descriptors
 };
-static_assert(sizeof(Fp4Shared) <= 4096, "Fp4Shared must fit behind the row blocks");
+static_assert(sizeof(WideShared) <= 4096, "WideShared must fit behind the row blocks");
 
 
 // K (which = 0) or V (which = 1) load warp.
@@ -262,9 +269,9 @@ __device__ __forceinline__ void load_role(const CUtensorMap& tmap, const AttnPar
 // FP4 load warp: codes and scales of K and V of a page lie side by side in the cache, so one untiled bulk copy a page
 // brings both (2304 bytes at d = 128).  Otherwise the K load warp's walk: see load_role.
 template <int D, int MODE>
-__device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, unsigned char* raw, Fp4Shared* f4, const Range rg,
+__device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
                                               int* bad, volatile int* abort) {
-    using C = Cfg<D, MODE, true>;
+    using C = Cfg<D, MODE, FD_KV_FP4>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     int issued = 0;
     const uint64_t policy = make_policy_evict_first();
@@ -303,7 +310,78 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
             if (lane == 0) mbar_arrive_expect_tx(&f4->raw_full[st], npg * C::kRawPage);
             __syncwarp();
             if (lane < 8 && phys >= 0)
-                bulk_load_hint(raw + st * C::kRawBytes + lane * C::kRawPage, p.kv4 + fp4_page_offset(phys, p.Hkv, pc.kvh, 0, D), C::kRawPage,
+                bulk_load_hint(raw + st * C::kRawBytes + lane * C::kRawPage, p.kvq + fp4_page_offset(phys, p.Hkv, pc.kvh, 0, D), C::kRawPage,
+                               &f4->raw_full[st], policy);
+            issued = g + 1;
+        }
+        w.advance(pc);
+    }
+    if (*abort) {  // drain copies still in flight before the shared memory is given back
+        for (int g = max(0, issued - C::kRawStages); g < issued; ++g) {
+            const unsigned long long t0 = global_ns();
+            for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
+                if (mbar_try_wait(&f4->raw_full[g % C::kRawStages], (g / C::kRawStages) & 1)) break;
+        }
+    }
+}
+
+// FP8 load warp.  K and V of a tile are stages of their own, in the order in which the widening warps take them: K 0, K 1, V 0,
+// K 2, V 1, ..., the last V.  Stage i of a piece of nt tiles:
+__device__ __forceinline__ bool fp8_stage_is_k(int i, int nt) { return i == 0 || ((i & 1) && i != 2 * nt - 1); }
+__device__ __forceinline__ int fp8_k_stage(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int fp8_v_stage(int j, int nt) { return j == nt - 1 ? 2 * nt - 1 : 2 * j + 2; }
+
+template <int D, int MODE>
+__device__ __forceinline__ void load_role_fp8(const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
+                                              int* bad, volatile int* abort) {
+    using C = Cfg<D, MODE, FD_KV_FP8>;
+    const int lane = threadIdx.x & 31, cta = blockIdx.x;
+    int issued = 0;
+    const uint64_t policy = make_policy_evict_first();
+    const int s_c = rg.s_c, e_c = rg.e_c;
+    Walk w = {s_c, 0, {0, 0}, 0, rg.first};
+    bool ok = true, waited = !p.early;
+    bool bad_early = false;
+    while (w.t < e_c && ok) {
+        const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
+        const int32_t* table = p.page_table + (long long)pc.b * p.max_pages;
+        auto load_ids = [&](int batch) -> int {  // four tiles (32 pages, one per lane), one batch ahead
+            const int j = batch * 4 + (lane >> 3);
+            const int pos = ((pc.tile0 + j) * 8 + (lane & 7)) * 16;
+            if (!(j < pc.nt && pos < pc.kv_len)) return -1;
+            int id = table[pos >> 4];
+            if ((unsigned)id >= (unsigned)p.num_pages) {  // never form an address from a bad id
+                if (!waited && p.early >= 2) { wait_prior_launch(); waited = true; }
+                if (waited) atomicOr(p.status, FD_DEV_BAD_PAGE); else bad_early = true;
+                atomicOr(bad, 1 << (w.piece & 31));
+                id = 0;
+            }
+            return id;
+        };
+        int ids_cur = load_ids(0), ids_next = load_ids(1);
+        int j = -1, phys_k = -1, phys_before = -1;  // the last K's tile, this lane's page of it, and of the tile before
+        for (int i = 0; i < 2 * pc.nt; ++i) {
+            const int g = 2 * w.g0 + i, st = g % C::kRawStages, use = g / C::kRawStages;
+            const bool is_k = fp8_stage_is_k(i, pc.nt);
+            if (is_k) {
+                ++j;
+                if (j > 0 && (j & 3) == 0) { ids_cur = ids_next; ids_next = load_ids((j >> 2) + 1); }
+                phys_before = phys_k;
+                phys_k = __shfl_sync(0xffffffffu, ids_cur, (j & 3) * 8 + (lane & 7));
+            }
+            const bool last_v = i == 2 * pc.nt - 1;
+            const int tile = pc.tile0 + (is_k || last_v ? j : j - 1), phys = is_k || last_v ? phys_k : phys_before;
+            if (!waited && (p.early == 1 || (p.early == 3 && (tile + 1) * kTileTokens > pc.n))) {
+                wait_prior_launch();
+                waited = true;
+                if (bad_early) atomicOr(p.status, FD_DEV_BAD_PAGE);
+            }
+            if (!wait_all(&f4->raw_empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
+            const int npg = min(8, (pc.kv_len - tile * kTileTokens + 15) >> 4);
+            if (lane == 0) mbar_arrive_expect_tx(&f4->raw_full[st], npg * C::kRawPage);
+            __syncwarp();
+            if (lane < 8 && phys >= 0)
+                bulk_load_hint(raw + st * C::kRawBytes + lane * C::kRawPage, p.kvq + fp8_block_offset(phys, p.Hkv, pc.kvh, is_k ? 0 : 1, D), C::kRawPage,
                                &f4->raw_full[st], policy);
             issued = g + 1;
         }
@@ -375,6 +453,54 @@ __device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char*
     }
 }
 
+// The same for 8-bit pages: 16 codes a thread and pass, whose block's scale stands behind the page's codes.  Eight (d = 64: four)
+// neighbouring lanes share a token, so the reads are contiguous; of the two 16-byte words each lane stores, the lanes of the upper
+// half of d store the second first, which puts the eight lanes of a store on different banks.
+template <int D>
+struct RawWords8 {
+    static constexpr int kChunks = D / 16;
+    static constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
+    uint4 codes[kPasses];
+    float sc[kPasses];
+    __device__ __forceinline__ void load(const unsigned char* raw) {
+        const int t = (int)threadIdx.x - 384, c = t % kChunks;
+#pragma unroll
+        for (int it = 0; it < kPasses; ++it) {
+            const int tok = t / kChunks + it * (kWidenThreads / kChunks);
+            const unsigned char* page = raw + (tok >> 4) * fp8_block_bytes(D);
+            codes[it] = *reinterpret_cast<const uint4*>(page + (tok & 15) * D + c * 16);
+            sc[it] = *reinterpret_cast<const float*>(page + 16 * D);
+        }
+    }
+};
+
+template <int D, bool ZERO_TAIL>
+__device__ __forceinline__ void widen_tile(const RawWords8<D>& in, unsigned char* tile, int valid) {
+    constexpr int kChunks = RawWords8<D>::kChunks;
+    constexpr int kHalves = D / 64;
+    const int t = (int)threadIdx.x - 384, c = t % kChunks;
+    const bool swap = kHalves == 2 && (c & 4);
+#pragma unroll
+    for (int it = 0; it < RawWords8<D>::kPasses; ++it) {
+        const int tok = t / kChunks + it * (kWidenThreads / kChunks);
+        const __half2 s2 = __float2half2_rn(in.sc[it]);  // (a power of two from 2^-15 on: exact)
+        const bool dead = ZERO_TAIL && tok >= valid;
+        const uint4 cd = in.codes[it];
+        const uint32_t wd[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
+        unsigned char* row = tile + (tok >> 3) * (kHalves * 1024) + (c >> 2) * 1024 + (tok & 7) * 128;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint32_t h[4];
+            e4m3x4_to_half(wd[2 * k], h[0], h[1]);
+            e4m3x4_to_half(wd[2 * k + 1], h[2], h[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = dead ? 0u : as_u32(__hmul2(as_half2(h[i]), s2));
+            const int unit = (c & 3) * 2 + (swap ? k ^ 1 : k);
+            *reinterpret_cast<uint4*>(row + ((unit ^ (tok & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+    }
+}
+
 // The Q tile of a piece, bf16 -> fp16 in place, kPer neighbouring threads a row (of two, the second starts at unit 4 of its
 // part: its words then lie on the other banks).  A row is multiplied by the power of two that brings its
 // largest element into [2^14, 2^15): bf16's 8 bits then fit fp16 exactly down to 2^-31 of that element (below, the loss is
@@ -419,34 +545,41 @@ __device__ __forceinline__ void q_to_half(unsigned char* sq, float* row_scale, f
     if (part == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 141)), 1.17549435e-38f), 3.4028234e38f);
 }
 
-// FP4: the widening warps.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
+// Wide formats: the widening warps.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
 // is widened before its Q is touched, while that Q is still on its way.
-template <int D, int MODE>
+template <int D, int MODE, int FMT>
 __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv,
-                                           const unsigned char* raw, Bars* bars, Fp4Shared* f4, const Piece* ring, const Range rg,
+                                           const unsigned char* raw, Bars* bars, WideShared* f4, const Piece* ring, const Range rg,
                                            volatile int* abort) {
-    using C = Cfg<D, MODE, true>;
+    using C = Cfg<D, MODE, FMT>;
     const int lane = threadIdx.x & 31;
     Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
     while (w.t < rg.e_c) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
         const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
+        using Words = std::conditional_t<FMT == FD_KV_FP8, RawWords8<D>, RawWords<D>>;
         auto do_k = [&](int j) -> bool {
-            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
-            if (!wait_all(&f4->raw_full[rs], (g / C::kRawStages) & 1, abort)) return false;
-            RawWords<D> in;
+            const int g = w.g0 + j, st = g % C::kStages;
+            const int rg_ = FMT == FD_KV_FP8 ? 2 * w.g0 + fp8_k_stage(j) : g, rs = rg_ % C::kRawStages;
+            if (!wait_all(&f4->raw_full[rs], (rg_ / C::kRawStages) & 1, abort)) return false;
+            Words in;
             in.load(raw + rs * C::kRawBytes);
             if (!wait_all(&bars->k_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             widen_tile<D, false>(in, sk + st * C::kKBytes, 0);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->k_full[st]);
+            if (lane == 0) {
+                mbar_arrive(&bars->k_full[st]);
+                if (FMT == FD_KV_FP8) mbar_arrive(&f4->raw_empty[rs]);  // (as below)
+            }
             return true;
         };
         auto do_v = [&](int j) -> bool {
-            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
-            RawWords<D> in;  // (the tile has landed: do_k has waited for it)
-            in.load(raw + rs * C::kRawBytes + fp4_page_bytes(D));
+            const int g = w.g0 + j, st = g % C::kStages;
+            const int rg_ = FMT == FD_KV_FP8 ? 2 * w.g0 + fp8_v_stage(j, pc.nt) : g, rs = rg_ % C::kRawStages;
+            if (FMT == FD_KV_FP8 && !wait_all(&f4->raw_full[rs], (rg_ / C::kRawStages) & 1, abort)) return false;
+            Words in;  // (FP4: the tile has landed, do_k has waited for it)
+            in.load(raw + rs * C::kRawBytes + (FMT == FD_KV_FP8 ? 0 : fp4_page_bytes(D)));
             if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
             if (valid >= kTileTokens) widen_tile<D, false>(in, sv + st * C::kKBytes, 0);
@@ -488,15 +621,15 @@ __device__ __forceinline__ void zero_v_tail(unsigned char* vt, int valid, int la
 }
 
 // MMA issuing warp.
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv, Bars* bars,
-                                         Fp4Shared* f4, const Piece* ring, uint32_t tmem, const Range rg, volatile int* abort) {
-    using C = Cfg<D, MODE, FP4>;
+                                         WideShared* f4, const Piece* ring, uint32_t tmem, const Range rg, volatile int* abort) {
+    using C = Cfg<D, MODE, FMT>;
     const int lane = threadIdx.x & 31;
-    constexpr uint32_t idesc_qk = FP4 ? make_idesc_f16(128, kTileTokens, false) : make_idesc_bf16(128, kTileTokens, false);
+    constexpr uint32_t idesc_qk = wide(FMT) ? make_idesc_f16(128, kTileTokens, false) : make_idesc_bf16(128, kTileTokens, false);
     constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
     const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
-    const bool group_pv = FP4 || pv_by_group<MODE>(rg.e_c - rg.s_c);  // FP4: pv_role_fp4
+    const bool group_pv = wide(FMT) || pv_by_group<MODE>(rg.e_c - rg.s_c);  // wide formats: pv_role_wide
     if (p.early == 1) wait_prior_launch();  // (this role touches shared and tensor memory only; p.early >= 2 lets it run ahead)
     const uint64_t qd0 = make_smem_desc(smem_u32(sq), 16, 1024);
     const int s_c = rg.s_c, e_c = rg.e_c;
@@ -505,7 +638,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     while (w.t < e_c && ok) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) break;
         const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
-        if (!wait_all(FP4 ? &f4->q_ready : &bars->q_full, w.piece & 1, abort)) break;
+        if (!wait_all(wide(FMT) ? &f4->q_ready : &bars->q_full, w.piece & 1, abort)) break;
         auto issue_pv = [&](int jj) {  // (ranges whose P V this warp issues: see kGroupPvMinTiles)
             const int gg = w.g0 + jj, s = jj & 1, st = gg % C::kStages, u = w.u_base[s] + (jj >> 1);
             if (!wait_all(&bars->v_full[st], (gg / C::kStages) & 1, abort)) { ok = false; return; }
@@ -542,10 +675,10 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
             [[maybe_unused]] const int u_prev = w.u_base[s] + (j >> 1) - 1;  // the stream's previous tile, over all pieces
             const uint64_t kd0 = make_smem_desc(smem_u32(sk + st * C::kKBytes), 16, C::kGroupBytes);
 #if FD_QK_MODE != 0
-            if (!FP4 && u_prev >= 0 && !wait_all(&bars->pv_done[s], u_prev & 1, abort)) { ok = false; break; }
+            if (!wide(FMT) && u_prev >= 0 && !wait_all(&bars->pv_done[s], u_prev & 1, abort)) { ok = false; break; }
 #endif
-            if (FP4 && g >= 3 && !wait_all(&f4->pv_done[g % 3], ((g - 3) / 3) & 1, abort)) { ok = false; break; }
-            const uint32_t s_col = FP4 ? (uint32_t)(g % 3) * 128u : col_s[s];
+            if (wide(FMT) && g >= 3 && !wait_all(&f4->pv_done[g % 3], ((g - 3) / 3) & 1, abort)) { ok = false; break; }
+            const uint32_t s_col = wide(FMT) ? (uint32_t)(g % 3) * 128u : col_s[s];
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
@@ -555,7 +688,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
                             kd0 + (uint64_t)(((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
                 }
                 umma_commit(&bars->k_empty[st]);
-                umma_commit(FP4 ? &f4->s_full[g % 3] : &bars->s_full[s]);
+                umma_commit(wide(FMT) ? &f4->s_full[g % 3] : &bars->s_full[s]);
                 if (j == pc.nt - 1) umma_commit(&bars->q_free);  // the next piece's Q may come in
             }
             __syncwarp();
@@ -566,11 +699,11 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     }
 }
 
-// FP4: the warp that issues P V, in tile order (they add into one O; and Q K^T of the tiles ahead does not stand behind them).
-template <int D, int MODE>
-__device__ __forceinline__ void pv_role_fp4(unsigned char* sv, Bars* bars, Fp4Shared* f4, const Piece* ring, uint32_t tmem, const Range rg,
+// Wide formats: the warp that issues P V, in tile order (they add into one O; and Q K^T of the tiles ahead does not stand behind them).
+template <int D, int MODE, int FMT>
+__device__ __forceinline__ void pv_role_wide(unsigned char* sv, Bars* bars, WideShared* f4, const Piece* ring, uint32_t tmem, const Range rg,
                                             volatile int* abort) {
-    using C = Cfg<D, MODE, true>;
+    using C = Cfg<D, MODE, FMT>;
     constexpr uint32_t idesc = make_idesc_f16(128, D, true);
     Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
     while (w.t < rg.e_c) {
@@ -626,10 +759,10 @@ __host__ __device__ constexpr int cluster_share(int c) { return (kMaxRows + c - 
 // What one CTA hands one owner: the O rows as [d / 4 words][share rows][16 bytes], then (m, l) per row.
 __host__ __device__ constexpr uint32_t cluster_block_bytes(int c, int d) { return (uint32_t)((cluster_share(c) * (d * 4 + 8) + 15) / 16 * 16); }
 // Do the two scratch slots of a CTA, and the K ring where the blocks land, hold the c blocks of a cluster of c?
-// (FP4: the K and V rings, which lie side by side and are both idle by then.)
-__host__ __device__ constexpr bool cluster_fits(int c, int d, bool fp4) {
+// (Wide formats: the K and V rings, which lie side by side and are both idle by then.)
+__host__ __device__ constexpr bool cluster_fits(int c, int d, bool wide_format) {
     return (uint32_t)c * cluster_block_bytes(c, d) <= 2u * kMaxRows * d * 4 &&
-           (uint32_t)c * cluster_block_bytes(c, d) <= (uint32_t)(fp4 ? (d == 128 ? 4 : 8) : (d == 128 ? 3 : 6)) * kTileTokens * d * 2;
+           (uint32_t)c * cluster_block_bytes(c, d) <= (uint32_t)(wide_format ? (d == 128 ? 4 : 8) : (d == 128 ? 3 : 6)) * kTileTokens * d * 2;
 }
 
 // Addresses of the exchange.  In global memory: CTA `cta` of the grid owns scratch slots 2 cta and 2 cta + 1, one block
@@ -722,20 +855,20 @@ __device__ __forceinline__ void cluster_reduce(const AttnParams& p, const Exchan
 // this CTA's own piece -- the own_pos-th of the segment in CTA order -- is in registers (own: the thread's D / 2
 // columns).  Same arithmetic, same order as merge_row: the result does not depend on who merges.  Called by all 256
 // threads of the softmax groups (it holds barriers); `active`: the thread has a row to write.
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 struct Stage {
-    static constexpr uint32_t kBytes = Cfg<D, MODE, FP4>::kQBytes + 2 * Cfg<D, MODE, FP4>::kStages * Cfg<D, MODE, FP4>::kKBytes;
+    static constexpr uint32_t kBytes = Cfg<D, MODE, FMT>::kQBytes + 2 * Cfg<D, MODE, FMT>::kStages * Cfg<D, MODE, FMT>::kKBytes;
     static constexpr uint32_t kPieceBytes = kMaxRows * D * 4;
     static constexpr int kRound = (kBytes - 8192) / kPieceBytes;
     static constexpr uint32_t kMlOffset = kRound * kPieceBytes;
     static constexpr int kMaxOthers = (kBytes - kMlOffset) / (2 * kMaxRows * 4) - 1;
 };
 
-template <int D, int MODE, bool FP4, class IssueRound>
+template <int D, int MODE, int FMT, class IssueRound>
 __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, const unsigned char* stage, int n_other, int own_pos,
                                              const float* own, int r, int cg, bool active, bool bad, int kvh, int row0,
                                              volatile int* abort, IssueRound issue_round) {
-    using S = Stage<D, MODE, FP4>;
+    using S = Stage<D, MODE, FMT>;
     constexpr int CW = D / 2;
     const float* ml = reinterpret_cast<const float*>(stage + S::kMlOffset);  // [1 + n_other][2][128]
     float acc[CW];
@@ -790,14 +923,14 @@ __device__ __forceinline__ void merge_staged(const AttnParams& p, Bars* bars, co
 }
 
 // Two weights in the 16-bit type of the P V product.
-template <bool FP4>
+template <int FMT>
 __device__ __forceinline__ uint32_t pack16(float2 v) {
-    if (FP4) return as_u32(__floats2half2_rn(v.x, v.y));
+    if (wide(FMT)) return as_u32(__floats2half2_rn(v.x, v.y));
     const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
     return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-// One row of a tile in the FP4 kernel.  Both groups add into one O (three S / P buffers instead of two and a second
+// One row of a tile in the kernel of the wide formats.  Both groups add into one O (three S / P buffers instead of two and a second
 // accumulator: a group then finds its next S ready, where the chain softmax -> P V -> Q K^T of its own buffer used to stand
 // between two of its tiles), so a row's reference -- what its scores are taken against -- is shared by the two threads of
 // the row, and its changes have to follow the order of the tiles: a tile settles its reference after the tile before it
@@ -808,7 +941,7 @@ __device__ __forceinline__ uint32_t pack16(float2 v) {
 // they are formed (a chunk's weights only ever land on scores that have been read).
 // m, l: the reference and the sum of this thread's weights so far.
 template <int D>
-__device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_addr, float c, float head, bool masked, int lim, int blo, int bhi,
+__device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_addr, float c, float head, bool masked, int lim, int blo, int bhi,
                                                  int j, volatile float* ref, uint64_t* decided_before, uint32_t before_parity, uint64_t* decided,
                                                  uint64_t* pv_before, uint32_t pv_parity, volatile int* abort, float& m, float& l) {
     const int lane = threadIdx.x & 31;
@@ -928,23 +1061,23 @@ __device__ __forceinline__ void softmax_tile_fp4(uint32_t s_addr, uint32_t o_add
 }
 
 // The two softmax groups (256 threads).
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, float* ex, int* s_cs, const CtaStarts cs, const Piece* ring,
                                              uint32_t tmem, const Range rg, const Exchange<D> exch, int cl_rank, unsigned char* stage,
-                                             unsigned char* sv, Fp4Shared* f4, volatile int* abort) {
-    using C = Cfg<D, MODE, FP4>;
+                                             unsigned char* sv, WideShared* f4, volatile int* abort) {
+    using C = Cfg<D, MODE, FMT>;
     constexpr uint32_t idesc_pv = make_idesc_bf16(128, D, true);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     const int s_c = rg.s_c, e_c = rg.e_c;
     const int s = warp >> 2;                  // stream
     const int r = (warp & 3) * 32 + lane;     // query row == TMEM lane
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {FP4 ? 384u : 256u, 384u};
-    int chain = 0;                            // FP4: tiles this warp's rows have been through, both groups' (phase of decided)
-    float c = p.scale_log2e;  // (FP4: of this row and piece, from the conversion of q)
-    // FP4 holds P in fp16: everything is scaled by 2^7, so that weights between 2^-21 and, with the deferred rescaling, 2^15 keep
+    const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {wide(FMT) ? 384u : 256u, 384u};
+    int chain = 0;                            // wide formats: tiles this warp's rows have been through, both groups' (phase of decided)
+    float c = p.scale_log2e;  // (wide formats: of this row and piece, from the conversion of q)
+    // The wide formats hold P in fp16: everything is scaled by 2^7, so that weights between 2^-21 and, with the deferred rescaling, 2^15 keep
     // all of their bits; m carries the factor, so sums, partials and merges need not know
-    constexpr float kHead = FP4 ? 7.f : 0.f;
+    constexpr float kHead = wide(FMT) ? 7.f : 0.f;
     // fill the window of range starts; the barrier below orders it before its first use
     if (MODE == kTcPlanned && tid < kCsWindow) {  // (a call that plans for itself has filled it while planning)
         const int cc = cs.base + tid;
@@ -973,7 +1106,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         // arrives on p_full for them, and they wait at the epilogue's hardware barrier, not by polling.
         const int n_idle_threads = 32 * (4 - min(4, (pc.rows + 31) >> 5));
 
-        if constexpr (FP4) {
+        if constexpr (wide(FMT)) {
             for (int j = s; j < pc.nt && warp_active; j += 2) {
                 const int g = w.g0 + j, b3 = g % 3, e = chain + j;
                 if (!wait_all(&f4->s_full[b3], (g / 3) & 1, abort)) { ok = false; break; }
@@ -981,7 +1114,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 if (j < 2) c = f4->row_scale[w.piece & 3][r];
                 const int pos0 = (pc.tile0 + j) * kTileTokens;
                 // masked: the tile reaches into the query block (or past kv_len): the row's mask applies, in tile-local columns
-                softmax_tile_fp4<D>(tmem + lane_base + b3 * 128u, tmem + lane_base + 384u, c, kHead, pos0 + kTileTokens > pc.n, rm.limit - pos0,
+                softmax_tile_wide<D>(tmem + lane_base + b3 * 128u, tmem + lane_base + 384u, c, kHead, pos0 + kTileTokens > pc.n, rm.limit - pos0,
                                     rm.blk_lo - pos0, rm.blk_hi - pos0, j, &f4->ref[w.piece & 1][r], &f4->decided[warp & 3][(e - 1) & 1],
                                     (uint32_t)((e - 1) >> 1) & 1u, &f4->decided[warp & 3][e & 1], &f4->pv_done[(g + 2) % 3], (uint32_t)((g - 1) / 3) & 1u,
                                     abort, m, l);
@@ -991,7 +1124,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
             }
             if (warp_active) chain += pc.nt;
         }
-        for (int j = s; j < pc.nt && warp_active && !FP4; j += 2) {
+        for (int j = s; j < pc.nt && warp_active && !wide(FMT); j += 2) {
             const int u = w.u_base[s] + (j >> 1);
             if (!wait_all(&bars->s_full[s], u & 1, abort)) { ok = false; break; }
             tc_fence_after();
@@ -1111,7 +1244,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         const int seg_t0 = w.t - pc.tile0, seg_t1 = seg_t0 + pc.seg_nt;
         int c_first = cta, c_last = cta, n_pieces = 1, ticket = -1;  // (no ticket drawn: never the merger)
         int* seg_cnt = p.plan.seg_count + 2 * (pc.v * p.Hkv + pc.kvh);  // [0] tickets drawn, [1] partials delivered
-        using St = Stage<D, MODE, FP4>;
+        using St = Stage<D, MODE, FMT>;
         if (MODE != kTcCluster && !pc.complete) {
             segment_ctas(cs, p.n_ctas, cta, seg_t0, seg_t1, c_first, c_last);
             if (tid == 0 && !*abort) {
@@ -1119,16 +1252,16 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 ticket = atomicAdd(seg_cnt, 1);
             }
         }
-        if (FP4 && warp_active) {  // P V are issued in tile order by one warp: the last one has completed
+        if (wide(FMT) && warp_active) {  // P V are issued in tile order by one warp: the last one has completed
             const int g_last = w.g0 + pc.nt - 1;
             ok = ok && wait_all(&f4->pv_done[g_last % 3], (g_last / 3) & 1, abort);
         }
-        if (!FP4 && warp_active) {  // every P V of the piece has completed: the last one of each stream
+        if (!wide(FMT) && warp_active) {  // every P V of the piece has completed: the last one of each stream
             ok = ok && wait_all(&bars->pv_done[0], (w.u_base[0] + ((pc.nt + 1) >> 1) - 1) & 1, abort);
             if (pc.nt >= 2) ok = ok && wait_all(&bars->pv_done[1], (w.u_base[1] + (pc.nt >> 1) - 1) & 1, abort);
         }
         tc_fence_after();
-        const bool two = pc.nt >= 2 && !FP4;
+        const bool two = pc.nt >= 2 && !wide(FMT);
         // Stream exchange: group 1 hands its (m, l) to group 0, which answers with the two scale factors.
         // A thread only ever touches the two slots of its own row, so one barrier each way is enough.
         if (s == 1) { ex[r] = m; ex[kMaxRows + r] = l; }
@@ -1139,7 +1272,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
         const bool stage_ok = merger && w.t + pc.nt == e_c && (bars->epi_flag >> 8) <= St::kMaxOthers;  // uniform: from shared memory
         float a0 = 0.f, a1 = 0.f, mm = -INFINITY, L = 0.f;
         if (s == 0) {
-            if constexpr (FP4) {
+            if constexpr (wide(FMT)) {
                 // one O, against the row's last reference; the two threads' sums are brought there
                 const float m1 = ex[r], l1 = ex[kMaxRows + r];
                 mm = f4->ref[w.piece & 1][r];
@@ -1309,7 +1442,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                         if (rr < pc.rows)
                             merge_row<D, D / 2>(p, cs, c_first, c_last, (bars->epi_flag & 8) != 0, pc.kvh, pc.row0, seg_t0, seg_t1, rr, cg, &o[0][0], cta);
                     } else {
-                        merge_staged<D, MODE, FP4>(p, bars, stage, (int)((bars->epi_flag >> 8) & 0xff), (int)(bars->epi_flag >> 16), &o[0][0], rr, cg,
+                        merge_staged<D, MODE, FMT>(p, bars, stage, (int)((bars->epi_flag >> 8) & 0xff), (int)(bars->epi_flag >> 16), &o[0][0], rr, cg,
                                               rr < pc.rows, (bars->epi_flag & 8) != 0, pc.kvh, pc.row0, abort, issue_round);
                     }
                 }
@@ -1322,10 +1455,10 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
     if (MODE == kTcCluster && !cl_synced) cluster_sync_all();
 }
 
-template <int D, int MODE, bool FP4>
-__global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
+template <int D, int MODE, int FMT>
+__global__ void __launch_bounds__(Cfg<D, MODE, FMT>::kThreads, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
                                                               const AttnParams p_in) {
-    using C = Cfg<D, MODE, FP4>;
+    using C = Cfg<D, MODE, FMT>;
     extern __shared__ __align__(1024) unsigned char smem[];  // the swizzled tiles need 1024-byte alignment
     unsigned char* sq = smem;
     unsigned char* sk = smem + C::kQBytes;                      // K ring
@@ -1335,8 +1468,8 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
     int* s_cs = reinterpret_cast<int*>(smem + C::kCsOffset);
     SelfScans* scans = reinterpret_cast<SelfScans*>(smem + C::kScanOffset);
     RowBlock* rbs = reinterpret_cast<RowBlock*>(smem + C::kRbOffset);
-    Fp4Shared* f4 = reinterpret_cast<Fp4Shared*>(smem + C::kFp4Offset);  // FP4 only
-    Piece* ring = FP4 ? f4->ring : reinterpret_cast<Piece*>(smem + C::kDescOffset);
+    WideShared* f4 = reinterpret_cast<WideShared*>(smem + C::kWideOffset);  // wide formats only
+    Piece* ring = wide(FMT) ? f4->ring : reinterpret_cast<Piece*>(smem + C::kDescOffset);
     volatile int* abort = &bars->abort;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -1350,10 +1483,10 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
     //      griddepcontrol.wait below is where that launch's results are needed
     if (warp == 1 && lane == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(&bars->k_full[i], FP4 ? C::kWidenWarps : 1); mbar_init(&bars->k_empty[i], 1);  // FP4: the widening warps
-            mbar_init(&bars->v_full[i], FP4 ? C::kWidenWarps : 1); mbar_init(&bars->v_empty[i], 1);
+            mbar_init(&bars->k_full[i], wide(FMT) ? C::kWidenWarps : 1); mbar_init(&bars->k_empty[i], 1);  // wide formats: the widening warps
+            mbar_init(&bars->v_full[i], wide(FMT) ? C::kWidenWarps : 1); mbar_init(&bars->v_empty[i], 1);
         }
-        if (FP4) {
+        if (wide(FMT)) {
             for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], C::kWidenWarps); }
             mbar_init(&f4->q_ready, C::kWidenWarps);
             for (int i = 0; i < 3; ++i) { mbar_init(&f4->s_full[i], 1); mbar_init(&f4->p_full[i], 128); mbar_init(&f4->pv_done[i], 1); }
@@ -1376,7 +1509,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         mbar_fence_init();
     }
     if (warp == kMmaWarp) tmem_alloc(&bars->tmem_base, 512);
-    if (FP4 && tid < 2 * kMaxRows) f4->ref[tid / kMaxRows][tid % kMaxRows] = -INFINITY;
+    if (wide(FMT) && tid < 2 * kMaxRows) f4->ref[tid / kMaxRows][tid % kMaxRows] = -INFINITY;
     if (warp == kKWarp && lane == 0) { prefetch_tmap(&tmap); prefetch_tmap(&qmap); }
     // a call that plans for itself: warp 0 does so meanwhile (it needs the earlier kernels' results -- the lengths --
     // and waits for them on its own; its global loads then overlap the set-up of the other warps)
@@ -1483,24 +1616,26 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FP4>::kThreads, 1) attn_tc_kernel
         // Warp-specialised register budgets: the softmax groups keep a whole 128-column row of S in registers.
         // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168, what the launch allocated: the increase is served exactly by what
         // the decrease released (a request for more than that does not return).
-        // FP4: see Cfg.
+        // Wide formats: see Cfg.
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegSoftmax));
-        softmax_role<D, MODE, FP4>(p, bars, ex, s_cs, cs, ring, tmem, rg, exch, cl_rank, sq, sv, f4, abort);
+        softmax_role<D, MODE, FMT>(p, bars, ex, s_cs, cs, ring, tmem, rg, exch, cl_rank, sq, sv, f4, abort);
     } else {
-        if (FP4 && warp >= 12) {
+        if (wide(FMT) && warp >= 12) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegWiden));
         }
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegHelper));
-        if constexpr (FP4) {
+        if constexpr (wide(FMT)) {
             unsigned char* raw = smem + C::kRawOffset;
-            if (warp == kKWarp) load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
-            else if (warp == kVWarp) pv_role_fp4<D, MODE>(sv, bars, f4, ring, tmem, rg, abort);
-            else if (warp >= 12) widen_role<D, MODE>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
+            if (warp == kKWarp) {
+                if constexpr (FMT == FD_KV_FP8) load_role_fp8<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
+                else load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
+            } else if (warp == kVWarp) pv_role_wide<D, MODE, FMT>(sv, bars, f4, ring, tmem, rg, abort);
+            else if (warp >= 12) widen_role<D, MODE, FMT>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
         } else {
             if (warp == kKWarp) load_role<D, MODE>(tmap, p, n_rb, sk, bars->k_full, bars->k_empty, 0, rg, &bars->k_full[0], &bars->bad, abort);
             else if (warp == kVWarp) load_role<D, MODE>(tmap, p, n_rb, sv, bars->v_full, bars->v_empty, 1, rg, &bars->k_full[0], &bars->bad, abort);
         }
-        if (warp == kMmaWarp) mma_role<D, MODE, FP4>(p, sq, sk, sv, bars, f4, ring, tmem, rg, abort);
+        if (warp == kMmaWarp) mma_role<D, MODE, FMT>(p, sq, sk, sv, bars, f4, ring, tmem, rg, abort);
         else if (warp == kQWarp) q_role<D, C::kDescSlots>(qmap, p, n_rb, sq, bars, ring, rg, abort);
         if (MODE == kTcCluster) cluster_sync_all();  // the cluster barrier of the merge counts every thread
     }
@@ -1547,37 +1682,37 @@ struct TcState {
     int d, hkv;
     const CUtensorMap* current;
     const CUtensorMap* qcurrent;
-    // per cache format (0: bf16, 1: FP4): set up by its first call
-    bool ready[2];
-    int max_clusters[2][kMaxCluster + 1];  // [C]: clusters of C CTAs of the cluster kernel the device holds at once (0 = not launchable)
+    // per cache format (FD_KV_*): set up by its first call
+    bool ready[3];
+    int max_clusters[3][kMaxCluster + 1];  // [C]: clusters of C CTAs of the cluster kernel the device holds at once (0 = not launchable)
 };
 
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 cudaError_t configure_kernel() {
-    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MODE, FP4>::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MODE, FMT>::kSmemBytes);
     if (e == cudaSuccess && MODE == kTcCluster)
-        e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FP4>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FMT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     return e;
 }
 
 // How many clusters of `c` CTAs of the cluster kernel can be resident together (0 if such a launch is refused).
-template <int D, bool FP4>
+template <int D, int FMT>
 int query_clusters(int c, int n_sms) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((n_sms / c) * c);
-    cfg.blockDim = dim3(Cfg<D, kTcCluster, FP4>::kThreads);
-    cfg.dynamicSmemBytes = Cfg<D, kTcCluster, FP4>::kSmemBytes;
+    cfg.blockDim = dim3(Cfg<D, kTcCluster, FMT>::kThreads);
+    cfg.dynamicSmemBytes = Cfg<D, kTcCluster, FMT>::kSmemBytes;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kTcCluster, FP4>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
+    if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kTcCluster, FMT>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
     return n;
 }
 
-template <int D, int MODE, bool FP4>
+template <int D, int MODE, int FMT>
 void launch_mode(const TcState* st, const AttnParams& p, cudaStream_t s) {
     // Programmatic dependent launch: the CTAs may start while the previous launch on the stream (the plan kernel,
     // or the previous layer's call) is still running; they do their set-up and then wait for it inside the kernel.
@@ -1586,39 +1721,39 @@ void launch_mode(const TcState* st, const AttnParams& p, cudaStream_t s) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.n_ctas);
-    cfg.blockDim = dim3(Cfg<D, MODE, FP4>::kThreads);
+    cfg.blockDim = dim3(Cfg<D, MODE, FMT>::kThreads);
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cfg.dynamicSmemBytes = Cfg<D, MODE, FP4>::kSmemBytes;
+    cfg.dynamicSmemBytes = Cfg<D, MODE, FMT>::kSmemBytes;
     if (MODE == kTcCluster) {
         cfg.gridDim = dim3(p.batch * p.Hkv * p.cluster);  // one cluster per (sequence, kv-head) segment
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = p.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
-    cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, MODE, FP4>, *st->current, *st->qcurrent, p);
+    cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, MODE, FMT>, *st->current, *st->qcurrent, p);
 }
 
-template <int D, bool FP4>
+template <int D, int FMT>
 cudaError_t configure_format(TcState* st) {
-    cudaError_t e = configure_kernel<D, kTcPlanned, FP4>();
-    if (e == cudaSuccess) e = configure_kernel<D, kTcSelfPlanned, FP4>();
-    if (e == cudaSuccess) e = configure_kernel<D, kTcCluster, FP4>();
+    cudaError_t e = configure_kernel<D, kTcPlanned, FMT>();
+    if (e == cudaSuccess) e = configure_kernel<D, kTcSelfPlanned, FMT>();
+    if (e == cudaSuccess) e = configure_kernel<D, kTcCluster, FMT>();
     if (e != cudaSuccess) return e;
     int n_sms = 0, dev = 0;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev);
-    for (int c = 0; c <= kMaxCluster; ++c) st->max_clusters[FP4][c] = c >= 2 && cluster_fits(c, D, FP4) ? query_clusters<D, FP4>(c, n_sms) : 0;
-    st->ready[FP4] = true;
+    for (int c = 0; c <= kMaxCluster; ++c) st->max_clusters[FMT][c] = c >= 2 && cluster_fits(c, D, wide(FMT)) ? query_clusters<D, FMT>(c, n_sms) : 0;
+    st->ready[FMT] = true;
     return cudaSuccess;
 }
 
-template <int D, bool FP4>
+template <int D, int FMT>
 void launch_format(const TcState* st, const AttnParams& p, int mode, cudaStream_t s) {
-    if (mode == kTcCluster) launch_mode<D, kTcCluster, FP4>(st, p, s);
-    else if (mode == kTcSelfPlanned) launch_mode<D, kTcSelfPlanned, FP4>(st, p, s);
-    else launch_mode<D, kTcPlanned, FP4>(st, p, s);
+    if (mode == kTcCluster) launch_mode<D, kTcCluster, FMT>(st, p, s);
+    else if (mode == kTcSelfPlanned) launch_mode<D, kTcSelfPlanned, FMT>(st, p, s);
+    else launch_mode<D, kTcPlanned, FMT>(st, p, s);
 }
 
 }  // namespace
@@ -1639,13 +1774,16 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
         cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", reinterpret_cast<void**>(&st->encode), cudaEnableDefault, &qres);
         if (e != cudaSuccess || !st->encode) { delete st; return e != cudaSuccess ? e : cudaErrorNotSupported; }
         st->d = p.d; st->hkv = p.Hkv;
-        st->ready[0] = st->ready[1] = false;
+        st->ready[0] = st->ready[1] = st->ready[2] = false;
         *state = st;
     }
-    const bool fp4 = p.kv4 != nullptr;
-    if (!st->ready[fp4]) {
-        const cudaError_t e = p.d == 64 ? (fp4 ? configure_format<64, true>(st) : configure_format<64, false>(st))
-                                        : (fp4 ? configure_format<128, true>(st) : configure_format<128, false>(st));
+    if (!st->ready[p.fmt]) {
+        const cudaError_t e = p.d == 64 ? (p.fmt == FD_KV_FP8   ? configure_format<64, FD_KV_FP8>(st)
+                                           : p.fmt == FD_KV_FP4 ? configure_format<64, FD_KV_FP4>(st)
+                                                                : configure_format<64, FD_KV_BF16>(st))
+                                        : (p.fmt == FD_KV_FP8   ? configure_format<128, FD_KV_FP8>(st)
+                                           : p.fmt == FD_KV_FP4 ? configure_format<128, FD_KV_FP4>(st)
+                                                                : configure_format<128, FD_KV_BF16>(st));
         if (e != cudaSuccess) return e;
     }
     // q: a 3-D view [T][Hq][d], box = 64 elements x G q-heads (one kv-head) x q_box_t block rows
@@ -1666,7 +1804,7 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
         e.map = map;
         st->qcurrent = &e.map;
     }
-    if (fp4) {  // pages come by untiled bulk copies: no map of the pool (the kernel's first map goes unused)
+    if (wide(p.fmt)) {  // pages come by untiled bulk copies: no map of the pool (the kernel's first map goes unused)
         st->current = st->qcurrent;
         return cudaSuccess;
     }
@@ -1694,19 +1832,20 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
 // CTAs per cluster for a call with one cluster per segment: the largest size (any, not only powers of two: a GPC holds
 // a limited number of clusters of each size) for which all clusters of the call are resident together, so every SM it
 // can use streams at once and a CTA has the fewest tiles; 0 if there is none.
-int attn_tc_cluster_size(const void* state, bool fp4, int n_segments, int n_sms) {
+int attn_tc_cluster_size(const void* state, int fmt, int n_segments, int n_sms) {
     const TcState* st = static_cast<const TcState*>(state);
     if (!st || n_segments <= 0) return 0;
     for (int c = kMaxCluster; c >= 2; --c)
-        if (n_segments * c <= n_sms && st->max_clusters[fp4][c] >= n_segments) return c;
+        if (n_segments * c <= n_sms && st->max_clusters[fmt][c] >= n_segments) return c;
     return 0;
 }
 
 void launch_attn_tc(void* state, const AttnParams& p, int mode, cudaStream_t s) {
     if (p.batch == 0) return;
     const TcState* st = static_cast<const TcState*>(state);
-    if (p.kv4) p.d == 64 ? launch_format<64, true>(st, p, mode, s) : launch_format<128, true>(st, p, mode, s);
-    else p.d == 64 ? launch_format<64, false>(st, p, mode, s) : launch_format<128, false>(st, p, mode, s);
+    if (p.fmt == FD_KV_FP8) p.d == 64 ? launch_format<64, FD_KV_FP8>(st, p, mode, s) : launch_format<128, FD_KV_FP8>(st, p, mode, s);
+    else if (p.fmt == FD_KV_FP4) p.d == 64 ? launch_format<64, FD_KV_FP4>(st, p, mode, s) : launch_format<128, FD_KV_FP4>(st, p, mode, s);
+    else p.d == 64 ? launch_format<64, FD_KV_BF16>(st, p, mode, s) : launch_format<128, FD_KV_BF16>(st, p, mode, s);
 }
 
 void attn_tc_free(void* state) { delete static_cast<TcState*>(state); }

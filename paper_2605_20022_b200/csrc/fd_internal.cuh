@@ -93,7 +93,8 @@ struct AttnParams {
                       // 3: as 2, but the launch before this one is the KV append of this cache: tiles of the prefix are
                       //    read early, a tile that reaches into the query block after the wait
     int* status;
-    const unsigned char* kv4;  // the 4-bit cache (fd_fp4.cuh), nullptr in a call on bf16 pages
+    int fmt;                   // FD_KV_*: what the cache holds
+    const unsigned char* kvq;  // the 4-bit (fd_fp4.cuh) or 8-bit (fd_fp8.cuh) cache, nullptr in a call on bf16 pages
     float out_scale;           // what the merged output is multiplied by: 1, or v_scale of a 4-bit cache
 };
 
@@ -291,11 +292,11 @@ enum { kTcPlanned = 0, kTcSelfPlanned = 1, kTcCluster = 2 };
 // Launchers (defined next to their kernels).
 void launch_plan(const AttnParams& p, cudaStream_t s);
 cudaError_t attn_simt_prepare(int d);
-void launch_attn_simt(const AttnParams& p, cudaStream_t s);  // either cache: p.kv4 says which
+void launch_attn_simt(const AttnParams& p, cudaStream_t s);  // any cache: p.fmt says which
 bool attn_tc_supported(int d, int G, int max_q_len);
-cudaError_t attn_tc_prepare(void** state, const AttnParams& p);  // tensor maps of this call (either cache)
+cudaError_t attn_tc_prepare(void** state, const AttnParams& p);  // tensor maps of this call (any cache)
 void launch_attn_tc(void* state, const AttnParams& p, int mode, cudaStream_t s);  // mode: kTcPlanned, kTcSelfPlanned, kTcCluster
-int attn_tc_cluster_size(const void* state, bool fp4, int n_segments, int n_sms);  // CTAs per cluster for a call of n_segments, or 0
+int attn_tc_cluster_size(const void* state, int fmt, int n_segments, int n_sms);  // CTAs per cluster for a call of n_segments, or 0
 void attn_tc_free(void* state);
 void launch_wait_timeout_selftest(int* status, unsigned long long limit_ns, cudaStream_t s);
 void launch_merge(const AttnParams& p, cudaStream_t s);
@@ -406,6 +407,80 @@ struct Fp4RowsParams {
 void launch_kv_append_fp4(const Fp4RowsParams& p, cudaStream_t s);
 void launch_kv_read_fp4(const Fp4RowsParams& p, cudaStream_t s);
 
+// Rows into the cache and out of it in 8 bits.
+struct Fp8RowsParams {
+    int batch, total_rows, num_pages, Hkv, d, max_pages;
+    __nv_bfloat16* k;         // append: read only
+    __nv_bfloat16* v;
+    unsigned char* kv8;       // read: read only
+    const int32_t* page_table;
+    const int32_t* prefix_lens;
+    const int32_t* q_lens;
+    int n_sms;
+    int* status;
+};
+void launch_kv_append_fp8(const Fp8RowsParams& p, cudaStream_t s);
+void launch_kv_read_fp8(const Fp8RowsParams& p, cudaStream_t s);
+
+struct ForkParams {
+    int n_forks, batch, num_pages, max_pages;
+    const int32_t* parents;
+    const int32_t* children;
+    int32_t* page_table;
+    int32_t* prefix_lens;
+    int32_t* shared;
+    const int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* n_free_out;
+    int32_t* copy_src;
+    int32_t* copy_dst;
+    unsigned int* ticket;     // [1] CTAs finished, zero between calls
+    int n_sms;
+    int* status;
+};
+void launch_kv_fork(const ForkParams& p, cudaStream_t s);
+
+struct FreeParams {
+    int n_seqs, batch, num_pages, max_pages;
+    const int32_t* seqs;
+    int32_t* page_table;
+    int32_t* prefix_lens;
+    int32_t* shared;
+    int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* n_free_out;
+    int* status;
+};
+void launch_kv_free(const FreeParams& p, cudaStream_t s);
+
+struct CompactParams {
+    int batch, num_pages, max_pages, max_copies;
+    int32_t* page_table;
+    int32_t* shared;          // may be nullptr
+    int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* page_map;
+    int32_t* copy_src;
+    int32_t* copy_dst;
+    int32_t* n_copies;
+    int* failed;              // [1] scratch: the first kernel tells the second that nothing is to be renamed
+    int n_sms;
+    int* status;
+};
+int launch_kv_compact(const CompactParams& p, cudaStream_t s);  // returns the number of kernels launched
+
+struct CopyPagesParams {
+    int max_copies, num_pages;
+    const int32_t* n_copies;  // may be nullptr: max_copies
+    const int32_t* src;
+    const int32_t* dst;
+    unsigned char* cache;
+    long long page_bytes;     // a multiple of 32
+    int n_sms;
+    int* status;
+};
+void launch_kv_copy_pages(const CopyPagesParams& p, cudaStream_t s);
+
 struct NormRopeParams {
     int total_rows, num_pages, Hq, Hkv, d;
     const __nv_bfloat16* qkv;
@@ -418,8 +493,9 @@ struct NormRopeParams {
     const int32_t* positions;
     const int32_t* slot_map;
     __nv_bfloat16* q_out;
-    __nv_bfloat16* kv;        // one of the two caches
-    unsigned char* kv4;
+    __nv_bfloat16* kv;        // the cache, or rows, in bf16: where slot (page, token) of K of kv-head h starts is
+    long long page_step, tok_step, head_step, v_step;  //    page * page_step + token * tok_step + h * head_step, V's v_step behind
+    unsigned char* kv4;       // or the 4-bit cache
     float k_scale, v_scale;
     int n_sms;
     int* status;

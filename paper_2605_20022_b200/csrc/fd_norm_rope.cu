@@ -242,11 +242,11 @@ __global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(NormRopeParams p
         do_heads<D, FP4, LAYOUT, 0>(src, p.Hq, part, parts, wq, p.q_weight != nullptr, p.eps, turn, p.q_out + (long long)t * p.Hq * D, D, by_k, nullptr, tok,
                                     sub, hl);
         if (!store_kv) continue;
-        __nv_bfloat16* k_dst = FP4 ? nullptr : p.kv + ((long long)page * 2 * p.Hkv * 16 + tok) * D;
+        __nv_bfloat16* k_dst = FP4 ? nullptr : p.kv + page * p.page_step + tok * p.tok_step;
         unsigned char* k_dst4 = FP4 ? p.kv4 + fp4_page_offset(page, p.Hkv, 0, 0, D) : nullptr;
-        do_heads<D, FP4, LAYOUT, 1>(src + (long long)p.Hq * D, p.Hkv, ik, parts, wk, p.k_weight != nullptr, p.eps, turn, k_dst, 16 * D, by_k, k_dst4, tok, sub, hl);
-        do_heads<D, FP4, LAYOUT, 2>(src + (long long)(p.Hq + p.Hkv) * D, p.Hkv, iv, parts, wk, false, p.eps, turn, FP4 ? nullptr : k_dst + (long long)p.Hkv * 16 * D,
-                                    16 * D, by_v, FP4 ? k_dst4 + fp4_page_bytes(D) : nullptr, tok, sub, hl);
+        do_heads<D, FP4, LAYOUT, 1>(src + (long long)p.Hq * D, p.Hkv, ik, parts, wk, p.k_weight != nullptr, p.eps, turn, k_dst, p.head_step, by_k, k_dst4, tok, sub, hl);
+        do_heads<D, FP4, LAYOUT, 2>(src + (long long)(p.Hq + p.Hkv) * D, p.Hkv, iv, parts, wk, false, p.eps, turn, FP4 ? nullptr : k_dst + p.v_step,
+                                    p.head_step, by_v, FP4 ? k_dst4 + fp4_page_bytes(D) : nullptr, tok, sub, hl);
     }
 }
 

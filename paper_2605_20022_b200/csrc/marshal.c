@@ -74,7 +74,23 @@ typedef int (*rope_fn)(void*, int, void*, int64_t, void*, void*, float, void*, i
 typedef int (*append_fn)(void*, int, int, void*, void*, void*, int, void*, void*, void*, float, float, void*);
 typedef int (*read_fn)(void*, int, int, void*, int, void*, void*, void*, float, float, void*, void*, void*);
 typedef int (*attn_fn)(void*, int, int, void*, void*, int, void*, void*, void*, void*, void*, float, float, void*, void*);
+typedef int (*append8_fn)(void*, int, int, void*, void*, void*, int, void*, void*, void*, void*);
+typedef int (*read8_fn)(void*, int, int, void*, int, void*, void*, void*, void*, void*, void*);
+typedef int (*attn8_fn)(void*, int, int, void*, void*, int, void*, void*, void*, void*, void*, void*, void*);
+typedef int (*prompt_fn)(void*, int, int, int, void*, int64_t, void*, void*, int64_t, void*, void*, void*, void*);
+typedef int (*fork_fn)(void*, int, void*, void*, int, void*, void*, void*, void*, void*, void*, int, void*, void*, void*);
+typedef int (*free_fn)(void*, int, void*, int, void*, void*, void*, void*, void*, void*, int, void*);
+typedef int (*compact_fn)(void*, int, void*, void*, void*, void*, int, void*, int, void*, void*, void*, void*);
+typedef int (*copy_fn)(void*, int, void*, void*, void*, void*, int, int, void*);
 
+static append8_fn f_append8;
+static read8_fn f_read8;
+static attn8_fn f_attn8;
+static prompt_fn f_prompt;
+static fork_fn f_fork;
+static free_fn f_free;
+static compact_fn f_compact;
+static copy_fn f_copy;
 static reserve_fn f_reserve;
 static rope_fn f_rope;
 static append_fn f_append;
@@ -109,6 +125,22 @@ WRAPPER(fd_kv_read_fp4, f_read, "piipipppffppp",
         f_read(a[0].p, a[1].i, a[2].i, a[3].p, a[4].i, a[5].p, a[6].p, a[7].p, a[8].f, a[9].f, a[10].p, a[11].p, a[12].p))
 WRAPPER(fd_attn_draft_verify_fp4, f_attn, "piippipppppffpp",
         f_attn(a[0].p, a[1].i, a[2].i, a[3].p, a[4].p, a[5].i, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].f, a[12].f, a[13].p, a[14].p))
+WRAPPER(fd_kv_append_fp8, f_append8, "piipppipppp",
+        f_append8(a[0].p, a[1].i, a[2].i, a[3].p, a[4].p, a[5].p, a[6].i, a[7].p, a[8].p, a[9].p, a[10].p))
+WRAPPER(fd_kv_read_fp8, f_read8, "piipipppppp",
+        f_read8(a[0].p, a[1].i, a[2].i, a[3].p, a[4].i, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p))
+WRAPPER(fd_attn_draft_verify_fp8, f_attn8, "piippippppppp",
+        f_attn8(a[0].p, a[1].i, a[2].i, a[3].p, a[4].p, a[5].i, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p))
+WRAPPER(fd_attn_prompt, f_prompt, "piiiplpplpppp",
+        f_prompt(a[0].p, a[1].i, a[2].i, a[3].i, a[4].p, a[5].l, a[6].p, a[7].p, a[8].l, a[9].p, a[10].p, a[11].p, a[12].p))
+WRAPPER(fd_kv_fork, f_fork, "pippippppppippp",
+        f_fork(a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].i, a[12].p, a[13].p, a[14].p))
+WRAPPER(fd_kv_free, f_free, "pipippppppip",
+        f_free(a[0].p, a[1].i, a[2].p, a[3].i, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].i, a[11].p))
+WRAPPER(fd_kv_compact, f_compact, "pippppipipppp",
+        f_compact(a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].p, a[6].i, a[7].p, a[8].i, a[9].p, a[10].p, a[11].p, a[12].p))
+WRAPPER(fd_kv_copy_pages, f_copy, "pippppiip",
+        f_copy(a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].p, a[6].i, a[7].i, a[8].p))
 
 static PyObject* bind(PyObject* self, PyObject* path) {
     const char* s = PyUnicode_AsUTF8(path);
@@ -125,7 +157,16 @@ static PyObject* bind(PyObject* self, PyObject* path) {
     f_append = (append_fn)dlsym(lib, "fd_kv_append_fp4");
     f_read = (read_fn)dlsym(lib, "fd_kv_read_fp4");
     f_attn = (attn_fn)dlsym(lib, "fd_attn_draft_verify_fp4");
-    if (!f_reserve || !f_rope || !f_append || !f_read || !f_attn) {
+    f_append8 = (append8_fn)dlsym(lib, "fd_kv_append_fp8");
+    f_read8 = (read8_fn)dlsym(lib, "fd_kv_read_fp8");
+    f_attn8 = (attn8_fn)dlsym(lib, "fd_attn_draft_verify_fp8");
+    f_prompt = (prompt_fn)dlsym(lib, "fd_attn_prompt");
+    f_fork = (fork_fn)dlsym(lib, "fd_kv_fork");
+    f_free = (free_fn)dlsym(lib, "fd_kv_free");
+    f_compact = (compact_fn)dlsym(lib, "fd_kv_compact");
+    f_copy = (copy_fn)dlsym(lib, "fd_kv_copy_pages");
+    if (!f_reserve || !f_rope || !f_append || !f_read || !f_attn || !f_append8 || !f_read8 || !f_attn8 || !f_prompt || !f_fork || !f_free ||
+        !f_compact || !f_copy) {
         PyErr_SetString(PyExc_OSError, "the library lacks an entry point");
         return NULL;
     }
@@ -134,7 +175,9 @@ static PyObject* bind(PyObject* self, PyObject* path) {
 
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(fd_kv_reserve), METHOD(fd_qk_norm_rope_append), METHOD(fd_kv_append_fp4), METHOD(fd_kv_read_fp4),
-                                METHOD(fd_attn_draft_verify_fp4), {"bind", bind, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+                                METHOD(fd_attn_draft_verify_fp4), METHOD(fd_kv_append_fp8), METHOD(fd_kv_read_fp8),
+                                METHOD(fd_attn_draft_verify_fp8), METHOD(fd_attn_prompt), METHOD(fd_kv_fork), METHOD(fd_kv_free),
+                                METHOD(fd_kv_compact), METHOD(fd_kv_copy_pages), {"bind", bind, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void) {
