@@ -38,6 +38,7 @@ struct fd_ctx {
     unsigned int* rs_ticket;     // page reservation
     unsigned int* fk_ticket;     // fork
     int* cp_failed;              // compaction
+    fd::FreeScratch* fr_scratch; // free
     fd::PromptPlan prompt;       // work list of the prompt attention
     int* status;
     int max_rows;      // capacity of keys
@@ -222,6 +223,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     const size_t o_rst = take(sizeof(unsigned int));
     const size_t o_fkt = take(sizeof(unsigned int));
     const size_t o_cpf = take(sizeof(int));
+    const size_t o_frs = take(sizeof(fd::FreeScratch));
     const size_t o_pp = take((5 * (size_t)B + 4) * sizeof(int));
     const size_t o_stat = take(sizeof(int));
     if (cudaMalloc(&c->pool, off) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_WORKSPACE; }
@@ -254,6 +256,7 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->rs_ticket = reinterpret_cast<unsigned int*>(c->pool + o_rst);
     c->fk_ticket = reinterpret_cast<unsigned int*>(c->pool + o_fkt);
     c->cp_failed = reinterpret_cast<int*>(c->pool + o_cpf);
+    c->fr_scratch = reinterpret_cast<fd::FreeScratch*>(c->pool + o_frs);
     int* pp = reinterpret_cast<int*>(c->pool + o_pp);
     c->prompt = {pp, pp + B + 1, pp + 2 * B + 2, pp + 3 * B + 2, pp + 4 * B + 2, pp + 5 * B + 3};
     c->status = reinterpret_cast<int*>(c->pool + o_stat);
@@ -904,8 +907,8 @@ fd_status fd_kv_free(fd_ctx* c, int n_seqs, const int32_t* seqs, int batch, int3
     p.n_seqs = n_seqs; p.batch = batch; p.num_pages = num_pages; p.max_pages = c->cfg.max_pages_per_seq;
     p.seqs = seqs; p.page_table = page_table; p.prefix_lens = prefix_lens; p.shared = shared;
     p.free_pages = free_pages; p.n_free = n_free; p.n_free_out = n_free_out; p.status = c->status;
-    fd::launch_kv_free(p, static_cast<cudaStream_t>(stream));
-    c->launches += 1;
+    p.scratch = c->fr_scratch; p.n_sms = c->n_sms;
+    c->launches += fd::launch_kv_free(p, static_cast<cudaStream_t>(stream));
     return cudaGetLastError() == cudaSuccess ? FD_OK : FD_ERR_CUDA;
 }
 

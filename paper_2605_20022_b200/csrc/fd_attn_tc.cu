@@ -66,7 +66,6 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
-#include <type_traits>
 #include <vector>
 
 #include "fd_attn_common.cuh"
@@ -112,31 +111,35 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 
 template <int D, int MODE, int FMT>
 struct Cfg {
-    static constexpr int kWidenWarps = wide(FMT) ? 8 : 0;  // the warps behind warp 11 widen the tiles
+    // the warps behind warp 11 widen the tiles: K and V (FP4), or V alone (FP8)
+    static constexpr int kWidenWarps = FMT == FD_KV_FP4 ? 8 : FMT == FD_KV_FP8 ? 4 : 0;
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
-    // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps: the launch allocates 168 (bf16) or
-    // 96 (wide formats) to each, and what the groups take adds up to no more than that.
-    static constexpr int kRegSoftmax = wide(FMT) ? 144 : 224;
-    static constexpr int kRegHelper = wide(FMT) ? 48 : 56;
-    static constexpr int kRegWiden = 64;
-    static_assert(!wide(FMT) || 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden <= kThreads * 96, "register split");
+    // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps.  What the groups take adds up to no more
+    // than what the launch allocates: configure_kernel compares the two before the kernel's first launch.
+    static constexpr int kRegSoftmax = FMT == FD_KV_FP4 ? 144 : FMT == FD_KV_FP8 ? 176 : 224;
+    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? 72 : 56;
+    static constexpr int kRegWiden = FMT == FD_KV_FP8 ? 88 : 64;
+    static constexpr int kRegTotal = 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden;
+    static_assert(kRegTotal <= 65536, "register split");
     // buffers in the K ring, and again in the V ring (wide formats: of widened tiles, fed from the raw ring)
     static constexpr int kStages = wide(FMT) ? (D == 128 ? 2 : 4) : (D == 128 ? 3 : 6);
     static constexpr int kQBytes = kMaxRows * D * 2;
     static constexpr int kKBytes = kTileTokens * D * 2;  // one K (or V) tile
     static constexpr int kRawStages = wide(FMT) ? (D == 128 ? 3 : 6) : 0;
-    // one page of the kv-head in a stage: K and V, which lie side by side in the cache (FP4), or one of the two (FP8)
-    static constexpr int kRawPage = FMT == FD_KV_FP8 ? fp8_block_bytes(D) : 2 * fp4_page_bytes(D);
+    // one page of the kv-head in a stage: codes and scales of K and V, which lie side by side in the cache (FP4), or the codes (FP8)
+    static constexpr int kRawPage = FMT == FD_KV_FP8 ? 2 * 16 * D : 2 * fp4_page_bytes(D);
     static constexpr int kRawBytes = 8 * kRawPage;           // ... of a tile
-    static constexpr int kRawOffset = kQBytes + 2 * kStages * kKBytes;
-    static constexpr int kBarOffset = kRawOffset + kRawStages * kRawBytes;
+    // Behind Q: the K ring -- for FP8 the raw ring, whose K the MMAs read as it is -- then the V ring, then (FP4) the raw ring.
+    static constexpr int kVOffset = kQBytes + (FMT == FD_KV_FP8 ? kRawStages * kRawBytes : kStages * kKBytes);
+    static constexpr int kRawOffset = FMT == FD_KV_FP8 ? kQBytes : kVOffset + kStages * kKBytes;
+    static constexpr int kBarOffset = kVOffset + kStages * kKBytes + (FMT == FD_KV_FP4 ? kRawStages * kRawBytes : 0);
     static constexpr int kCsOffset = kBarOffset + 320;           // window of the CTA range starts
     static constexpr int kDescOffset = kBarOffset + 448;         // ring of piece descriptors
     static constexpr int kScanOffset = kBarOffset + 720;         // SelfScans: the scans of a call that plans for itself
     static constexpr int kExOffset = kBarOffset + 1024;          // [2][128] floats: stream exchange in the epilogue
     static constexpr int kRbOffset = kBarOffset + 2048;          // row blocks of a call that plans for itself
-    static constexpr int kWideOffset = kRbOffset + 1024;          // wide formats: WideShared
-    static constexpr int kSmemBytes = kRbOffset + 1024 + (wide(FMT) ? 4096 : 0);  // the dynamic shared memory is declared 1024-byte aligned
+    static constexpr int kWideOffset = kRbOffset + 1024;         // wide formats: WideShared
+    static constexpr int kSmemBytes = kRbOffset + 1024 + (wide(FMT) ? 5120 : 0);  // the dynamic shared memory is declared 1024-byte aligned
     static constexpr int kDescSlots = wide(FMT) ? 8 : 4;  // ring of piece descriptors: see publish_piece
     static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
@@ -176,8 +179,13 @@ struct WideShared {
     float row_scale[4][kMaxRows];
     float ref[2][kMaxRows];              // [piece & 1] the reference of each row, -inf while it has none
     Piece ring[8];                       // piece descriptors
+    uint64_t q_read;                     // FP8, d = 64: the Q tile of a piece is in registers
+    // FP8: the scales of a tile's pages, K's then V's.  Slot = tile & 15: it is written for tile t when the raw stage of t is free, hence
+    // V of the tile kRawStages before it widened, P V of the tile kStages before that one completed, and that tile's softmax done: of
+    // tile t - 5 (d = 128) or t - 10.
+    alignas(16) float sc[16][16];
 };
-static_assert(sizeof(WideShared) <= 4096, "WideShared must fit behind the row blocks");
+static_assert(sizeof(WideShared) <= 5120, "WideShared must fit behind the row blocks");
 
 
 // K (which = 0) or V (which = 1) load warp.
@@ -325,14 +333,12 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
     }
 }
 
-// FP8 load warp.  K and V of a tile are stages of their own, in the order in which the widening warps take them: K 0, K 1, V 0,
-// K 2, V 1, ..., the last V.  Stage i of a piece of nt tiles:
-__device__ __forceinline__ bool fp8_stage_is_k(int i, int nt) { return i == 0 || ((i & 1) && i != 2 * nt - 1); }
-__device__ __forceinline__ int fp8_k_stage(int j) { return j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int fp8_v_stage(int j, int nt) { return j == nt - 1 ? 2 * nt - 1 : 2 * j + 2; }
-
+// FP8 load warp.  One TMA box a page brings the codes of K and V, as [8-token group][K, V][8 rows][d]: the groups of K then lie a
+// fixed stride apart, as those of V do, and K is an operand of Q K^T as it stands.  (Two untiled copies a page, K and V apart, took 464 us
+// where this takes 335: what a copy costs the TMA unit is mostly per copy.)  The scales, 16 bytes behind the codes of either,
+// come by plain loads: those of a tile are on their way while the next tile is issued, and stored behind that.
 template <int D, int MODE>
-__device__ __forceinline__ void load_role_fp8(const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
+__device__ __forceinline__ void load_role_fp8(const CUtensorMap& tmap, const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
                                               int* bad, volatile int* abort) {
     using C = Cfg<D, MODE, FD_KV_FP8>;
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
@@ -342,6 +348,15 @@ __device__ __forceinline__ void load_role_fp8(const AttnParams& p, int n_rb, uns
     Walk w = {s_c, 0, {0, 0}, 0, rg.first};
     bool ok = true, waited = !p.early;
     bool bad_early = false;
+    float sc = 1.f;      // lanes 0-15: the scale of page (lane & 7) of K or V of the tile issued last,
+    int pending = -1;    // ... which is this one, or -1: none is waiting to be stored
+    auto publish_scales = [&]() {
+        if (pending < 0) return;
+        if (lane < 16) f4->sc[pending & 15][lane] = sc;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&f4->raw_full[pending % C::kRawStages]);
+        pending = -1;
+    };
     while (w.t < e_c && ok) {
         const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
         const int32_t* table = p.page_table + (long long)pc.b * p.max_pages;
@@ -359,35 +374,31 @@ __device__ __forceinline__ void load_role_fp8(const AttnParams& p, int n_rb, uns
             return id;
         };
         int ids_cur = load_ids(0), ids_next = load_ids(1);
-        int j = -1, phys_k = -1, phys_before = -1;  // the last K's tile, this lane's page of it, and of the tile before
-        for (int i = 0; i < 2 * pc.nt; ++i) {
-            const int g = 2 * w.g0 + i, st = g % C::kRawStages, use = g / C::kRawStages;
-            const bool is_k = fp8_stage_is_k(i, pc.nt);
-            if (is_k) {
-                ++j;
-                if (j > 0 && (j & 3) == 0) { ids_cur = ids_next; ids_next = load_ids((j >> 2) + 1); }
-                phys_before = phys_k;
-                phys_k = __shfl_sync(0xffffffffu, ids_cur, (j & 3) * 8 + (lane & 7));
-            }
-            const bool last_v = i == 2 * pc.nt - 1;
-            const int tile = pc.tile0 + (is_k || last_v ? j : j - 1), phys = is_k || last_v ? phys_k : phys_before;
-            if (!waited && (p.early == 1 || (p.early == 3 && (tile + 1) * kTileTokens > pc.n))) {
+        for (int j = 0; j < pc.nt; ++j) {
+            const int g = w.g0 + j, st = g % C::kRawStages, use = g / C::kRawStages;
+            if (j > 0 && (j & 3) == 0) { ids_cur = ids_next; ids_next = load_ids((j >> 2) + 1); }
+            const int phys = __shfl_sync(0xffffffffu, ids_cur, (j & 3) * 8 + (lane & 7));
+            if (!waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n))) {
                 wait_prior_launch();
                 waited = true;
                 if (bad_early) atomicOr(p.status, FD_DEV_BAD_PAGE);
             }
             if (!wait_all(&f4->raw_empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
-            const int npg = min(8, (pc.kv_len - tile * kTileTokens + 15) >> 4);
+            const int npg = min(8, (pc.kv_len - (pc.tile0 + j) * kTileTokens + 15) >> 4);
             if (lane == 0) mbar_arrive_expect_tx(&f4->raw_full[st], npg * C::kRawPage);
             __syncwarp();
-            if (lane < 8 && phys >= 0)
-                bulk_load_hint(raw + st * C::kRawBytes + lane * C::kRawPage, p.kvq + fp8_block_offset(phys, p.Hkv, pc.kvh, is_k ? 0 : 1, D), C::kRawPage,
-                               &f4->raw_full[st], policy);
+            if (lane < 8 && phys >= 0) tma_load_5d_hint(raw + st * C::kRawBytes + lane * C::kRawPage, &tmap, 0, 0, 0, 0, phys * p.Hkv + pc.kvh, &f4->raw_full[st], policy);
             issued = g + 1;
+            publish_scales();
+            sc = 1.f;  // (a page that no token owns: its scores are masked, but -inf times a stale scale need not be)
+            if (lane < 16 && phys >= 0) sc = __ldcg(reinterpret_cast<const float*>(p.kvq + fp8_block_offset(phys, p.Hkv, pc.kvh, lane >> 3, D) + 16 * D));
+            pending = g;
         }
+        publish_scales();
         w.advance(pc);
     }
     if (*abort) {  // drain copies still in flight before the shared memory is given back
+        publish_scales();
         for (int g = max(0, issued - C::kRawStages); g < issued; ++g) {
             const unsigned long long t0 = global_ns();
             for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
@@ -453,37 +464,38 @@ __device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char*
     }
 }
 
-// The same for 8-bit pages: 16 codes a thread and pass, whose block's scale stands behind the page's codes.  Eight (d = 64: four)
-// neighbouring lanes share a token, so the reads are contiguous; of the two 16-byte words each lane stores, the lanes of the upper
-// half of d store the second first, which puts the eight lanes of a store on different banks.
+// The V tile of 8-bit pages: 16 codes a thread and pass, 128 threads.  Eight (d = 64: four) neighbouring lanes share a token's row, so
+// the reads cover whole rows; of the two 16-byte words each lane stores, the lanes of the upper half of d store the second first,
+// which puts the eight lanes of a store on different banks.
+constexpr int kWidenThreads8 = 128;
+
 template <int D>
-struct RawWords8 {
+struct RawV8 {
     static constexpr int kChunks = D / 16;
-    static constexpr int kPasses = kTileTokens * kChunks / kWidenThreads;
+    static constexpr int kTokens = kWidenThreads8 / kChunks;  // of a pass
+    static constexpr int kPasses = kTileTokens / kTokens;
     uint4 codes[kPasses];
-    float sc[kPasses];
     __device__ __forceinline__ void load(const unsigned char* raw) {
         const int t = (int)threadIdx.x - 384, c = t % kChunks;
 #pragma unroll
         for (int it = 0; it < kPasses; ++it) {
-            const int tok = t / kChunks + it * (kWidenThreads / kChunks);
-            const unsigned char* page = raw + (tok >> 4) * fp8_block_bytes(D);
-            codes[it] = *reinterpret_cast<const uint4*>(page + (tok & 15) * D + c * 16);
-            sc[it] = *reinterpret_cast<const float*>(page + 16 * D);
+            const int tok = t / kChunks + it * kTokens, r = tok & 7;
+            const unsigned char* row = raw + (tok >> 3) * (2 * 8 * D) + 8 * D + r * D;
+            codes[it] = *reinterpret_cast<const uint4*>(row + ((c ^ (D == 128 ? r : r >> 1)) << 4));  // (the swizzle of the box)
         }
     }
 };
 
 template <int D, bool ZERO_TAIL>
-__device__ __forceinline__ void widen_tile(const RawWords8<D>& in, unsigned char* tile, int valid) {
-    constexpr int kChunks = RawWords8<D>::kChunks;
+__device__ __forceinline__ void widen_v8(const RawV8<D>& in, const float* v_scales, unsigned char* tile, int valid) {
+    constexpr int kChunks = RawV8<D>::kChunks;
     constexpr int kHalves = D / 64;
     const int t = (int)threadIdx.x - 384, c = t % kChunks;
     const bool swap = kHalves == 2 && (c & 4);
 #pragma unroll
-    for (int it = 0; it < RawWords8<D>::kPasses; ++it) {
-        const int tok = t / kChunks + it * (kWidenThreads / kChunks);
-        const __half2 s2 = __float2half2_rn(in.sc[it]);  // (a power of two from 2^-15 on: exact)
+    for (int it = 0; it < RawV8<D>::kPasses; ++it) {
+        const int tok = t / kChunks + it * RawV8<D>::kTokens;
+        const __half2 s2 = __float2half2_rn(v_scales[tok >> 4]);  // (a power of two from 2^-15 on: exact)
         const bool dead = ZERO_TAIL && tok >= valid;
         const uint4 cd = in.codes[it];
         const uint32_t wd[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
@@ -499,6 +511,58 @@ __device__ __forceinline__ void widen_tile(const RawWords8<D>& in, unsigned char
             *reinterpret_cast<uint4*>(row + ((unit ^ (tok & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
     }
+}
+
+// The Q tile of a piece for K in e4m3: q = hi + lo, both e4m3, in place -- rows of d bytes, hi's 128 rows then lo's, a thread a row.  A
+// row is multiplied by the power of two that brings its largest element into [2^7, 2^8).  hi keeps four of bf16's eight bits, what
+// is left has at most four and e4m3 holds it exactly where the element is at least 2^-9 of the largest; below that q is off by at most
+// half a step of e4m3's smallest, 2^-17 of the largest element.  Q K^T is then two products at twice the rate of one in fp16, and K
+// needs no widening.  Rows no query owns become zeros, as in q_to_half.
+template <int D>
+__device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, float scale_log2e, int rows, uint64_t* q_read, uint32_t parity,
+                                          volatile int* abort) {
+    const int r = (int)threadIdx.x - 384;
+    const bool live = r < rows;
+    auto unit = [&](int u) -> uint4 {  // eight elements
+        return live ? *reinterpret_cast<const uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4)) : make_uint4(0, 0, 0, 0);
+    };
+    // The last eight units stay in registers.  d = 128: lo's bytes land where they were; hi's first land where units 0-3 were, read by then.
+    uint4 v[8];
+    uint32_t mx = 0;
+#pragma unroll
+    for (int u = D / 8 - 1; u >= 0; --u) {
+        const uint4 x = unit(u);
+        if (u >= D / 8 - 8) v[u & 7] = x;
+        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+    }
+    if (D == 64) {  // (a row of 64 bytes lands on what were other rows; of 128, on the thread's own)
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(q_read);
+        if (!wait_all(q_read, parity, abort)) return false;
+    }
+    const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);  // biased exponent of the largest magnitude
+    const float f = __uint_as_float((uint32_t)(127 + 134 - e) << 23);  // 2^(134 - e), e in [14, 255]
+#pragma unroll
+    for (int u2 = 0; u2 < D / 16; ++u2) {  // 16 elements: 16 bytes of hi, 16 of lo
+        const uint4 a4 = 2 * u2 >= D / 8 - 8 ? v[(2 * u2) & 7] : unit(2 * u2), b4 = 2 * u2 >= D / 8 - 8 ? v[(2 * u2 + 1) & 7] : unit(2 * u2 + 1);
+        const uint32_t wd[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float x0 = __uint_as_float(wd[2 * k] << 16) * f, x1 = __uint_as_float(wd[2 * k] & 0xffff0000u) * f;
+            const float x2 = __uint_as_float(wd[2 * k + 1] << 16) * f, x3 = __uint_as_float(wd[2 * k + 1] & 0xffff0000u) * f;
+            hi[k] = to_e4m3x2(x0, x1) | to_e4m3x2(x2, x3) << 16;
+            uint32_t a, b;
+            e4m3x4_to_half(hi[k], a, b);
+            const float2 ha = __half22float2(as_half2(a)), hb = __half22float2(as_half2(b));
+            lo[k] = to_e4m3x2(x0 - ha.x, x1 - ha.y) | to_e4m3x2(x2 - hb.x, x3 - hb.y) << 16;
+        }
+        unsigned char* at = sq + r * D + ((u2 ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
+        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(at + kMaxRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
+    return true;
 }
 
 // The Q tile of a piece, bf16 -> fp16 in place, kPer neighbouring threads a row (of two, the second starts at unit 4 of its
@@ -545,41 +609,34 @@ __device__ __forceinline__ void q_to_half(unsigned char* sq, float* row_scale, f
     if (part == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 141)), 1.17549435e-38f), 3.4028234e38f);
 }
 
-// Wide formats: the widening warps.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
+// FP4: the widening warps.  K runs one tile ahead of V (the MMA warp needs K j + 1 before V j), and the next piece's first K tile
 // is widened before its Q is touched, while that Q is still on its way.
-template <int D, int MODE, int FMT>
-__device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv,
+template <int D, int MODE>
+__device__ __forceinline__ void widen_role_fp4(const AttnParams& p, unsigned char* sq, unsigned char* sk, unsigned char* sv,
                                            const unsigned char* raw, Bars* bars, WideShared* f4, const Piece* ring, const Range rg,
                                            volatile int* abort) {
-    using C = Cfg<D, MODE, FMT>;
+    using C = Cfg<D, MODE, FD_KV_FP4>;
     const int lane = threadIdx.x & 31;
     Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
     while (w.t < rg.e_c) {
         if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
         const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
-        using Words = std::conditional_t<FMT == FD_KV_FP8, RawWords8<D>, RawWords<D>>;
         auto do_k = [&](int j) -> bool {
-            const int g = w.g0 + j, st = g % C::kStages;
-            const int rg_ = FMT == FD_KV_FP8 ? 2 * w.g0 + fp8_k_stage(j) : g, rs = rg_ % C::kRawStages;
-            if (!wait_all(&f4->raw_full[rs], (rg_ / C::kRawStages) & 1, abort)) return false;
-            Words in;
+            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            if (!wait_all(&f4->raw_full[rs], (g / C::kRawStages) & 1, abort)) return false;
+            RawWords<D> in;
             in.load(raw + rs * C::kRawBytes);
             if (!wait_all(&bars->k_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             widen_tile<D, false>(in, sk + st * C::kKBytes, 0);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&bars->k_full[st]);
-                if (FMT == FD_KV_FP8) mbar_arrive(&f4->raw_empty[rs]);  // (as below)
-            }
+            if (lane == 0) mbar_arrive(&bars->k_full[st]);
             return true;
         };
         auto do_v = [&](int j) -> bool {
-            const int g = w.g0 + j, st = g % C::kStages;
-            const int rg_ = FMT == FD_KV_FP8 ? 2 * w.g0 + fp8_v_stage(j, pc.nt) : g, rs = rg_ % C::kRawStages;
-            if (FMT == FD_KV_FP8 && !wait_all(&f4->raw_full[rs], (rg_ / C::kRawStages) & 1, abort)) return false;
-            Words in;  // (FP4: the tile has landed, do_k has waited for it)
-            in.load(raw + rs * C::kRawBytes + (FMT == FD_KV_FP8 ? 0 : fp4_page_bytes(D)));
+            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            RawWords<D> in;  // (the tile has landed: do_k has waited for it)
+            in.load(raw + rs * C::kRawBytes + fp4_page_bytes(D));
             if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return false;
             const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
             if (valid >= kTileTokens) widen_tile<D, false>(in, sv + st * C::kKBytes, 0);
@@ -601,6 +658,42 @@ __device__ __forceinline__ void widen_role(const AttnParams& p, unsigned char* s
         for (int j = 0; j < pc.nt; ++j) {
             if (j + 1 < pc.nt && !do_k(j + 1)) return;
             if (!do_v(j)) return;
+        }
+        w.advance(pc);
+    }
+}
+
+// FP8: the widening warps turn Q into two e4m3 tiles and widen V; K is read as it is.
+template <int D, int MODE>
+__device__ __forceinline__ void widen_role_fp8(const AttnParams& p, unsigned char* sq, unsigned char* sv, const unsigned char* raw, Bars* bars,
+                                               WideShared* f4, const Piece* ring, const Range rg, volatile int* abort) {
+    using C = Cfg<D, MODE, FD_KV_FP8>;
+    const int lane = threadIdx.x & 31;
+    Walk w = {rg.s_c, 0, {0, 0}, 0, rg.first};
+    while (w.t < rg.e_c) {
+        if (!__all_sync(0xffffffffu, wait_piece(bars, w.piece, abort))) return;
+        const Piece pc = ring[w.piece & (C::kDescSlots - 1)];
+        if (!wait_all(&bars->q_full, w.piece & 1, abort)) return;
+        if (!q_to_e4m3<D>(sq, f4->row_scale[w.piece & 3], p.scale_log2e, pc.rows, &f4->q_read, w.piece & 1, abort)) return;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&f4->q_ready);
+        for (int j = 0; j < pc.nt; ++j) {
+            const int g = w.g0 + j, rs = g % C::kRawStages, st = g % C::kStages;
+            if (!wait_all(&f4->raw_full[rs], (g / C::kRawStages) & 1, abort)) return;
+            RawV8<D> in;
+            in.load(raw + rs * C::kRawBytes);
+            if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return;
+            const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
+            const float* vs = &f4->sc[g & 15][8];
+            if (valid >= kTileTokens) widen_v8<D, false>(in, vs, sv + st * C::kKBytes, 0);
+            else widen_v8<D, true>(in, vs, sv + st * C::kKBytes, valid);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&bars->v_full[st]);
+                mbar_arrive(&f4->raw_empty[rs]);  // (where every word read has been used: see RawWords)
+            }
         }
         w.advance(pc);
     }
@@ -631,7 +724,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
     const uint32_t col_s[2] = {0u, 128u}, col_o[2] = {256u, 384u};
     const bool group_pv = wide(FMT) || pv_by_group<MODE>(rg.e_c - rg.s_c);  // wide formats: pv_role_wide
     if (p.early == 1) wait_prior_launch();  // (this role touches shared and tensor memory only; p.early >= 2 lets it run ahead)
-    const uint64_t qd0 = make_smem_desc(smem_u32(sq), 16, 1024);
+    const uint64_t qd0 = FMT == FD_KV_FP8 ? make_smem_desc(smem_u32(sq), 16, 8 * D, D == 128 ? 2 : 4) : make_smem_desc(smem_u32(sq), 16, 1024);
     const int s_c = rg.s_c, e_c = rg.e_c;
     Walk w = {s_c, 0, {0, 0}, 0, rg.first};
     bool ok = true;
@@ -664,7 +757,8 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
         for (int j = 0; j < pc.nt && ok; ++j) {
             const int g = w.g0 + j, st = g % C::kStages, use = g / C::kStages;
             const int s = j & 1;
-            if (!wait_all(&bars->k_full[st], use & 1, abort)) { ok = false; break; }
+            const int rs = g % (wide(FMT) ? C::kRawStages : 1);  // FP8: the raw stage that holds K
+            if (FMT == FD_KV_FP8 ? !wait_all(&f4->raw_full[rs], (g / (wide(FMT) ? C::kRawStages : 1)) & 1, abort) : !wait_all(&bars->k_full[st], use & 1, abort)) { ok = false; break; }
             // S_s is written over P_s (its first 64 columns), which the P V of tile j - 2 of this stream reads, and
             // nothing orders two MMAs with different accumulators but the completion of the first: Q K^T waits for
             // that P V's completion barrier.  (FD_QK_MODE 0 drops the wait, relying on one thread's MMAs executing in
@@ -673,7 +767,8 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
             // MMA is ready first from a polling loop, 8 % slower -- the polling warp takes issue slots from the
             // softmax warps of its scheduler.)
             [[maybe_unused]] const int u_prev = w.u_base[s] + (j >> 1) - 1;  // the stream's previous tile, over all pieces
-            const uint64_t kd0 = make_smem_desc(smem_u32(sk + st * C::kKBytes), 16, C::kGroupBytes);
+            const uint64_t kd0 = FMT == FD_KV_FP8 ? make_smem_desc(smem_u32(sk + rs * C::kRawBytes), 16, 16 * D, D == 128 ? 2 : 4)
+                                                  : make_smem_desc(smem_u32(sk + st * C::kKBytes), 16, C::kGroupBytes);
 #if FD_QK_MODE != 0
             if (!wide(FMT) && u_prev >= 0 && !wait_all(&bars->pv_done[s], u_prev & 1, abort)) { ok = false; break; }
 #endif
@@ -681,13 +776,21 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
             const uint32_t s_col = wide(FMT) ? (uint32_t)(g % 3) * 128u : col_s[s];
             tc_fence_after();
             if (elect_one()) {
+                if constexpr (FMT == FD_KV_FP8) {
+                    constexpr uint32_t idesc = make_idesc_e4m3(128, kTileTokens);
+#pragma unroll
+                    for (int kk = 0; kk < 2 * (D / 32); ++kk) {  // hi's products, then lo's
+                        const int step = kk % (D / 32) * 32;
+                        umma_ss_f8(tmem + s_col, qd0 + (uint64_t)((kk / (D / 32) * (kMaxRows * D) + step) >> 4), kd0 + (uint64_t)(step >> 4), idesc, kk > 0);
+                    }
+                } else
 #pragma unroll
                 for (int kk = 0; kk < C::kKSteps; ++kk) {
                     constexpr int kQHalf = kMaxRows * 128;
                     umma_ss(tmem + s_col, qd0 + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
                             kd0 + (uint64_t)(((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
                 }
-                umma_commit(&bars->k_empty[st]);
+                umma_commit(FMT == FD_KV_FP8 ? &f4->raw_empty[rs] : &bars->k_empty[st]);
                 umma_commit(wide(FMT) ? &f4->s_full[g % 3] : &bars->s_full[s]);
                 if (j == pc.nt - 1) umma_commit(&bars->q_free);  // the next piece's Q may come in
             }
@@ -940,21 +1043,43 @@ __device__ __forceinline__ uint32_t pack16(float2 v) {
 // reference yet) and the tiles the mask cuts, S is gone over twice: for the maximum, then for the weights, written as
 // they are formed (a chunk's weights only ever land on scores that have been read).
 // m, l: the reference and the sum of this thread's weights so far.
-template <int D>
-__device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_addr, float c, float head, bool masked, int lim, int blo, int bhi,
+// FP8: S stands for the codes of K, page_scale holds what the 16 columns of each page are multiplied by.
+template <int D, int FMT>
+__device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_addr, float c, float head, const float* page_scale, bool masked, int lim, int blo, int bhi,
                                                  int j, volatile float* ref, uint64_t* decided_before, uint32_t before_parity, uint64_t* decided,
                                                  uint64_t* pv_before, uint32_t pv_parity, volatile int* abort, float& m, float& l) {
     const int lane = threadIdx.x & 31;
-    auto take_max = [&](const auto& sv, float& a, float& b) {
+    float ps[FMT == FD_KV_FP8 ? 8 : 1];
+    if (FMT == FD_KV_FP8) {
 #pragma unroll
-        for (int k = 0; k < (int)(sizeof(sv) / 4); k += 4) {
-            a = max3(a, __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
-            b = max3(b, __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
+        for (int k = 0; k < 8; k += 4) *reinterpret_cast<float4*>(ps + k) = *reinterpret_cast<const float4*>(page_scale + k);
+    }
+    // the largest of a chunk's scores, whose first page is `page`
+    auto take_max = [&](const auto& sv, float& a, float& b, [[maybe_unused]] int page) {
+        constexpr int N = sizeof(sv) / 4;
+        if constexpr (FMT == FD_KV_FP8) {
+#pragma unroll
+            for (int k0 = 0; k0 < N; k0 += 16) {
+                float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+                for (int k = k0; k < k0 + 16; k += 4) {
+                    x = max3(x, __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
+                    y = max3(y, __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
+                }
+                a = fmaxf(a, fmaxf(x, y) * ps[page + k0 / 16]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                a = max3(a, __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
+                b = max3(b, __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
+            }
         }
     };
-    auto weights = [&](const auto& x, float2 c2, float2 nm2, float2& sum0, float2& sum1, uint32_t* pk) {
+    auto weights = [&](const auto& x, float2 c2, float2 nm2, float2& sum0, float2& sum1, uint32_t* pk, [[maybe_unused]] int page) {
 #pragma unroll
         for (int k = 0; k < (int)(sizeof(x) / 4); k += 4) {
+            if (FMT == FD_KV_FP8 && k % 16 == 0) c2 = make_float2(c * ps[page + k / 16], c * ps[page + k / 16]);
             const float2 xa = __ffma2_rn(make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, nm2);
             const float2 xb = __ffma2_rn(make_float2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), c2, nm2);
             const float2 pa = make_float2(ex2_approx(xa.x), ex2_approx(xa.y)), pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
@@ -983,8 +1108,8 @@ __device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_ad
         for (int ch = 0; ch < 8; ++ch) {
             tc_wait_ld();
             if (ch < 7) tmem_ld16(s_addr + (ch + 1) * 16, sv[(ch + 1) & 1]);
-            take_max(sv[ch & 1], a, b);
-            weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 2][(ch & 3) * 8]);
+            take_max(sv[ch & 1], a, b, ch);
+            weights(sv[ch & 1], c2, nm2, sum0, sum1, &pk[ch >> 2][(ch & 3) * 8], ch);
         }
         if (j > 0) (void)wait_all(decided_before, before_parity, abort);  // (an abort is acted upon by the caller's next wait)
         slow = __any_sync(0xffffffffu, *ref != now || fmaxf(a, b) * c - head > now + kRescaleThreshold);
@@ -1011,12 +1136,21 @@ __device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_ad
                     if (!((vis >> k) & 1u)) sv[k] = 0xff800000u;  // -inf by select: S may be NaN there
             }
         };
+        // (these loops are not unrolled, and registers have no index: the chunk's two scales are read again)
+        auto reload_scales = [&]([[maybe_unused]] int ch) {
+            if constexpr (FMT == FD_KV_FP8) {
+                const float2 two = *reinterpret_cast<const float2*>(page_scale + 2 * ch);
+                ps[0] = two.x;
+                ps[1] = two.y;
+            }
+        };
         float a = -INFINITY, b = -INFINITY;
 #pragma unroll 1
         for (int ch = 0; ch < 4; ++ch) {
             uint32_t sv[32];
             load(ch, sv);
-            take_max(sv, a, b);
+            reload_scales(ch);
+            take_max(sv, a, b, 0);
         }
         const float m_new = fmaxf(a, b) * c - head;
         float alpha = 1.f, to = now;
@@ -1052,7 +1186,8 @@ __device__ __forceinline__ void softmax_tile_wide(uint32_t s_addr, uint32_t o_ad
         for (int ch = 0; ch < 4; ++ch) {
             uint32_t sv[32], pk[16];
             load(ch, sv);
-            weights(sv, c2, nm2, sum0, sum1, pk);
+            reload_scales(ch);
+            weights(sv, c2, nm2, sum0, sum1, pk, 0);
             tmem_st16(s_addr + ch * 16, pk);
         }
         l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
@@ -1114,7 +1249,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 if (j < 2) c = f4->row_scale[w.piece & 3][r];
                 const int pos0 = (pc.tile0 + j) * kTileTokens;
                 // masked: the tile reaches into the query block (or past kv_len): the row's mask applies, in tile-local columns
-                softmax_tile_wide<D>(tmem + lane_base + b3 * 128u, tmem + lane_base + 384u, c, kHead, pos0 + kTileTokens > pc.n, rm.limit - pos0,
+                softmax_tile_wide<D, FMT>(tmem + lane_base + b3 * 128u, tmem + lane_base + 384u, c, kHead, f4->sc[g & 15], pos0 + kTileTokens > pc.n, rm.limit - pos0,
                                     rm.blk_lo - pos0, rm.blk_hi - pos0, j, &f4->ref[w.piece & 1][r], &f4->decided[warp & 3][(e - 1) & 1],
                                     (uint32_t)((e - 1) >> 1) & 1u, &f4->decided[warp & 3][e & 1], &f4->pv_done[(g + 2) % 3], (uint32_t)((g - 1) / 3) & 1u,
                                     abort, m, l);
@@ -1462,7 +1597,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FMT>::kThreads, 1) attn_tc_kernel
     extern __shared__ __align__(1024) unsigned char smem[];  // the swizzled tiles need 1024-byte alignment
     unsigned char* sq = smem;
     unsigned char* sk = smem + C::kQBytes;                      // K ring
-    unsigned char* sv = sk + C::kStages * C::kKBytes;           // V ring
+    unsigned char* sv = smem + C::kVOffset;                     // V ring
     Bars* bars = reinterpret_cast<Bars*>(smem + C::kBarOffset);
     float* ex = reinterpret_cast<float*>(smem + C::kExOffset);
     int* s_cs = reinterpret_cast<int*>(smem + C::kCsOffset);
@@ -1487,8 +1622,12 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FMT>::kThreads, 1) attn_tc_kernel
             mbar_init(&bars->v_full[i], wide(FMT) ? C::kWidenWarps : 1); mbar_init(&bars->v_empty[i], 1);
         }
         if (wide(FMT)) {
-            for (int i = 0; i < C::kRawStages; ++i) { mbar_init(&f4->raw_full[i], 1); mbar_init(&f4->raw_empty[i], C::kWidenWarps); }
+            for (int i = 0; i < C::kRawStages; ++i) {  // FP8: codes and scales come apart; Q K^T reads a stage, too
+                mbar_init(&f4->raw_full[i], FMT == FD_KV_FP8 ? 2 : 1);
+                mbar_init(&f4->raw_empty[i], C::kWidenWarps + (FMT == FD_KV_FP8 ? 1 : 0));
+            }
             mbar_init(&f4->q_ready, C::kWidenWarps);
+            mbar_init(&f4->q_read, C::kWidenWarps);
             for (int i = 0; i < 3; ++i) { mbar_init(&f4->s_full[i], 1); mbar_init(&f4->p_full[i], 128); mbar_init(&f4->pv_done[i], 1); }
             for (int i = 0; i < 4; ++i) { mbar_init(&f4->decided[i][0], 1); mbar_init(&f4->decided[i][1], 1); }
         }
@@ -1627,10 +1766,13 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FMT>::kThreads, 1) attn_tc_kernel
         if constexpr (wide(FMT)) {
             unsigned char* raw = smem + C::kRawOffset;
             if (warp == kKWarp) {
-                if constexpr (FMT == FD_KV_FP8) load_role_fp8<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
+                if constexpr (FMT == FD_KV_FP8) load_role_fp8<D, MODE>(tmap, p, n_rb, raw, f4, rg, &bars->bad, abort);
                 else load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);
             } else if (warp == kVWarp) pv_role_wide<D, MODE, FMT>(sv, bars, f4, ring, tmem, rg, abort);
-            else if (warp >= 12) widen_role<D, MODE, FMT>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
+            else if (warp >= 12) {
+                if constexpr (FMT == FD_KV_FP8) widen_role_fp8<D, MODE>(p, sq, sv, raw, bars, f4, ring, rg, abort);
+                else widen_role_fp4<D, MODE>(p, sq, sk, sv, raw, bars, f4, ring, rg, abort);
+            }
         } else {
             if (warp == kKWarp) load_role<D, MODE>(tmap, p, n_rb, sk, bars->k_full, bars->k_empty, 0, rg, &bars->k_full[0], &bars->bad, abort);
             else if (warp == kVWarp) load_role<D, MODE>(tmap, p, n_rb, sv, bars->v_full, bars->v_empty, 1, rg, &bars->k_full[0], &bars->bad, abort);
@@ -1678,7 +1820,7 @@ struct TmapCache {
 
 struct TcState {
     PFN_cuTensorMapEncodeTiled_v12000 encode;
-    TmapCache kv, q;
+    TmapCache kv, kv8, q;
     int d, hkv;
     const CUtensorMap* current;
     const CUtensorMap* qcurrent;
@@ -1692,6 +1834,10 @@ cudaError_t configure_kernel() {
     cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, MODE, FMT>::kSmemBytes);
     if (e == cudaSuccess && MODE == kTcCluster)
         e = cudaFuncSetAttribute(attn_tc_kernel<D, MODE, FMT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    // the register split draws on what the launch allocates: a request beyond that would wait for ever
+    cudaFuncAttributes attr = {};
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, attn_tc_kernel<D, MODE, FMT>);
+    if (e == cudaSuccess && attr.numRegs * Cfg<D, MODE, FMT>::kThreads < Cfg<D, MODE, FMT>::kRegTotal) e = cudaErrorInvalidConfiguration;
     return e;
 }
 
@@ -1804,8 +1950,29 @@ cudaError_t attn_tc_prepare(void** state, const AttnParams& p) {
         e.map = map;
         st->qcurrent = &e.map;
     }
-    if (wide(p.fmt)) {  // pages come by untiled bulk copies: no map of the pool (the kernel's first map goes unused)
+    if (p.fmt == FD_KV_FP4) {  // pages come by untiled bulk copies: no map of the pool (the kernel's first map goes unused)
         st->current = st->qcurrent;
+        return cudaSuccess;
+    }
+    if (p.fmt == FD_KV_FP8) {
+        // d bytes x 8 rows x (K, V) x two groups of 8 rows x (page, kv-head): a box is the codes of a page and head
+        st->current = st->kv8.find(p.kvq, p.num_pages);
+        if (st->current) return cudaSuccess;
+        CUtensorMap map;
+        const cuuint64_t block = (cuuint64_t)fp8_block_bytes(p.d);
+        cuuint64_t dims[5] = {(cuuint64_t)p.d, 8, 2, 2, (cuuint64_t)p.num_pages * p.Hkv};
+        cuuint64_t strides[4] = {(cuuint64_t)p.d, block, (cuuint64_t)p.d * 8, 2 * block};
+        cuuint32_t box[5] = {(cuuint32_t)p.d, 8, 2, 2, 1};
+        cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+        const CUresult r = st->encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<unsigned char*>(p.kvq), dims, strides, box, estr,
+                                      CU_TENSOR_MAP_INTERLEAVE_NONE, p.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
+        TmapEntry& e = st->kv8.slot();
+        e.ptr = p.kvq;
+        e.n = p.num_pages;
+        e.map = map;
+        st->current = &e.map;
         return cudaSuccess;
     }
     st->current = st->kv.find(p.kv, p.num_pages);

@@ -440,6 +440,12 @@ struct ForkParams {
 };
 void launch_kv_fork(const ForkParams& p, cudaStream_t s);
 
+// What the passes of a free call hand on (in the context's scratch memory).
+struct FreeScratch {
+    int bad, total, n_free;
+    int cu[4096 + 1];     // exclusive scan of the listed sequences' pages
+    int count[1024 * 16]; // pages that each warp's run of occurrences releases (at most 1024 CTAs)
+};
 struct FreeParams {
     int n_seqs, batch, num_pages, max_pages;
     const int32_t* seqs;
@@ -449,9 +455,11 @@ struct FreeParams {
     int32_t* free_pages;
     const int32_t* n_free;
     int32_t* n_free_out;
+    FreeScratch* scratch;
+    int n_sms;
     int* status;
 };
-void launch_kv_free(const FreeParams& p, cudaStream_t s);
+int launch_kv_free(const FreeParams& p, cudaStream_t s);  // returns the number of kernels launched
 
 struct CompactParams {
     int batch, num_pages, max_pages, max_copies;

@@ -171,22 +171,27 @@ void launch_kv_fork(const ForkParams& p, cudaStream_t s) {
 }
 
 // ------------------------------------------------------------------------------------------------ free
-constexpr int kClusterThreads = 1024, kMaxPageCluster = 8;
+// The occurrences of pages in the listed sequences, numbered e = 0 .. T - 1 (sequence by sequence, page by page); a warp takes a
+// contiguous run of them.
+constexpr int kFreeThreads = 512;
+constexpr long long kFreeSmall = 8192;
 constexpr int kClaim = 0x40000000;  // a released page holds e - T - 1 - kClaim once occurrence e (of T) has claimed it: below any count
 
-__global__ void __launch_bounds__(kClusterThreads) free_kernel(FreeParams p) {
-    __shared__ int cu[kMaxBatch + 1];  // exclusive scan of the pages of the listed sequences
-    __shared__ unsigned seen[kMaxBatch / 32];
-    __shared__ int wsum[kClusterThreads / 32];
-    __shared__ int s_count;
-    const int tid = threadIdx.x, N = p.n_seqs, R = (int)cluster_rank(), C = (int)cluster_size();
-    for (int i = tid; i < kMaxBatch / 32; i += kClusterThreads) seen[i] = 0;
-    if (tid == 0) cu[0] = 0;
+struct FreeShared {
+    int cu[kMaxBatch + 1];  // exclusive scan of the pages of the listed sequences
+    unsigned seen[kMaxBatch / 32];
+    int wsum[kFreeThreads / 32];
+};
+
+// Checks and scan.  Returns whether the call is to be refused (the same in every thread).
+__device__ __forceinline__ bool free_scan(const FreeParams& p, FreeShared& sh, int n_free, int* T) {
+    const int tid = threadIdx.x, N = p.n_seqs;
+    for (int i = tid; i < kMaxBatch / 32; i += kFreeThreads) sh.seen[i] = 0;
+    if (tid == 0) sh.cu[0] = 0;
     __syncthreads();
-    const int n_free = *p.n_free;
     bool bad = n_free < 0 || n_free > p.num_pages;
     long long total = 0;
-    for (int base = 0; base < N; base += kClusterThreads) {
+    for (int base = 0; base < N; base += kFreeThreads) {
         const int i = base + tid;
         int pages = 0;
         if (i < N) {
@@ -197,86 +202,201 @@ __global__ void __launch_bounds__(kClusterThreads) free_kernel(FreeParams p) {
                 const int n = p.prefix_lens[b];
                 if (n < 0 || (long long)n > (long long)p.max_pages * 16) bad = true;
                 else pages = (n + 15) >> 4;
-                if (atomicOr(&seen[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u) bad = true;  // listed twice
+                if (atomicOr(&sh.seen[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u) bad = true;  // listed twice
             }
         }
-        if (pages > 0x1fffff) bad = true;  // (1024 of them must not pass 32 bits)
+        if (pages > 0x1fffff) bad = true;  // (512 of them must not pass 32 bits)
         pages = min(pages, 0x1fffff);
         int sum;
-        const int before = block_scan<kClusterThreads>(pages, wsum, &sum);
-        if (i < N) cu[i + 1] = (int)min(total + before + pages, 0x3fffffffLL);
+        const int before = block_scan<kFreeThreads>(pages, sh.wsum, &sum);
+        if (i < N) sh.cu[i + 1] = (int)min(total + before + pages, 0x3fffffffLL);
         total += sum;
     }
-    bad = __syncthreads_or(bad) != 0 || total >= kClaim / 2;  // the same in every CTA of the cluster
-    if (bad) {
-        if (R == 0 && tid == 0) {
+    *T = (int)min(total, 0x3fffffffLL);
+    return __syncthreads_or(bad) != 0 || total >= kClaim / 2;
+}
+
+// f(e, entry, id) for this lane's occurrences of [lo, hi), ascending, four page ids in flight; ids outside the pool are passed on.
+template <class F>
+__device__ __forceinline__ void each_occurrence(const FreeParams& p, const FreeShared& sh, int lo, int hi, F f) {
+    const int lane = threadIdx.x & 31;
+    if (lo >= hi) return;
+    int a = 0, z = p.n_seqs;  // the sequence that holds occurrence lo
+    while (z - a > 1) {
+        const int mid = (a + z) >> 1;
+        if (sh.cu[mid] <= lo) a = mid; else z = mid;
+    }
+    int32_t* row = p.page_table + (long long)p.seqs[a] * p.max_pages;
+    for (int base = lo; base < hi; base += 128) {
+        int32_t* entry[4];
+        int id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = base + u * 32 + lane;
+            entry[u] = nullptr;
+            id[u] = -1;
+            if (e < hi) {
+                if (e >= sh.cu[a + 1]) {
+                    do ++a; while (e >= sh.cu[a + 1]);
+                    row = p.page_table + (long long)p.seqs[a] * p.max_pages;
+                }
+                entry[u] = row + (e - sh.cu[a]);
+                id[u] = *entry[u];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f(base + u * 32 + lane, entry[u], id[u]);  // (entry nullptr: beyond the end; whole warps call)
+    }
+}
+
+// Owners go.
+__device__ __forceinline__ bool free_count_down(const FreeParams& p, const FreeShared& sh, int lo, int hi) {
+    bool bad_page = false;
+    each_occurrence(p, sh, lo, hi, [&](int, int32_t* entry, int id) {
+        if (!entry) return;
+        if ((unsigned)id >= (unsigned)p.num_pages || atomicSub(p.shared + id, 1) < 0) bad_page = true;  // (below 0: more owners than it has)
+    });
+    return bad_page;
+}
+// A page without owners goes to the list at its first occurrence.
+__device__ __forceinline__ void free_claim(const FreeParams& p, const FreeShared& sh, int T, int lo, int hi) {
+    each_occurrence(p, sh, lo, hi, [&](int e, int32_t* entry, int id) {
+        if (entry && (unsigned)id < (unsigned)p.num_pages && __ldcg(p.shared + id) < 0) atomicMin(p.shared + id, e - T - 1 - kClaim);
+    });
+}
+__device__ __forceinline__ bool free_claimed(const FreeParams& p, int T, int e, int32_t* entry, int id) {
+    return entry && (unsigned)id < (unsigned)p.num_pages && __ldcg(p.shared + id) == e - T - 1 - kClaim;
+}
+__device__ __forceinline__ int free_claims(const FreeParams& p, const FreeShared& sh, int T, int lo, int hi) {  // of the warp's run, in every lane
+    int n = 0;
+    each_occurrence(p, sh, lo, hi, [&](int e, int32_t* entry, int id) { n += free_claimed(p, T, e, entry, id); });
+    return __reduce_add_sync(0xffffffffu, n);
+}
+// The list: the last occurrence first, `end` the place behind the warp's run's.
+__device__ __forceinline__ bool free_push(const FreeParams& p, const FreeShared& sh, int T, int lo, int hi, int end) {
+    bool bad_page = false;
+    each_occurrence(p, sh, lo, hi, [&](int e, int32_t* entry, int id) {
+        const bool push = free_claimed(p, T, e, entry, id);
+        const unsigned who = __ballot_sync(0xffffffffu, push);
+        if (entry) *entry = -1;
+        if (push) {
+            const int at = end - 1 - __popc(who & ((1u << (threadIdx.x & 31)) - 1u));
+            p.shared[id] = 0;  // (no other occurrence's claim: theirs compare unequal to this as well)
+            if (at < p.num_pages) p.free_pages[at] = id;
+            else bad_page = true;
+        }
+        end -= __popc(who);
+    });
+    return bad_page;
+}
+__device__ __forceinline__ void run_of(int warp, int warps, int T, int* lo, int* hi) {
+    const int per = ((T + warps - 1) / warps + 31) & ~31;
+    *lo = (int)min((long long)warp * per, (long long)T);
+    *hi = (int)min((long long)*lo + per, (long long)T);
+}
+
+// Few pages: one CTA, one launch.
+__global__ void __launch_bounds__(kFreeThreads) free_small_kernel(FreeParams p) {
+    __shared__ FreeShared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, n_free = *p.n_free;
+    int T, lo, hi, all;
+    if (free_scan(p, sh, n_free, &T)) {
+        if (tid == 0) {
             atomicOr(p.status, FD_DEV_BAD_LENGTHS);
-            *p.n_free_out = n_free;  // (where that is the word others still read, they find the same in it)
+            *p.n_free_out = n_free;
         }
         return;
     }
-    const int T = (int)total;
-    const int per = (T + C - 1) / C, lo = min(R * per, T), hi = min(lo + per, T);  // this CTA's occurrences
-    auto entry = [&](int e) -> int32_t* {
-        int a = 0, z = N;
-        while (z - a > 1) {
-            const int mid = (a + z) >> 1;
-            if (cu[mid] <= e) a = mid; else z = mid;
-        }
-        return p.page_table + (long long)p.seqs[a] * p.max_pages + (e - cu[a]);
-    };
-    bool bad_page = false;
-    // ---- owners go
-    for (int e = lo + tid; e < hi; e += kClusterThreads) {
-        const int id = *entry(e);
-        if ((unsigned)id >= (unsigned)p.num_pages) { bad_page = true; continue; }
-        if (atomicSub(p.shared + id, 1) < 0) bad_page = true;  // more owners than it has
-    }
-    cluster_barrier();
-    // ---- a page without owners goes to the list at its first occurrence
-    for (int e = lo + tid; e < hi; e += kClusterThreads) {
-        const int id = *entry(e);
-        if ((unsigned)id < (unsigned)p.num_pages && __ldcg(p.shared + id) < 0) atomicMin(p.shared + id, e - T - 1 - kClaim);
-    }
-    cluster_barrier();
-    int mine = 0;
-    for (int e = lo + tid; e < hi; e += kClusterThreads) {
-        const int id = *entry(e);
-        mine += (unsigned)id < (unsigned)p.num_pages && __ldcg(p.shared + id) == e - T - 1 - kClaim;
-    }
-    int count;
-    block_scan<kClusterThreads>(mine, wsum, &count);
-    if (tid == 0) s_count = count;
-    cluster_barrier();
-    int at = n_free, all = 0;  // the last occurrences come first: this CTA's stand behind those of the ranks above it
-    for (int r = 0; r < C; ++r) {
-        const int c = peer_int(&s_count, r);
-        all += c;
-        if (r > R) at += c;
-    }
-    for (int top = hi; top > lo; top -= kClusterThreads) {  // uniform over the CTA
-        const int e = top - 1 - tid;
-        int id = -1, push = 0;
-        if (e >= lo) {
-            int32_t* en = entry(e);
-            id = *en;
-            *en = -1;
-            push = (unsigned)id < (unsigned)p.num_pages && __ldcg(p.shared + id) == e - T - 1 - kClaim;
-        }
-        int sum;
-        const int before = block_scan<kClusterThreads>(push, wsum, &sum);
-        if (push) {
-            p.shared[id] = 0;
-            if (at + before < p.num_pages) p.free_pages[at + before] = id;
-            else bad_page = true;
-        }
-        at += sum;
-    }
+    run_of(warp, kFreeThreads / 32, T, &lo, &hi);
+    bool bad_page = free_count_down(p, sh, lo, hi);
+    __syncthreads();
+    free_claim(p, sh, T, lo, hi);
+    __syncthreads();
+    const int mine = free_claims(p, sh, T, lo, hi);
+    const int before = block_scan<kFreeThreads>((tid & 31) == 0 ? mine : 0, sh.wsum, &all);
+    // the warps behind this one push first: the run ends where theirs and its own have been pushed
+    bad_page |= free_push(p, sh, T, lo, hi, n_free + all - __shfl_sync(0xffffffffu, before, 0));
     if (bad_page) atomicOr(p.status, FD_DEV_BAD_PAGE);
-    for (int i = R * kClusterThreads + tid; i < N; i += C * kClusterThreads) p.prefix_lens[p.seqs[i]] = 0;
-    if (R == 0 && tid == 0) *p.n_free_out = min(n_free + all, p.num_pages);
-    cluster_barrier();  // (a CTA's shared memory stays until its peers have read s_count)
+    for (int i = tid; i < p.n_seqs; i += kFreeThreads) p.prefix_lens[p.seqs[i]] = 0;
+    if (tid == 0) *p.n_free_out = min(n_free + all, p.num_pages);
 }
+
+// Many: a launch for each pass, the scan handed on through scratch (the last pass clears the lengths it was made from).
+template <int PASS>
+__global__ void __launch_bounds__(kFreeThreads) free_pass_kernel(FreeParams p) {
+    __shared__ FreeShared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, N = p.n_seqs;
+    constexpr int W = kFreeThreads / 32;
+    int T, n_free;
+    bool bad;
+    if (PASS == 0) {
+        n_free = *p.n_free;
+        bad = free_scan(p, sh, n_free, &T);
+        if (blockIdx.x == 0) {
+            for (int i = tid; i <= N; i += kFreeThreads) p.scratch->cu[i] = sh.cu[i];
+            if (tid == 0) {
+                p.scratch->bad = bad;
+                p.scratch->total = T;
+                p.scratch->n_free = n_free;
+                if (bad) atomicOr(p.status, FD_DEV_BAD_LENGTHS);
+            }
+        }
+    } else {
+        bad = p.scratch->bad != 0;
+        T = p.scratch->total;
+        n_free = p.scratch->n_free;
+        for (int i = tid; i <= N && !bad; i += kFreeThreads) sh.cu[i] = p.scratch->cu[i];
+        __syncthreads();
+    }
+    if (bad) {
+        if (PASS == 3 && blockIdx.x == 0 && tid == 0) *p.n_free_out = n_free;
+        return;
+    }
+    int lo, hi;
+    run_of(blockIdx.x * W + warp, gridDim.x * W, T, &lo, &hi);
+    if (PASS == 0) {
+        if (free_count_down(p, sh, lo, hi)) atomicOr(p.status, FD_DEV_BAD_PAGE);
+    } else if (PASS == 1) {
+        free_claim(p, sh, T, lo, hi);
+    } else if (PASS == 2) {
+        const int mine = free_claims(p, sh, T, lo, hi);
+        if ((tid & 31) == 0) p.scratch->count[blockIdx.x * W + warp] = mine;
+    } else {
+        // warps in front of this CTA's, and all: the counts' prefix sums
+        int before = 0, all = 0;
+        for (int i = tid; i < (int)gridDim.x * W; i += kFreeThreads) {
+            const int n = p.scratch->count[i];
+            all += n;
+            if (i < (int)blockIdx.x * W) before += n;
+        }
+        int sum_before, sum_all;
+        block_scan<kFreeThreads>(before, sh.wsum, &sum_before);
+        block_scan<kFreeThreads>(all, sh.wsum, &sum_all);
+        for (int w = 0; w < warp; ++w) sum_before += p.scratch->count[blockIdx.x * W + w];
+        if (free_push(p, sh, T, lo, hi, n_free + sum_all - sum_before)) atomicOr(p.status, FD_DEV_BAD_PAGE);
+        for (int i = blockIdx.x * kFreeThreads + tid; i < N; i += gridDim.x * kFreeThreads) p.prefix_lens[p.seqs[i]] = 0;
+        if (blockIdx.x == 0 && tid == 0) *p.n_free_out = min(n_free + sum_all, p.num_pages);
+    }
+}
+
+int launch_kv_free(const FreeParams& p, cudaStream_t s) {
+    // (the lengths are on the device: the table's width bounds what a sequence holds)
+    const long long most = (long long)p.n_seqs * p.max_pages;
+    // (up to here one CTA's passes take less than three more launches do)
+    if (most <= kFreeSmall) {
+        free_small_kernel<<<1, kFreeThreads, 0, s>>>(p);
+        return 1;
+    }
+    const int grid = (int)std::min<long long>((most + 4 * kFreeThreads - 1) / (4 * kFreeThreads), std::min(p.n_sms, 1024));
+    free_pass_kernel<0><<<grid, kFreeThreads, 0, s>>>(p);
+    free_pass_kernel<1><<<grid, kFreeThreads, 0, s>>>(p);
+    free_pass_kernel<2><<<grid, kFreeThreads, 0, s>>>(p);
+    free_pass_kernel<3><<<grid, kFreeThreads, 0, s>>>(p);
+    return 4;
+}
+
+// ------------------------------------------------------------------------------------------------ compact
+constexpr int kClusterThreads = 1024, kMaxPageCluster = 8;
 
 template <class K, class P>
 static void launch_cluster(K kernel, const P& p, int ctas, cudaStream_t s) {
@@ -292,13 +412,6 @@ static void launch_cluster(K kernel, const P& p, int ctas, cudaStream_t s) {
     cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-void launch_kv_free(const FreeParams& p, cudaStream_t s) {
-    // (the lengths are on the device: the table's width bounds what a sequence holds)
-    const long long most = (long long)p.n_seqs * p.max_pages;
-    launch_cluster(free_kernel, p, most <= 2 * kClusterThreads ? 1 : kMaxPageCluster, s);
-}
-
-// ------------------------------------------------------------------------------------------------ compact
 __global__ void __launch_bounds__(kClusterThreads) compact_kernel(CompactParams p) {
     __shared__ int wsum[kClusterThreads / 32];
     __shared__ int s_holes, s_movers, s_bad;
