@@ -112,13 +112,13 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 template <int D, int MODE, int FMT>
 struct Cfg {
     // the warps behind warp 11 widen the tiles: K and V (FP4), or V alone (FP8)
-    static constexpr int kWidenWarps = FMT == FD_KV_FP4 ? 8 : FMT == FD_KV_FP8 ? 4 : 0;
+    static constexpr int kWidenWarps = wide(FMT) ? 8 : 0;
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
     // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps.  What the groups take adds up to no more
     // than what the launch allocates: configure_kernel compares the two before the kernel's first launch.
-    static constexpr int kRegSoftmax = FMT == FD_KV_FP4 ? 144 : FMT == FD_KV_FP8 ? 176 : 224;
-    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? 72 : 56;
-    static constexpr int kRegWiden = FMT == FD_KV_FP8 ? 88 : 64;
+    static constexpr int kRegSoftmax = wide(FMT) ? 144 : 224;
+    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? 64 : 56;
+    static constexpr int kRegWiden = 64;
     static constexpr int kRegTotal = 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden;
     static_assert(kRegTotal <= 65536, "register split");
     // buffers in the K ring, and again in the V ring (wide formats: of widened tiles, fed from the raw ring)
@@ -464,15 +464,13 @@ __device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char*
     }
 }
 
-// The V tile of 8-bit pages: 16 codes a thread and pass, 128 threads.  Eight (d = 64: four) neighbouring lanes share a token's row, so
+// The V tile of 8-bit pages: 16 codes a thread and pass.  Eight (d = 64: four) neighbouring lanes share a token's row, so
 // the reads cover whole rows; of the two 16-byte words each lane stores, the lanes of the upper half of d store the second first,
 // which puts the eight lanes of a store on different banks.
-constexpr int kWidenThreads8 = 128;
-
 template <int D>
 struct RawV8 {
     static constexpr int kChunks = D / 16;
-    static constexpr int kTokens = kWidenThreads8 / kChunks;  // of a pass
+    static constexpr int kTokens = kWidenThreads / kChunks;  // of a pass
     static constexpr int kPasses = kTileTokens / kTokens;
     uint4 codes[kPasses];
     __device__ __forceinline__ void load(const unsigned char* raw) {
@@ -513,7 +511,7 @@ __device__ __forceinline__ void widen_v8(const RawV8<D>& in, const float* v_scal
     }
 }
 
-// The Q tile of a piece for K in e4m3: q = hi + lo, both e4m3, in place -- rows of d bytes, hi's 128 rows then lo's, a thread a row.  A
+// The Q tile of a piece for K in e4m3: q = hi + lo, both e4m3, in place -- rows of d bytes, hi's 128 rows then lo's, two neighbouring threads a row.  A
 // row is multiplied by the power of two that brings its largest element into [2^7, 2^8).  hi keeps four of bf16's eight bits, what
 // is left has at most four and e4m3 holds it exactly where the element is at least 2^-9 of the largest; below that q is off by at most
 // half a step of e4m3's smallest, 2^-17 of the largest element.  Q K^T is then two products at twice the rate of one in fp16, and K
@@ -521,21 +519,19 @@ __device__ __forceinline__ void widen_v8(const RawV8<D>& in, const float* v_scal
 template <int D>
 __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, float scale_log2e, int rows, uint64_t* q_read, uint32_t parity,
                                           volatile int* abort) {
-    const int r = (int)threadIdx.x - 384;
+    constexpr int kUnits = D / 16;  // eight-element units of a thread: half of its row
+    const int t = (int)threadIdx.x - 384, r = t >> 1, part = t & 1;
     const bool live = r < rows;
-    auto unit = [&](int u) -> uint4 {  // eight elements
-        return live ? *reinterpret_cast<const uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4)) : make_uint4(0, 0, 0, 0);
-    };
-    // The last eight units stay in registers.  d = 128: lo's bytes land where they were; hi's first land where units 0-3 were, read by then.
-    uint4 v[8];
+    uint4 v[kUnits];
     uint32_t mx = 0;
 #pragma unroll
-    for (int u = D / 8 - 1; u >= 0; --u) {
-        const uint4 x = unit(u);
-        if (u >= D / 8 - 8) v[u & 7] = x;
-        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = part * kUnits + i;
+        v[i] = live ? *reinterpret_cast<const uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4)) : make_uint4(0, 0, 0, 0);
+        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu)));
     }
-    if (D == 64) {  // (a row of 64 bytes lands on what were other rows; of 128, on the thread's own)
+    mx = __vmaxu2(mx, __shfl_xor_sync(0xffffffffu, mx, 1));  // (and both threads have read: d = 128, where a row lands on itself)
+    if (D == 64) {  // a row of 64 bytes lands on what were other rows
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(q_read);
         if (!wait_all(q_read, parity, abort)) return false;
@@ -543,9 +539,8 @@ __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, f
     const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);  // biased exponent of the largest magnitude
     const float f = __uint_as_float((uint32_t)(127 + 134 - e) << 23);  // 2^(134 - e), e in [14, 255]
 #pragma unroll
-    for (int u2 = 0; u2 < D / 16; ++u2) {  // 16 elements: 16 bytes of hi, 16 of lo
-        const uint4 a4 = 2 * u2 >= D / 8 - 8 ? v[(2 * u2) & 7] : unit(2 * u2), b4 = 2 * u2 >= D / 8 - 8 ? v[(2 * u2 + 1) & 7] : unit(2 * u2 + 1);
-        const uint32_t wd[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
+    for (int i = 0; i < kUnits / 2; ++i) {  // 16 elements: 16 bytes of hi, 16 of lo
+        const uint32_t wd[8] = {v[2 * i].x, v[2 * i].y, v[2 * i].z, v[2 * i].w, v[2 * i + 1].x, v[2 * i + 1].y, v[2 * i + 1].z, v[2 * i + 1].w};
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -557,11 +552,12 @@ __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, f
             const float2 ha = __half22float2(as_half2(a)), hb = __half22float2(as_half2(b));
             lo[k] = to_e4m3x2(x0 - ha.x, x1 - ha.y) | to_e4m3x2(x2 - hb.x, x3 - hb.y) << 16;
         }
-        unsigned char* at = sq + r * D + ((u2 ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
+        const int chunk = part * (kUnits / 2) + i;
+        unsigned char* at = sq + r * D + ((chunk ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + kMaxRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
-    row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
+    if (part == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
     return true;
 }
 
