@@ -109,16 +109,20 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 #define FD_STAGGER 1
 #endif
 
+// FP8: warps that widen V.  Four leave the softmax warps 176 registers; at d = 64, where the products of a tile take half the time,
+// four are not enough.  Measured, four / eight: 32k prefix, batch 16, d = 128 309 / 330 us; 4 sequences with 17 branches, d = 64 100 / 77.
+__host__ __device__ constexpr int widen_warps8(int d) { return d == 128 ? 4 : 8; }
+
 template <int D, int MODE, int FMT>
 struct Cfg {
     // the warps behind warp 11 widen the tiles: K and V (FP4), or V alone (FP8)
-    static constexpr int kWidenWarps = wide(FMT) ? 8 : 0;
+    static constexpr int kWidenWarps = FMT == FD_KV_FP4 ? 8 : FMT == FD_KV_FP8 ? widen_warps8(D) : 0;
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
     // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps.  What the groups take adds up to no more
     // than what the launch allocates: configure_kernel compares the two before the kernel's first launch.
-    static constexpr int kRegSoftmax = wide(FMT) ? 144 : 224;
-    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? 64 : 56;
-    static constexpr int kRegWiden = 64;
+    static constexpr int kRegSoftmax = FMT == FD_KV_FP4 ? 144 : FMT == FD_KV_FP8 ? (kWidenWarps == 4 ? 176 : 144) : 224;
+    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? (kWidenWarps == 4 ? 72 : 64) : 56;
+    static constexpr int kRegWiden = kWidenWarps == 4 ? 88 : 64;
     static constexpr int kRegTotal = 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden;
     static_assert(kRegTotal <= 65536, "register split");
     // buffers in the K ring, and again in the V ring (wide formats: of widened tiles, fed from the raw ring)
@@ -336,7 +340,7 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
 // FP8 load warp.  One TMA box a page brings the codes of K and V, as [8-token group][K, V][8 rows][d]: the groups of K then lie a
 // fixed stride apart, as those of V do, and K is an operand of Q K^T as it stands.  (Two untiled copies a page, K and V apart, took 464 us
 // where this takes 335: what a copy costs the TMA unit is mostly per copy.)  The scales, 16 bytes behind the codes of either,
-// come by plain loads: those of a tile are on their way while the next tile is issued, and stored behind that.
+// come by plain loads, a tile ahead.
 template <int D, int MODE>
 __device__ __forceinline__ void load_role_fp8(const CUtensorMap& tmap, const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
                                               int* bad, volatile int* abort) {
@@ -348,14 +352,11 @@ __device__ __forceinline__ void load_role_fp8(const CUtensorMap& tmap, const Att
     Walk w = {s_c, 0, {0, 0}, 0, rg.first};
     bool ok = true, waited = !p.early;
     bool bad_early = false;
-    float sc = 1.f;      // lanes 0-15: the scale of page (lane & 7) of K or V of the tile issued last,
-    int pending = -1;    // ... which is this one, or -1: none is waiting to be stored
-    auto publish_scales = [&]() {
-        if (pending < 0) return;
-        if (lane < 16) f4->sc[pending & 15][lane] = sc;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&f4->raw_full[pending % C::kRawStages]);
-        pending = -1;
+    // The scale of page (lane & 7) of K (lanes 0-7) or V (8-15).  A page that no token owns has 1: its scores are masked, but -inf times
+    // a stale scale need not be -inf.
+    auto load_scale = [&](int phys, int kvh) -> float {
+        if (lane >= 16 || phys < 0) return 1.f;
+        return __ldcg(reinterpret_cast<const float*>(p.kvq + fp8_block_offset(phys, p.Hkv, kvh, lane >> 3, D) + 16 * D));
     };
     while (w.t < e_c && ok) {
         const Piece pc = decode_piece(p, n_rb, w.t, s_c, e_c, cta, w.b);
@@ -374,31 +375,34 @@ __device__ __forceinline__ void load_role_fp8(const CUtensorMap& tmap, const Att
             return id;
         };
         int ids_cur = load_ids(0), ids_next = load_ids(1);
+        auto needs_wait = [&](int j) { return !waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n)); };
+        float sc = 1.f;
+        bool have = false;  // sc is the next tile's
         for (int j = 0; j < pc.nt; ++j) {
             const int g = w.g0 + j, st = g % C::kRawStages, use = g / C::kRawStages;
             if (j > 0 && (j & 3) == 0) { ids_cur = ids_next; ids_next = load_ids((j >> 2) + 1); }
             const int phys = __shfl_sync(0xffffffffu, ids_cur, (j & 3) * 8 + (lane & 7));
-            if (!waited && (p.early == 1 || (p.early == 3 && (pc.tile0 + j + 1) * kTileTokens > pc.n))) {
+            if (needs_wait(j)) {
                 wait_prior_launch();
                 waited = true;
                 if (bad_early) atomicOr(p.status, FD_DEV_BAD_PAGE);
             }
+            const float now = have ? sc : load_scale(phys, pc.kvh);
+            have = j + 1 < pc.nt && !needs_wait(j + 1);
+            if (have) sc = load_scale(__shfl_sync(0xffffffffu, (j & 3) == 3 ? ids_next : ids_cur, ((j + 1) & 3) * 8 + (lane & 7)), pc.kvh);
             if (!wait_all(&f4->raw_empty[st], (use & 1) ^ 1, abort)) { ok = false; break; }
             const int npg = min(8, (pc.kv_len - (pc.tile0 + j) * kTileTokens + 15) >> 4);
             if (lane == 0) mbar_arrive_expect_tx(&f4->raw_full[st], npg * C::kRawPage);
             __syncwarp();
             if (lane < 8 && phys >= 0) tma_load_5d_hint(raw + st * C::kRawBytes + lane * C::kRawPage, &tmap, 0, 0, 0, 0, phys * p.Hkv + pc.kvh, &f4->raw_full[st], policy);
+            if (lane < 16) f4->sc[g & 15][lane] = now;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&f4->raw_full[st]);
             issued = g + 1;
-            publish_scales();
-            sc = 1.f;  // (a page that no token owns: its scores are masked, but -inf times a stale scale need not be)
-            if (lane < 16 && phys >= 0) sc = __ldcg(reinterpret_cast<const float*>(p.kvq + fp8_block_offset(phys, p.Hkv, pc.kvh, lane >> 3, D) + 16 * D));
-            pending = g;
         }
-        publish_scales();
         w.advance(pc);
     }
     if (*abort) {  // drain copies still in flight before the shared memory is given back
-        publish_scales();
         for (int g = max(0, issued - C::kRawStages); g < issued; ++g) {
             const unsigned long long t0 = global_ns();
             for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
@@ -464,83 +468,101 @@ __device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char*
     }
 }
 
-// The V tile of 8-bit pages: 16 codes a thread and pass.  Eight (d = 64: four) neighbouring lanes share a token's row, so
-// the reads cover whole rows; of the two 16-byte words each lane stores, the lanes of the upper half of d store the second first,
-// which puts the eight lanes of a store on different banks.
+// The V tile of 8-bit pages: 16 codes a thread and pass.
+// Which of a pass's tokens, and which 16 codes of its row, are a thread's.  d = 128: of eight lanes that read or write together four
+// have half a row of token x, four of token x ^ 5.  The swizzle of the raw rows puts their chunks c ^ x on all eight places of a
+// 128-byte line, and that of the widened ones their units 2 c + k ^ x as well.  d = 64: two rows of four chunks.
 template <int D>
-struct RawV8 {
-    static constexpr int kChunks = D / 16;
-    static constexpr int kTokens = kWidenThreads / kChunks;  // of a pass
+struct V8Map {
+    static constexpr int kTokens = 32 * widen_warps8(D) / (D / 16);  // of a pass
     static constexpr int kPasses = kTileTokens / kTokens;
-    uint4 codes[kPasses];
-    __device__ __forceinline__ void load(const unsigned char* raw) {
-        const int t = (int)threadIdx.x - 384, c = t % kChunks;
-#pragma unroll
-        for (int it = 0; it < kPasses; ++it) {
-            const int tok = t / kChunks + it * kTokens, r = tok & 7;
-            const unsigned char* row = raw + (tok >> 3) * (2 * 8 * D) + 8 * D + r * D;
-            codes[it] = *reinterpret_cast<const uint4*>(row + ((c ^ (D == 128 ? r : r >> 1)) << 4));  // (the swizzle of the box)
+    int tok, c;
+    __device__ __forceinline__ V8Map() {
+        const int t = (int)threadIdx.x - 384;
+        if (D == 128) {
+            const int x = (t >> 4) & 3;
+            tok = (t >> 6) * 8 + ((t & 4) ? x ^ 5 : x);
+            c = (t & 3) + ((t & 8) >> 1);
+        } else {
+            tok = t >> 2;
+            c = t & 3;
         }
     }
 };
 
-template <int D, bool ZERO_TAIL>
-__device__ __forceinline__ void widen_v8(const RawV8<D>& in, const float* v_scales, unsigned char* tile, int valid) {
-    constexpr int kChunks = RawV8<D>::kChunks;
-    constexpr int kHalves = D / 64;
-    const int t = (int)threadIdx.x - 384, c = t % kChunks;
-    const bool swap = kHalves == 2 && (c & 4);
+template <int D>
+struct RawV8 {
+    uint4 codes[V8Map<D>::kPasses];
+    __device__ __forceinline__ void load(const unsigned char* raw) {
+        const V8Map<D> m;
+        const int r = m.tok & 7;
+        const unsigned char* row = raw + (m.tok >> 3) * (2 * 8 * D) + 8 * D + r * D + ((m.c ^ (D == 128 ? r : r >> 1)) << 4);  // (the swizzle of the box)
 #pragma unroll
-    for (int it = 0; it < RawV8<D>::kPasses; ++it) {
-        const int tok = t / kChunks + it * RawV8<D>::kTokens;
-        const __half2 s2 = __float2half2_rn(v_scales[tok >> 4]);  // (a power of two from 2^-15 on: exact)
-        const bool dead = ZERO_TAIL && tok >= valid;
-        const uint4 cd = in.codes[it];
-        const uint32_t wd[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
-        unsigned char* row = tile + (tok >> 3) * (kHalves * 1024) + (c >> 2) * 1024 + (tok & 7) * 128;
+        for (int it = 0; it < V8Map<D>::kPasses; ++it) codes[it] = *reinterpret_cast<const uint4*>(row + it * (V8Map<D>::kTokens / 8) * (2 * 8 * D));
+    }
+};
+
+// Tokens at or beyond `valid` become zeros, as codes: a second form of the loop below, run once a piece, would not be in the instruction
+// cache when its turn comes (2.4 us where this takes 0.6).
+template <int D>
+__device__ __forceinline__ void widen_v8(RawV8<D>& in, const float* v_scales, unsigned char* tile, int valid) {
+    constexpr int kHalves = D / 64;
+    const V8Map<D> m;
+    const int r = m.tok & 7, unit = (m.c & 3) * 2;
+    unsigned char* row = tile + (m.tok >> 3) * (kHalves * 1024) + (m.c >> 2) * 1024 + r * 128;
+    if (valid < kTileTokens) {
+#pragma unroll
+        for (int it = 0; it < V8Map<D>::kPasses; ++it)
+            if (m.tok + it * V8Map<D>::kTokens >= valid) in.codes[it] = make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int it = 0; it < V8Map<D>::kPasses; ++it) {
+        const __half2 s2 = __float2half2_rn(v_scales[(m.tok + it * V8Map<D>::kTokens) >> 4]);  // (a power of two from 2^-15 on: exact)
+        const uint32_t wd[4] = {in.codes[it].x, in.codes[it].y, in.codes[it].z, in.codes[it].w};
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             uint32_t h[4];
             e4m3x4_to_half(wd[2 * k], h[0], h[1]);
             e4m3x4_to_half(wd[2 * k + 1], h[2], h[3]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = dead ? 0u : as_u32(__hmul2(as_half2(h[i]), s2));
-            const int unit = (c & 3) * 2 + (swap ? k ^ 1 : k);
-            *reinterpret_cast<uint4*>(row + ((unit ^ (tok & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            for (int i = 0; i < 4; ++i) h[i] = as_u32(__hmul2(as_half2(h[i]), s2));
+            *reinterpret_cast<uint4*>(row + it * (V8Map<D>::kTokens / 8) * (kHalves * 1024) + (((unit + k) ^ r) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
     }
 }
 
-// The Q tile of a piece for K in e4m3: q = hi + lo, both e4m3, in place -- rows of d bytes, hi's 128 rows then lo's, two neighbouring threads a row.  A
-// row is multiplied by the power of two that brings its largest element into [2^7, 2^8).  hi keeps four of bf16's eight bits, what
-// is left has at most four and e4m3 holds it exactly where the element is at least 2^-9 of the largest; below that q is off by at most
+// The Q tile of a piece for K in e4m3: q = hi + lo, both e4m3, in place -- rows of d bytes, hi's 128 rows then lo's.  A row is
+// multiplied by the power of two that brings its largest element into [2^7, 2^8).  hi keeps four of bf16's eight bits, what is left
+// has at most four and e4m3 holds it exactly where the element is at least 2^-9 of the largest; below that q is off by at most
 // half a step of e4m3's smallest, 2^-17 of the largest element.  Q K^T is then two products at twice the rate of one in fp16, and K
 // needs no widening.  Rows no query owns become zeros, as in q_to_half.
+// d / 16 neighbouring lanes share a row, 16 elements each.  d = 128: a row lands on itself, and a rolled loop takes four rows a warp at a time
+// -- this runs once a piece, and straight-line code for it took 6 us out of a cold instruction cache.  d = 64: a row of 64 bytes
+// lands on what were other rows, so all warps read before any writes.
 template <int D>
 __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, float scale_log2e, int rows, uint64_t* q_read, uint32_t parity,
                                           volatile int* abort) {
-    constexpr int kUnits = D / 16;  // eight-element units of a thread: half of its row
-    const int t = (int)threadIdx.x - 384, r = t >> 1, part = t & 1;
-    const bool live = r < rows;
-    uint4 v[kUnits];
-    uint32_t mx = 0;
+    constexpr int kLanes = D / 16, kRows = 32 * widen_warps8(D) / kLanes, kPasses = kMaxRows / kRows;
+    const int t = (int)threadIdx.x - 384, c = t % kLanes;
+    uint4 v[D == 64 ? kPasses : 1][2];
+    auto read = [&](int n, uint4 (&x)[2]) {
+        const int r = t / kLanes + n * kRows;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = part * kUnits + i;
-        v[i] = live ? *reinterpret_cast<const uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4)) : make_uint4(0, 0, 0, 0);
-        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu)));
-    }
-    mx = __vmaxu2(mx, __shfl_xor_sync(0xffffffffu, mx, 1));  // (and both threads have read: d = 128, where a row lands on itself)
-    if (D == 64) {  // a row of 64 bytes lands on what were other rows
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(q_read);
-        if (!wait_all(q_read, parity, abort)) return false;
-    }
-    const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);  // biased exponent of the largest magnitude
-    const float f = __uint_as_float((uint32_t)(127 + 134 - e) << 23);  // 2^(134 - e), e in [14, 255]
+        for (int i = 0; i < 2; ++i) {
+            const int u = 2 * c + i;
+            x[i] = r < rows ? *reinterpret_cast<const uint4*>(sq + r * 128 + (u >> 3) * (kMaxRows * 128) + (((u & 7) ^ (r & 7)) << 4)) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    auto write = [&](int n, const uint4 (&x)[2]) {
+        const int r = t / kLanes + n * kRows;
+        const uint32_t wd[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+        uint32_t mx = 0;
 #pragma unroll
-    for (int i = 0; i < kUnits / 2; ++i) {  // 16 elements: 16 bytes of hi, 16 of lo
-        const uint32_t wd[8] = {v[2 * i].x, v[2 * i].y, v[2 * i].z, v[2 * i].w, v[2 * i + 1].x, v[2 * i + 1].y, v[2 * i + 1].z, v[2 * i + 1].w};
+        for (int k = 0; k < 8; ++k) mx = __vmaxu2(mx, wd[k] & 0x7fff7fffu);
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) mx = __vmaxu2(mx, __shfl_xor_sync(0xffffffffu, mx, o));  // (and all lanes of the row have read)
+        const int e = max((int)(max(mx & 0xffffu, mx >> 16) >> 7), 14);        // biased exponent of the largest magnitude
+        const float f = __uint_as_float((uint32_t)(127 + 134 - e) << 23);      // 2^(134 - e), e in [14, 255]
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -552,12 +574,26 @@ __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, f
             const float2 ha = __half22float2(as_half2(a)), hb = __half22float2(as_half2(b));
             lo[k] = to_e4m3x2(x0 - ha.x, x1 - ha.y) | to_e4m3x2(x2 - hb.x, x3 - hb.y) << 16;
         }
-        const int chunk = part * (kUnits / 2) + i;
-        unsigned char* at = sq + r * D + ((chunk ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
+        unsigned char* at = sq + r * D + ((c ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + kMaxRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        if (c == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
+    };
+    if (D == 128) {
+#pragma unroll 1
+        for (int n = 0; n < kPasses; ++n) {
+            read(n, v[0]);
+            write(n, v[0]);
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < kPasses; ++n) read(n, v[D == 64 ? n : 0]);
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(q_read);
+        if (!wait_all(q_read, parity, abort)) return false;
+#pragma unroll
+        for (int n = 0; n < kPasses; ++n) write(n, v[D == 64 ? n : 0]);
     }
-    if (part == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
     return true;
 }
 
@@ -681,9 +717,7 @@ __device__ __forceinline__ void widen_role_fp8(const AttnParams& p, unsigned cha
             in.load(raw + rs * C::kRawBytes);
             if (!wait_all(&bars->v_empty[st], ((g / C::kStages) & 1) ^ 1, abort)) return;
             const int valid = pc.kv_len - (pc.tile0 + j) * kTileTokens;
-            const float* vs = &f4->sc[g & 15][8];
-            if (valid >= kTileTokens) widen_v8<D, false>(in, vs, sv + st * C::kKBytes, 0);
-            else widen_v8<D, true>(in, vs, sv + st * C::kKBytes, valid);
+            widen_v8<D>(in, &f4->sc[g & 15][8], sv + st * C::kKBytes, valid);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
