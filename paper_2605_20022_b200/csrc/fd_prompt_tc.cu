@@ -1,16 +1,22 @@
 // Causal attention of packed sequences on the tensor cores: the prompt on its way in.
 //
-// A CTA works on two row tiles at a time (fd_prompt.cuh), each a stream of its own: 128 query rows, a softmax warpgroup, an S / P
-// buffer and an O accumulator in tensor memory, an MMA-issuing warp.  Both streams read the same K and V tiles (128 keys, brought
-// in by TMA through one ring), so a tile's bytes serve 256 rows, and while one stream is in its softmax the tensor pipe works on
-// the other.  Per tile and stream:
+// A CTA works on two row tiles at a time (fd_prompt.cuh), each a stream of its own: 128 query rows, a softmax warpgroup, S, P and O
+// in tensor memory, an MMA-issuing warp.  Both streams read the same K and V tiles, brought in by TMA through one ring, so a tile's
+// bytes serve 256 rows, and while one stream is in its softmax the tensor pipe works on the other.  Per tile and stream:
 //     S = Q K^T      tcgen05.mma, Q and K from shared memory, S in tensor memory
 //     P = exp2(..)   a thread a row: the row of S in registers, causal mask in the tiles the row's last key cuts, running maximum and
-//                    sum in fp32; P goes back over S in bf16 (V is bf16, and the operands of an MMA are of one type)
+//                    sum in fp32; P goes to tensor memory in bf16 (V is bf16, and the operands of an MMA are of one type)
 //     O += P V       A = P from tensor memory, B = V MN-major; O is rescaled only when a row's maximum has grown by more than 2^8
+// S and P do not share columns, so S of the next tile is made as soon as the softmax has read this one's: a warpgroup finds it ready
+// when it has written P, and the hand-overs (P -> product, product -> S, S -> softmax, 300 to 500 clocks each) run beside the
+// exponentials.  At d = 128 that leaves room for tiles of 80 keys: two streams of S (80 columns), P (40) and O (128).  With
+// tiles of 128 keys and P over S, a stream went through all of it once a tile, 5200 clocks of which the products are 1024.
 // Roles: warps 0-3 and 4-7 softmax of streams 0 and 1, 8 K and V loads, 9 and 10 MMAs of streams 0 and 1, 11 Q loads and the
 // descriptors of the items, which every role copies from a ring in shared memory.
-// Tensor memory: S0 / P0 [0,128)  S1 / P1 [128,256)  O0 [256,256+d)  O1 [384,384+d).
+//
+// Keys behind a row's last one get a weight of 0, but 0 times an infinity is not 0: in the tiles that the mask cuts for any row of the
+// item the MMA warps look for values that are not finite among the keys some row must not see, put zeros in their place, and the
+// epilogue adds what each row does see of them.
 //
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
 // given back, FD_DEV_TIMEOUT is set.
@@ -33,13 +39,22 @@ constexpr float kPRescale = 8.0f;  // log2 units
 
 template <int D>
 struct PCfg {
+    static constexpr int kKeys = D == 128 ? 80 : 128;         // keys of a tile
     static constexpr int kHalves = D / 64;
-    static constexpr int kTileBytes = kTileTokens * D * 2;    // one K, V or Q tile
-    static constexpr int kHalfBytes = kTileTokens * 128;      // 64 elements of d of its rows
-    static constexpr int kStages = D == 128 ? 5 : 10;         // tiles in the ring: K and V in turn
-    static constexpr int kBarOffset = (2 + kStages) * kTileBytes;
+    static constexpr int kQBytes = kMaxRows * D * 2;          // one Q tile
+    static constexpr int kQHalf = kMaxRows * 128;             // 64 elements of d of its rows
+    static constexpr int kTileBytes = kKeys * D * 2;          // one K or V tile
+    static constexpr int kHalfBytes = kKeys * 128;
+    static constexpr int kStages = D == 128 ? 8 : 10;         // tiles in the ring: K and V in turn
+    static constexpr int kBarOffset = 2 * kQBytes + kStages * kTileBytes;
     static constexpr int kSmemBytes = kBarOffset + 1024;
-    static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
+    // tensor memory, columns: S, P and O of stream s
+    static constexpr uint32_t kStream = kKeys + kKeys / 2 + 8 * (D == 128);  // 128 or 192
+    __device__ static constexpr uint32_t col_s(int s) { return s * kStream; }
+    __device__ static constexpr uint32_t col_p(int s) { return s * kStream + kKeys; }
+    __device__ static constexpr uint32_t col_o(int s) { return 2 * kStream + s * D; }
+    static_assert(2 * kStream + 2 * D <= 512, "tensor memory");
+    static_assert(kHalfBytes % 1024 == 0 && kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 };
 
 // What the roles know of an item.
@@ -53,11 +68,12 @@ struct ItemDesc {
 
 struct PBars {
     uint64_t full[10], empty[10];
-    uint64_t q_full[2], q_free[2], s_full[2], p_full[2], pv_done[2], o_free[2];
+    uint64_t q_full[2], q_free[2], s_full[2], s_read[2], p_full[2], pv_done[2], o_free[2];
     uint64_t desc_full[4], desc_empty[4];
     ItemDesc desc[4];
     uint32_t tmem_base;
     int abort;
+    unsigned odd[2];   // per stream, bit (item & 31): values that are not finite were taken out of a tile of the item
 };
 static_assert(sizeof(PBars) <= 1024, "barriers and descriptors");
 
@@ -93,7 +109,7 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
             for (int s = 0; s < 2; ++s) {
                 const int toks = min(p.tile_tokens, it.Lq - t0 - s * p.tile_tokens);
                 d.rows[s] = max(toks, 0) * p.G;
-                d.tiles[s] = toks > 0 ? (max(d.limit0 + s * p.tile_tokens + toks - 1, 0) + kTileTokens - 1) / kTileTokens : 0;
+                d.tiles[s] = toks > 0 ? (max(d.limit0 + s * p.tile_tokens + toks - 1, 0) + PCfg<D>::kKeys - 1) / PCfg<D>::kKeys : 0;
             }
         }
         if (n >= 4 && !wait_all(&bars->desc_empty[n & 3], ((n >> 2) + 1) & 1, abort)) break;
@@ -113,7 +129,7 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
                 mbar_arrive_expect_tx(&bars->q_full[s], p.tile_tokens * p.G * 128 * C::kHalves);
 #pragma unroll
                 for (int h = 0; h < C::kHalves; ++h)
-                    tma_load_3d(sq + s * C::kTileBytes + h * C::kHalfBytes, &qmap, h * 64, d.kvh * p.G, d.row0 + s * p.tile_tokens, &bars->q_full[s]);
+                    tma_load_3d(sq + s * C::kQBytes + h * C::kQHalf, &qmap, h * 64, d.kvh * p.G, d.row0 + s * p.tile_tokens, &bars->q_full[s]);
             }
             __syncwarp();
             ++loads[s];
@@ -145,7 +161,7 @@ __device__ __forceinline__ void prompt_load_role(const CUtensorMap& kmap, const 
                 mbar_arrive_expect_tx(&bars->full[st], C::kTileBytes);
 #pragma unroll
                 for (int h = 0; h < C::kHalves; ++h)
-                    tma_load_3d(ring + st * C::kTileBytes + h * C::kHalfBytes, (j & 1) ? &vmap : &kmap, h * 64, d.kvh, d.kv0 + (j >> 1) * kTileTokens,
+                    tma_load_3d(ring + st * C::kTileBytes + h * C::kHalfBytes, (j & 1) ? &vmap : &kmap, h * 64, d.kvh, d.kv0 + (j >> 1) * C::kKeys,
                                 &bars->full[st]);
             }
             __syncwarp();
@@ -159,96 +175,142 @@ __device__ __forceinline__ void prompt_load_role(const CUtensorMap& kmap, const 
         }
 }
 
+// Values of a V tile that are not finite, rows [lo, hi): found, reported to both streams, and replaced by zeros.  One warp.  (Both streams'
+// warps do so before their own product; whichever comes second may find zeros already, and the report.)
+template <int D>
+__device__ __forceinline__ void take_out_odd(unsigned char* vt, int lo, int hi, PBars* bars, int item) {
+    using C = PCfg<D>;
+    const int lane = threadIdx.x & 31;
+    auto at = [&](int e) -> uint4* {
+        const int r = lo + e / (8 * C::kHalves), w = e % (8 * C::kHalves);
+        return reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16);
+    };
+    const int n = (hi - lo) * 8 * C::kHalves;
+    auto odd = [](uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); };  // 0xffff where an element's exponent is all ones
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int e = lane; e < n; e += 32) {
+        const uint4 x = *at(e);
+        any |= odd(x.x) | odd(x.y) | odd(x.z) | odd(x.w);
+    }
+    if (!__any_sync(0xffffffffu, any != 0)) return;
+    if (lane < 2) atomicOr(&bars->odd[lane], 1u << (item & 31));
+    __threadfence_block();
+    __syncwarp();
+    for (int e = lane; e < n; e += 32) {
+        uint4 x = *at(e);
+        x.x &= ~odd(x.x); x.y &= ~odd(x.y); x.z &= ~odd(x.z); x.w &= ~odd(x.w);
+        *at(e) = x;
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
 template <int D>
 __device__ __forceinline__ void prompt_mma_role(int s, unsigned char* sq, unsigned char* ring, PBars* bars, uint32_t tmem, volatile int* abort) {
     using C = PCfg<D>;
-    constexpr uint32_t idesc_qk = make_idesc_bf16(128, kTileTokens, false), idesc_pv = make_idesc_bf16(128, D, true);
+    constexpr uint32_t idesc_qk = make_idesc_bf16(128, C::kKeys, false), idesc_pv = make_idesc_bf16(128, D, true);
     const int lane = threadIdx.x & 31;
-    const uint32_t col_s = tmem + s * 128u, col_o = tmem + 256u + s * 128u;
-    const uint64_t qd = make_smem_desc(smem_u32(sq + s * C::kTileBytes), 16, 1024);
+    const uint32_t col_s = tmem + C::col_s(s), col_p = tmem + C::col_p(s), col_o = tmem + C::col_o(s);
+    const uint64_t qd = make_smem_desc(smem_u32(sq + s * C::kQBytes), 16, 1024);
     int g = 0, u = 0, loads = 0;  // ring tiles, tiles of this stream, Q tiles of this stream before this item
     ItemDesc d;
     for (int n = 0; next_item(bars, n, d, abort); ++n) {
         const int mine = d.tiles[s], nt = max(d.tiles[0], d.tiles[1]);
-        if (mine > 0 && !wait_all(&bars->q_full[s], loads & 1, abort)) return;
-        for (int j = 0; j < nt; ++j, g += 2) {
-            const int ks = g % C::kStages, vs = (g + 1) % C::kStages;
-            if (!wait_all(&bars->full[ks], (g / C::kStages) & 1, abort)) return;
-            if (j >= mine) {  // the other stream's alone (what has landed only: an arrival ahead would count for the tile before)
-                if (lane == 0) mbar_arrive(&bars->empty[ks]);
-                if (!wait_all(&bars->full[vs], ((g + 1) / C::kStages) & 1, abort)) return;
-                if (lane == 0) mbar_arrive(&bars->empty[vs]);
-                continue;
-            }
-            // S is written over the P of the tile before: its product has to have completed
-            const uint64_t kd = make_smem_desc(smem_u32(ring + ks * C::kTileBytes), 16, 1024);
-            if (u > 0 && !wait_all(&bars->pv_done[s], (u - 1) & 1, abort)) return;
+        // a bit of `odd` is used again 32 items on; the roles are at most the four items of the descriptor ring apart
+        if (lane == 0) atomicAnd(&bars->odd[s], ~(1u << ((n + 16) & 31)));
+        auto issue_qk = [&](int j) -> bool {
+            const int k = g + 2 * j, st = k % C::kStages;
+            if (!wait_all(&bars->full[st], (k / C::kStages) & 1, abort)) return false;
+            // S of the tile before has been read
+            if (u + j > 0 && !wait_all(&bars->s_read[s], (u + j - 1) & 1, abort)) return false;
+            const uint64_t kd = make_smem_desc(smem_u32(ring + st * C::kTileBytes), 16, 1024);
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint64_t off = (uint64_t)(((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4);
-                    umma_ss(col_s, qd + off, kd + off, idesc_qk, kk > 0);
-                }
+                for (int kk = 0; kk < D / 16; ++kk)
+                    umma_ss(col_s, qd + (uint64_t)(((kk >> 2) * C::kQHalf + (kk & 3) * 32) >> 4),
+                            kd + (uint64_t)(((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
                 umma_commit(&bars->s_full[s]);
-                umma_commit(&bars->empty[ks]);
+                umma_commit(&bars->empty[st]);
                 if (j == mine - 1) umma_commit(&bars->q_free[s]);
             }
             __syncwarp();
-            if (!wait_all(&bars->full[vs], ((g + 1) / C::kStages) & 1, abort)) return;
-            unsigned char* vt = ring + vs * C::kTileBytes;
-            const int valid = d.Lk - j * kTileTokens;
-            if (valid < kTileTokens) {  // rows behind the sequence's last key are another's: P is 0 there, but 0 * NaN is not
-                for (int e = lane; e < (kTileTokens - valid) * 8 * C::kHalves; e += 32) {
+            return true;
+        };
+        auto issue_pv = [&](int j) -> bool {
+            const int k = g + 2 * j + 1, st = k % C::kStages;
+            if (!wait_all(&bars->full[st], (k / C::kStages) & 1, abort)) return false;
+            unsigned char* vt = ring + st * C::kTileBytes;
+            const int key0 = j * C::kKeys, valid = min(C::kKeys, d.Lk - key0);
+            if (valid < C::kKeys) {  // rows behind the sequence's last key are another's
+                for (int e = lane; e < (C::kKeys - valid) * 8 * C::kHalves; e += 32) {
                     const int r = valid + e / (8 * C::kHalves), w = e % (8 * C::kHalves);
                     *reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
             }
+            if (key0 + valid > d.limit0) take_out_odd<D>(vt, max(d.limit0 - key0, 0), valid, bars, n);
             // the first product of an item overwrites O: the epilogue of the item before must have read it
-            if (j == 0 && loads > 0 && !wait_all(&bars->o_free[s], (loads - 1) & 1, abort)) return;
+            if (j == 0 && loads > 0 && !wait_all(&bars->o_free[s], (loads - 1) & 1, abort)) return false;
             const uint64_t vd = make_smem_desc(smem_u32(vt), C::kHalfBytes, 1024);
-            if (!wait_all(&bars->p_full[s], u & 1, abort)) return;
+            if (!wait_all(&bars->p_full[s], (u + j) & 1, abort)) return false;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < kTileTokens / 16; ++kk)
-                    umma_ts(col_o, col_s + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), idesc_pv, j > 0 || kk > 0);
+                for (int kk = 0; kk < C::kKeys / 16; ++kk)
+                    umma_ts(col_o, col_p + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), idesc_pv, j > 0 || kk > 0);
                 umma_commit(&bars->pv_done[s]);
-                umma_commit(&bars->empty[vs]);
+                umma_commit(&bars->empty[st]);
             }
             __syncwarp();
-            ++u;
+            return true;
+        };
+        if (mine > 0) {
+            if (!wait_all(&bars->q_full[s], loads & 1, abort)) return;
+            if (!issue_qk(0)) return;
+            for (int j = 0; j < mine; ++j) {
+                if (j + 1 < mine && !issue_qk(j + 1)) return;
+                if (!issue_pv(j)) return;
+            }
         }
+        for (int k = g + 2 * mine; k < g + 2 * nt; ++k) {  // the other stream's alone (what has landed only: an arrival ahead would count for the tile before)
+            if (!wait_all(&bars->full[k % C::kStages], (k / C::kStages) & 1, abort)) return;
+            if (lane == 0) mbar_arrive(&bars->empty[k % C::kStages]);
+        }
+        g += 2 * nt;
+        u += mine;
         loads += mine > 0;
     }
 }
 
-// One row of S: weights against the running maximum, P over S, sums.
+// One row of S: weights against the running maximum into P, sums.  Returns false if a wait gave up.
 template <int D>
-__device__ __forceinline__ void prompt_softmax_tile(uint32_t s_addr, uint32_t o_addr, float c, int lim, bool first, float& m, float& l) {
-    uint32_t sv[4][32];
+__device__ __forceinline__ bool prompt_softmax_tile(uint32_t s_addr, uint32_t p_addr, uint32_t o_addr, float c, int lim, bool first, uint64_t* s_read,
+                                                    uint64_t* pv_done, uint32_t pv_parity, volatile int* abort, float& m, float& l) {
+    constexpr int K = PCfg<D>::kKeys;
+    uint32_t sv[K];
 #pragma unroll
-    for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_addr + ch * 32, sv[ch]);
+    for (int k = 0; k + 32 <= K; k += 32) tmem_ld32(s_addr + k, reinterpret_cast<uint32_t(&)[32]>(sv[k]));
+    if (K % 32) tmem_ld16(s_addr + K / 32 * 32, reinterpret_cast<uint32_t(&)[16]>(sv[K / 32 * 32 % K]));
     tc_wait_ld();
-    if (__any_sync(0xffffffffu, lim < kTileTokens)) {
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(s_read);
+    if (__any_sync(0xffffffffu, lim < K)) {
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (ch * 32 + k >= lim) sv[ch][k] = 0xff800000u;  // -inf by select: S may be NaN there
+        for (int k = 0; k < K; ++k)
+            if (k >= lim) sv[k] = 0xff800000u;  // -inf by select: S may be NaN there
     }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-            mx[0] = max3(mx[0], __uint_as_float(sv[ch][k]), __uint_as_float(sv[ch][k + 1]));
-            mx[1] = max3(mx[1], __uint_as_float(sv[ch][k + 2]), __uint_as_float(sv[ch][k + 3]));
-            mx[2] = max3(mx[2], __uint_as_float(sv[ch][k + 4]), __uint_as_float(sv[ch][k + 5]));
-            mx[3] = max3(mx[3], __uint_as_float(sv[ch][k + 6]), __uint_as_float(sv[ch][k + 7]));
-        }
+    for (int k = 0; k < K; k += 8) {
+        mx[0] = max3(mx[0], __uint_as_float(sv[k]), __uint_as_float(sv[k + 1]));
+        mx[1] = max3(mx[1], __uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3]));
+        mx[2] = max3(mx[2], __uint_as_float(sv[k + 4]), __uint_as_float(sv[k + 5]));
+        mx[3] = max3(mx[3], __uint_as_float(sv[k + 6]), __uint_as_float(sv[k + 7]));
+    }
     const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
     float alpha = 1.f;
     if (first || m == -INFINITY) {
@@ -258,7 +320,8 @@ __device__ __forceinline__ void prompt_softmax_tile(uint32_t s_addr, uint32_t o_
         m = m_new;
     }
     if (__any_sync(0xffffffffu, alpha != 1.f)) {
-        // the product of the tile before has completed (S was written behind it), so O is quiescent
+        if (!wait_all(pv_done, pv_parity, abort)) return false;  // O is quiescent once the product of the tile before has completed
+        tc_fence_after();
 #pragma unroll 1
         for (int ch = 0; ch < D / 16; ++ch) {
             uint32_t o[16];
@@ -273,31 +336,48 @@ __device__ __forceinline__ void prompt_softmax_tile(uint32_t s_addr, uint32_t o_
     const float mc = (m == -INFINITY) ? 0.f : m;
     const float2 c2 = make_float2(c, c), nm2 = make_float2(-mc, -mc);
     float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
+    uint32_t pk[K / 2];
 #pragma unroll
-    for (int hp = 0; hp < 2; ++hp) {
-        uint32_t pk[32];
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-            const float2 xa = __ffma2_rn(make_float2(__uint_as_float(sv[2 * hp][k]), __uint_as_float(sv[2 * hp][k + 1])), c2, nm2);
-            const float2 xb = __ffma2_rn(make_float2(__uint_as_float(sv[2 * hp + 1][k]), __uint_as_float(sv[2 * hp + 1][k + 1])), c2, nm2);
-            const float2 pa = make_float2(ex2_approx(xa.x), ex2_approx(xa.y)), pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
-            sum0 = __fadd2_rn(sum0, pa);
-            sum1 = __fadd2_rn(sum1, pb);
-            const __nv_bfloat162 ha = __floats2bfloat162_rn(pa.x, pa.y), hb = __floats2bfloat162_rn(pb.x, pb.y);
-            pk[k >> 1] = *reinterpret_cast<const uint32_t*>(&ha);
-            pk[16 + (k >> 1)] = *reinterpret_cast<const uint32_t*>(&hb);
-        }
-        tmem_st32(s_addr + hp * 32, pk);  // over columns of S that are in registers
+    for (int k = 0; k < K; k += 4) {
+        const float2 xa = __ffma2_rn(make_float2(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, nm2);
+        const float2 xb = __ffma2_rn(make_float2(__uint_as_float(sv[k + 2]), __uint_as_float(sv[k + 3])), c2, nm2);
+        const float2 pa = make_float2(ex2_approx(xa.x), ex2_approx(xa.y)), pb = make_float2(ex2_approx(xb.x), ex2_approx(xb.y));
+        sum0 = __fadd2_rn(sum0, pa);
+        sum1 = __fadd2_rn(sum1, pb);
+        const __nv_bfloat162 ha = __floats2bfloat162_rn(pa.x, pa.y), hb = __floats2bfloat162_rn(pb.x, pb.y);
+        pk[k >> 1] = *reinterpret_cast<const uint32_t*>(&ha);
+        pk[(k >> 1) + 1] = *reinterpret_cast<const uint32_t*>(&hb);
     }
     l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+    if (!first) {  // P of the tile before has been read (an item's first: its epilogue has waited)
+        if (!wait_all(pv_done, pv_parity, abort)) return false;
+        tc_fence_after();
+    }
+    tmem_st32(p_addr, reinterpret_cast<uint32_t(&)[32]>(pk[0]));
+    if (K == 128) tmem_st32(p_addr + 32, reinterpret_cast<uint32_t(&)[32]>(pk[K == 128 ? 32 : 0]));
+    else tmem_st8(p_addr + 32, reinterpret_cast<uint32_t(&)[8]>(pk[K == 128 ? 0 : 32]));
     tc_wait_st();
+    return true;
+}
+
+// What a row of the item sees of the values that were taken out, for columns [col, col + 32).
+__device__ __forceinline__ void add_odd(const PromptParams& p, const ItemDesc& d, int limit, int D, int col, float (&o)[32]) {
+    for (int j = max(d.limit0, 0); j < limit; ++j) {
+        const __nv_bfloat16* v = p.v + ((long long)d.kv0 + j) * p.kv_stride + (long long)d.kvh * D + col;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const float x = __bfloat162float(v[k]);
+            if (!(fabsf(x) <= 3.4028234e38f)) o[k] += x;  // (its weight is positive)
+        }
+    }
 }
 
 template <int D>
 __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p, PBars* bars, uint32_t tmem, volatile int* abort) {
+    using C = PCfg<D>;
     const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, r = warp * 32 + lane, G = p.G;
     const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
-    const uint32_t s_addr = tmem + lane_base + s * 128u, o_addr = tmem + lane_base + 256u + s * 128u;
+    const uint32_t s_addr = tmem + lane_base + C::col_s(s), p_addr = tmem + lane_base + C::col_p(s), o_addr = tmem + lane_base + C::col_o(s);
     const int tok = r / G;
     int u = 0;
     ItemDesc d;
@@ -312,7 +392,15 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
         for (int j = 0; j < nt; ++j, ++u) {
             if (!wait_all(&bars->s_full[s], u & 1, abort)) return;
             tc_fence_after();
-            if (warp_live) prompt_softmax_tile<D>(s_addr, o_addr, c, live ? limit - j * kTileTokens : kTileTokens, j == 0, m, l);
+            if (warp_live) {
+                if (!prompt_softmax_tile<D>(s_addr, p_addr, o_addr, c, live ? limit - j * C::kKeys : C::kKeys, j == 0, &bars->s_read[s], &bars->pv_done[s],
+                                            (u - 1) & 1, abort, m, l))
+                    return;
+            } else {
+                if (lane == 0) mbar_arrive(&bars->s_read[s]);
+                // (every phase of pv_done is waited for, so that the epilogue's wait means the last one)
+                if (j > 0 && !wait_all(&bars->pv_done[s], (u - 1) & 1, abort)) return;
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->p_full[s]);
@@ -322,6 +410,7 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
             if (!wait_all(&bars->pv_done[s], (u - 1) & 1, abort)) return;
             tc_fence_after();
         }
+        const bool odd = (*static_cast<volatile unsigned*>(&bars->odd[s]) >> (n & 31) & 1u) != 0;
         const float inv = limit > 0 ? 1.f / l : 0.f;
 #pragma unroll
         for (int ch = 0; ch < D / 32; ++ch) {
@@ -337,6 +426,7 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars->o_free[s]);  // O has been read: the next item may overwrite it
                 }
+                if (odd && live) add_odd(p, d, limit, D, ch * 32, o);
             } else {
 #pragma unroll
                 for (int k = 0; k < 32; ++k) o[k] = 0.f;
@@ -352,7 +442,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     using C = PCfg<D>;
     extern __shared__ __align__(1024) unsigned char smem[];  // the swizzled tiles need 1024-byte alignment
     unsigned char* sq = smem;
-    unsigned char* ring = smem + 2 * C::kTileBytes;
+    unsigned char* ring = smem + 2 * C::kQBytes;
     PBars* bars = reinterpret_cast<PBars*>(smem + C::kBarOffset);
     volatile int* abort = &bars->abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -366,12 +456,14 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
             mbar_init(&bars->q_full[s], 1);
             mbar_init(&bars->q_free[s], 1);
             mbar_init(&bars->s_full[s], 1);
+            mbar_init(&bars->s_read[s], 4);
             mbar_init(&bars->p_full[s], 4);
             mbar_init(&bars->pv_done[s], 1);
             mbar_init(&bars->o_free[s], 4);
         }
         for (int i = 0; i < 4; ++i) { mbar_init(&bars->desc_full[i], 1); mbar_init(&bars->desc_empty[i], 11); }  // 8 softmax, 2 MMA, 1 load warps
         bars->abort = 0;
+        bars->odd[0] = bars->odd[1] = 0;
         mbar_fence_init();
         prefetch_tmap(&qmap); prefetch_tmap(&kmap); prefetch_tmap(&vmap);
     }
@@ -457,8 +549,8 @@ cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s)
     const __nv_bfloat16 *kp = p.total_kv ? p.k : p.q, *vp = p.total_kv ? p.v : p.q;
     const int kv_rows = p.total_kv ? p.total_kv : 1;
     if (!find_map(st, p.q, p.q_stride, p.total_q, p.Hq, p.d, p.G, p.tile_tokens, &q) ||
-        !find_map(st, kp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, kTileTokens, &k) ||
-        !find_map(st, vp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, kTileTokens, &v))
+        !find_map(st, kp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &k) ||
+        !find_map(st, vp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &v))
         return cudaErrorInvalidValue;
     if (p.d == 64) prompt_tc_kernel<64><<<p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s>>>(q, k, v, p);
     else prompt_tc_kernel<128><<<p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s>>>(q, k, v, p);
