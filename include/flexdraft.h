@@ -484,9 +484,8 @@ fd_status fd_attn_draft_verify_fp8(fd_ctx* ctx, int batch, int total_q_rows, con
  *   kv_lens         device, [B] int32, or NULL: the same as q_lens
  *   out             device, [T, Hq, d] bf16, 16-byte aligned; fully overwritten; shares no bytes with q, k or v
  *
- * Inconsistent lengths zero all T rows (FD_DEV_BAD_LENGTHS).  Keys and values of a sequence never reach another one.  Within a
- * sequence the elements of v are taken to be finite: an infinity or a NaN in v_b[j] reaches the rows in front of j whose last key
- * lies in the same 128 keys.
+ * Inconsistent lengths zero all T rows (FD_DEV_BAD_LENGTHS).  What a row must not see -- another sequence, a later position --
+ * never reaches it, infinities and NaN included.
  * Arithmetic: bf16 inputs, fp32 scores / softmax / accumulation, softmax weights rounded to bf16 in front of the product with v,
  * bf16 output.
  */

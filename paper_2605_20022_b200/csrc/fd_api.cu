@@ -866,8 +866,10 @@ fd_status fd_attn_prompt(fd_ctx* c, int batch, int total_q_rows, int total_kv_ro
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;
     if (tc && fd::prompt_tc_prepare(&c->prompt_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
-    fd::launch_prompt_plan(p, s);
-    c->launches += 1;
+    if (!tc || !fd::prompt_tc_plans_itself(batch)) {
+        fd::launch_prompt_plan(p, s);
+        c->launches += 1;
+    }
     if (tc) {
         if (fd::launch_prompt_tc(c->prompt_state, p, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
         c->launches += 1;

@@ -81,6 +81,7 @@ void launch_prompt_plan(const PromptParams& p, cudaStream_t s);
 cudaError_t prompt_simt_prepare(int d);
 void launch_prompt_simt(const PromptParams& p, cudaStream_t s);
 cudaError_t prompt_tc_prepare(void** state, const PromptParams& p);
+bool prompt_tc_plans_itself(int batch);  // (then the plan kernel is not needed)
 cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s);
 void prompt_tc_free(void* state);
 

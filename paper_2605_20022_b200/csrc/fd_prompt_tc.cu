@@ -36,6 +36,9 @@ namespace {
 
 constexpr int kPThreads = 384;
 constexpr float kPRescale = 8.0f;  // log2 units
+// Calls of at most this many sequences plan for themselves, a lane a sequence: the one warp that hands out items makes the scans and
+// sorts, 0.4 us instead of a launch in front.
+constexpr int kSelfBatch = 32;
 
 template <int D>
 struct PCfg {
@@ -45,15 +48,16 @@ struct PCfg {
     static constexpr int kQHalf = kMaxRows * 128;             // 64 elements of d of its rows
     static constexpr int kTileBytes = kKeys * D * 2;          // one K or V tile
     static constexpr int kHalfBytes = kKeys * 128;
-    static constexpr int kStages = D == 128 ? 8 : 10;         // tiles in the ring: K and V in turn
-    static constexpr int kBarOffset = 2 * kQBytes + kStages * kTileBytes;
-    static constexpr int kSmemBytes = kBarOffset + 1024;
+    static constexpr int kStages = D == 128 ? 7 : 10;         // tiles in the ring: K and V in turn
+    static constexpr int kOutOffset = 2 * kQBytes + kStages * kTileBytes;  // a softmax warp's 32 rows x 32 columns on their way out
+    static constexpr int kBarOffset = kOutOffset + 8 * 2048;
+    static constexpr int kSmemBytes = kBarOffset + 2048;
     // tensor memory, columns: S, P and O of stream s
-    static constexpr uint32_t kStream = kKeys + kKeys / 2 + 8 * (D == 128);  // 128 or 192
+    static constexpr uint32_t kStream = D == 128 ? 128 : 192;
     __device__ static constexpr uint32_t col_s(int s) { return s * kStream; }
     __device__ static constexpr uint32_t col_p(int s) { return s * kStream + kKeys; }
     __device__ static constexpr uint32_t col_o(int s) { return 2 * kStream + s * D; }
-    static_assert(2 * kStream + 2 * D <= 512, "tensor memory");
+    static_assert(kKeys + kKeys / 2 <= kStream && 2 * kStream + 2 * D <= 512, "tensor memory");
     static_assert(kHalfBytes % 1024 == 0 && kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 };
 
@@ -74,8 +78,10 @@ struct PBars {
     uint32_t tmem_base;
     int abort;
     unsigned odd[2];   // per stream, bit (item & 31): values that are not finite were taken out of a tile of the item
+    int fatal;         // lengths inconsistent: no item is handed out, the output is zeros
+    int plan[5 * kSelfBatch + 3];  // a call that plans for itself: its PromptPlan
 };
-static_assert(sizeof(PBars) <= 1024, "barriers and descriptors");
+static_assert(sizeof(PBars) <= 2048, "barriers, descriptors and the plan");
 
 // A role's next item, copied from the ring.  Whole warps.
 __device__ __forceinline__ bool next_item(PBars* bars, int n, ItemDesc& d, volatile int* abort) {
@@ -86,11 +92,60 @@ __device__ __forceinline__ bool next_item(PBars* bars, int n, ItemDesc& d, volat
     return d.kvh >= 0;
 }
 
+// The plan of a call of at most kSelfBatch sequences, by one warp.  Returns whether the lengths are consistent.
+__device__ __forceinline__ bool self_plan_prompt(const PromptParams& p, PBars* bars, PromptPlan* pl) {
+    const int lane = threadIdx.x & 31, B = p.batch;
+    int* a = bars->plan;
+    *pl = {a, a + kSelfBatch + 1, a + 2 * kSelfBatch + 2, a + 3 * kSelfBatch + 2, a + 4 * kSelfBatch + 2, nullptr};
+    long long Lq = 0, Lk = 0;
+    bool bad = false;
+    if (lane < B) {
+        Lq = p.q_lens[lane];
+        Lk = p.kv_lens ? p.kv_lens[lane] : Lq;
+        bad = Lq < 0 || Lk < 0;
+    }
+    long long sq = Lq, sk = Lk;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long uq = __shfl_up_sync(0xffffffffu, sq, o), uk = __shfl_up_sync(0xffffffffu, sk, o);
+        if (lane >= o) { sq += uq; sk += uk; }
+    }
+    bad = __any_sync(0xffffffffu, bad) || __shfl_sync(0xffffffffu, sq, 31) != p.total_q || __shfl_sync(0xffffffffu, sk, 31) != p.total_kv;
+    const int n = lane < B && !bad ? (int)((Lq + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens)) : -1;
+    int rank = 0;  // sequences in front of this one: longer, or as long and earlier
+#pragma unroll
+    for (int o = 0; o < 32; ++o) {
+        const int x = __shfl_sync(0xffffffffu, n, o);
+        rank += x > n || (x == n && o < lane);
+    }
+    if (lane < B) {
+        pl->cu_q[lane + 1] = (int)sq;
+        pl->cu_kv[lane + 1] = (int)sk;
+        pl->perm[rank] = lane;
+        pl->blocks[rank] = n;
+    }
+    if (lane == 0) { pl->cu_q[0] = 0; pl->cu_kv[0] = 0; pl->pre[0] = 0; }
+    __syncwarp();
+    int pre = lane < B ? pl->blocks[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, pre, o);
+        if (lane >= o) pre += u;
+    }
+    if (lane < B) pl->pre[lane + 1] = pre;
+    __syncwarp();
+    if (bad && lane == 0 && blockIdx.x == 0) atomicOr(p.status, FD_DEV_BAD_LENGTHS);
+    return !bad;
+}
+
 template <int D>
 __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const PromptParams& p, unsigned char* sq, PBars* bars, volatile int* abort) {
     using C = PCfg<D>;
     const int lane = threadIdx.x & 31;
-    const long long total = *p.plan.fatal ? 0 : (long long)p.plan.pre[p.batch] * p.Hkv;
+    PromptPlan plan = p.plan;
+    const bool fine = p.batch <= kSelfBatch ? self_plan_prompt(p, bars, &plan) : *p.plan.fatal == 0;
+    if (!fine && lane == 0) bars->fatal = 1;
+    const long long total = fine ? (long long)plan.pre[p.batch] * p.Hkv : 0;
     int loads[2] = {0, 0};
     for (int turn = 0, n = 0;; ++turn) {
         const long long t = prompt_turn(turn, blockIdx.x, gridDim.x);
@@ -98,7 +153,7 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
         if (!done && t >= total) continue;
         ItemDesc d = {-1, 0, 0, 0, 0, {0, 0}, {0, 0}, 0};
         if (!done) {
-            const PromptItem it = prompt_item(p.plan, p.batch, p.Hkv, t);
+            const PromptItem it = prompt_item(plan, p.batch, p.Hkv, t);
             const int t0 = it.place * 2 * p.tile_tokens;
             d.kvh = it.kvh;
             d.row0 = it.row0 + t0;
@@ -186,9 +241,10 @@ __device__ __forceinline__ void take_out_odd(unsigned char* vt, int lo, int hi, 
         return reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16);
     };
     const int n = (hi - lo) * 8 * C::kHalves;
-    auto odd = [](uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); };  // 0xffff where an element's exponent is all ones
+    // bits 15 and 31: the element's exponent is all ones (its magnitude carries past 0x7f80)
+    auto odd = [](uint32_t x) { return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
     uint32_t any = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int e = lane; e < n; e += 32) {
         const uint4 x = *at(e);
         any |= odd(x.x) | odd(x.y) | odd(x.z) | odd(x.w);
@@ -197,10 +253,11 @@ __device__ __forceinline__ void take_out_odd(unsigned char* vt, int lo, int hi, 
     if (lane < 2) atomicOr(&bars->odd[lane], 1u << (item & 31));
     __threadfence_block();
     __syncwarp();
+    auto keep = [&](uint32_t x) { const uint32_t o = odd(x) >> 15; return x & ~(o * 0xffffu); };
+#pragma unroll 1
     for (int e = lane; e < n; e += 32) {
         uint4 x = *at(e);
-        x.x &= ~odd(x.x); x.y &= ~odd(x.y); x.z &= ~odd(x.z); x.w &= ~odd(x.w);
-        *at(e) = x;
+        *at(e) = make_uint4(keep(x.x), keep(x.y), keep(x.z), keep(x.w));
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -356,29 +413,40 @@ __device__ __forceinline__ bool prompt_softmax_tile(uint32_t s_addr, uint32_t p_
     tmem_st32(p_addr, reinterpret_cast<uint32_t(&)[32]>(pk[0]));
     if (K == 128) tmem_st32(p_addr + 32, reinterpret_cast<uint32_t(&)[32]>(pk[K == 128 ? 32 : 0]));
     else tmem_st8(p_addr + 32, reinterpret_cast<uint32_t(&)[8]>(pk[K == 128 ? 0 : 32]));
+    static_assert(K == 80 || K == 128, "columns of P");
     tc_wait_st();
     return true;
 }
 
-// What a row of the item sees of the values that were taken out, for columns [col, col + 32).
-__device__ __forceinline__ void add_odd(const PromptParams& p, const ItemDesc& d, int limit, int D, int col, float (&o)[32]) {
-    for (int j = max(d.limit0, 0); j < limit; ++j) {
-        const __nv_bfloat16* v = p.v + ((long long)d.kv0 + j) * p.kv_stride + (long long)d.kvh * D + col;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const float x = __bfloat162float(v[k]);
-            if (!(fabsf(x) <= 3.4028234e38f)) o[k] += x;  // (its weight is positive)
+// What a row of the item sees of the values that were taken out of its tiles goes into its output, which stands in `dst` without them.
+// (Their weights are positive: an infinity or a NaN of them is the sum's, whatever the rest.)
+__device__ __forceinline__ void add_odd(const PromptParams& p, const ItemDesc& d, int limit, int D, __nv_bfloat16* dst) {
+    for (int c = 0; c < D; ++c) {
+        float x = 0.f;
+        for (int j = max(d.limit0, 0); j < limit; ++j) {
+            const float v = __bfloat162float(p.v[((long long)d.kv0 + j) * p.kv_stride + (long long)d.kvh * D + c]);
+            if (!(fabsf(v) <= 3.4028234e38f)) x += v;
         }
+        if (x != 0.f) dst[c] = __float2bfloat16(__bfloat162float(dst[c]) + x);
     }
 }
 
 template <int D>
-__device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p, PBars* bars, uint32_t tmem, volatile int* abort) {
+__device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p, unsigned char* out_stage, PBars* bars, uint32_t tmem, volatile int* abort) {
     using C = PCfg<D>;
     const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, r = warp * 32 + lane, G = p.G;
     const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + C::col_s(s), p_addr = tmem + lane_base + C::col_p(s), o_addr = tmem + lane_base + C::col_o(s);
     const int tok = r / G;
+    // Results leave through shared memory, 32 columns at a time: a thread has a row, but four neighbouring lanes write 64 bytes of one
+    // row, eight rows an instruction (a thread's row by itself is a line of memory for every 16 bytes: FIGURE_EPI).
+    unsigned char* stage = out_stage + (threadIdx.x >> 5) * 2048;
+    int off[4];  // where the rows that this lane writes start, from the item's first
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int R = warp * 32 + i * 8 + (lane >> 2);
+        off[i] = (R / G * p.Hq + R % G) * D + (lane & 3) * 8;
+    }
     int u = 0;
     ItemDesc d;
     for (int n = 0; next_item(bars, n, d, abort); ++n) {
@@ -405,33 +473,46 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->p_full[s]);
         }
-        __nv_bfloat16* dst = p.out + (((long long)d.row0 + s * p.tile_tokens + tok) * p.Hq + d.kvh * G + r % G) * D;
+        __nv_bfloat16* base = p.out + (((long long)d.row0 + s * p.tile_tokens) * p.Hq + d.kvh * G) * D;
         if (nt > 0) {
             if (!wait_all(&bars->pv_done[s], (u - 1) & 1, abort)) return;
             tc_fence_after();
         }
-        const bool odd = (*static_cast<volatile unsigned*>(&bars->odd[s]) >> (n & 31) & 1u) != 0;
         const float inv = limit > 0 ? 1.f / l : 0.f;
 #pragma unroll
         for (int ch = 0; ch < D / 32; ++ch) {
-            float o[32];
+            uint32_t raw[32];
             if (nt > 0) {
-                uint32_t raw[32];
                 tmem_ld32(o_addr + ch * 32, raw);
                 tc_wait_ld();
-#pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = limit > 0 ? __uint_as_float(raw[k]) : 0.f;  // (a row that sees no key: zeros)
                 if (ch == D / 32 - 1) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars->o_free[s]);  // O has been read: the next item may overwrite it
                 }
-                if (odd && live) add_odd(p, d, limit, D, ch * 32, o);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = 0.f;
             }
-            if (live) store_cols_bf16<32>(dst + ch * 32, o, inv);
+            if (!warp_live) continue;
+            __syncwarp();  // the chunk before has been read
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                __align__(16) __nv_bfloat162 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)  // (a row that sees no key: zeros)
+                    v[k] = limit > 0 ? __floats2bfloat162_rn(__uint_as_float(raw[8 * q + 2 * k]) * inv, __uint_as_float(raw[8 * q + 2 * k + 1]) * inv)
+                                     : __floats2bfloat162_rn(0.f, 0.f);
+                *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = *reinterpret_cast<const uint4*>(v);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = i * 8 + (lane >> 2);
+                const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + (((lane & 3) ^ ((row >> 1) & 3)) << 4));
+                if (warp * 32 + row < rows) *reinterpret_cast<uint4*>(base + off[i] + ch * 32) = v;
+            }
+        }
+        if (*static_cast<volatile unsigned*>(&bars->odd[s]) >> (n & 31) & 1u) {
+            __syncwarp();
+            if (live) add_odd(p, d, limit, D, base + ((long long)tok * p.Hq + r % G) * D);
         }
     }
 }
@@ -443,6 +524,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     extern __shared__ __align__(1024) unsigned char smem[];  // the swizzled tiles need 1024-byte alignment
     unsigned char* sq = smem;
     unsigned char* ring = smem + 2 * C::kQBytes;
+    unsigned char* out_stage = smem + C::kOutOffset;
     PBars* bars = reinterpret_cast<PBars*>(smem + C::kBarOffset);
     volatile int* abort = &bars->abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -464,6 +546,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) { mbar_init(&bars->desc_full[i], 1); mbar_init(&bars->desc_empty[i], 11); }  // 8 softmax, 2 MMA, 1 load warps
         bars->abort = 0;
         bars->odd[0] = bars->odd[1] = 0;
+        bars->fatal = 0;
         mbar_fence_init();
         prefetch_tmap(&qmap); prefetch_tmap(&kmap); prefetch_tmap(&vmap);
     }
@@ -472,14 +555,10 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
-    if (*p.plan.fatal) {  // inconsistent lengths: a defined output, zeros (no role has started: the Q warp would find no item)
-        const long long n16 = (long long)p.total_q * p.Hq * D / 8;
-        for (long long i = (long long)blockIdx.x * kPThreads + tid; i < n16; i += (long long)gridDim.x * kPThreads)
-            reinterpret_cast<uint4*>(p.out)[i] = make_uint4(0, 0, 0, 0);
-    } else if (warp < 8) {
+    if (warp < 8) {
         // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168, what the launch allocated
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(224));
-        prompt_softmax_role<D>(warp >> 2, p, bars, tmem, abort);
+        prompt_softmax_role<D>(warp >> 2, p, out_stage, bars, tmem, abort);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(56));
         if (warp == 8) prompt_load_role<D>(kmap, vmap, ring, bars, abort);
@@ -490,6 +569,11 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     tc_fence_before();
     __syncthreads();
     if (warp == 9) tmem_dealloc(tmem, 512);
+    if (bars->fatal) {  // inconsistent lengths: a defined output, zeros
+        const long long n16 = (long long)p.total_q * p.Hq * D / 8;
+        for (long long i = (long long)blockIdx.x * kPThreads + tid; i < n16; i += (long long)gridDim.x * kPThreads)
+            reinterpret_cast<uint4*>(p.out)[i] = make_uint4(0, 0, 0, 0);
+    }
 }
 
 // Tensor maps already encoded, by what they were made from.
@@ -541,6 +625,8 @@ cudaError_t prompt_tc_prepare(void** state, const PromptParams& p) {
     *state = st;
     return cudaSuccess;
 }
+
+bool prompt_tc_plans_itself(int batch) { return batch <= kSelfBatch; }
 
 cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s) {
     PromptState* st = static_cast<PromptState*>(state);

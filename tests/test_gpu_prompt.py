@@ -157,10 +157,20 @@ def test_what_a_sequence_must_not_see(d, path):
         k3[253 + 200:253 + 300] = float("nan")                  # keys of the fourth sequence from 200 on
         got = _call(ctx, q, k3, v, ql, None)
         assert torch.equal(got[253:453].view(torch.int16), clean[253:453].view(torch.int16))
+        for at, value in ((0, float("inf")), (77, float("nan")), (130, -float("inf")), (200, float("inf")), (299, float("nan"))):
+            v3 = v.clone()                                      # a value of the fourth sequence, kv-head 1: the rows in front, and the other head
+            v3[253 + at, 1, 3:d:7] = value
+            got = _call(ctx, q, k, v3, ql, None)
+            assert torch.equal(got[:253 + at].view(torch.int16), clean[:253 + at].view(torch.int16))
+            assert torch.equal(got[:, :4].view(torch.int16), clean[:, :4].view(torch.int16))
+            behind, kept = got[253 + at:553, 4:].float(), torch.ones(d, dtype=torch.bool)
+            kept[3:d:7] = False
+            assert torch.equal(behind[..., kept], clean[253 + at:553, 4:].float()[..., kept])
+            assert torch.isnan(behind[..., 3:d:7]).all() if value != value else (behind[..., 3:d:7] == value).all()
         v3 = v.clone()
-        v3[253 + 256:] = float("inf")                           # values: rows whose last key lies in an earlier tile
-        got = _call(ctx, q, k, v3, ql, None)
-        assert torch.equal(got[:253 + 256].view(torch.int16), clean[:253 + 256].view(torch.int16))
+        v3[253 + 160, 1, 0], v3[253 + 170, 1, 0] = float("inf"), -float("inf")
+        got = _call(ctx, q, k, v3, ql, None)[253:553, 4:, 0].float()
+        assert torch.isfinite(got[:160]).all() and (got[160:170] == float("inf")).all() and torch.isnan(got[170:]).all()
         assert fd.fd_last_device_status(ctx) == 0
     finally:
         fd.fd_destroy(ctx)
