@@ -11,11 +11,11 @@
 // when it has written P, and the hand-overs (P -> product, product -> S, S -> softmax, 300 to 500 clocks each) run beside the
 // exponentials.  At d = 128 that leaves room for tiles of 80 keys: two streams of S (80 columns), P (40) and O (128).  With
 // tiles of 128 keys and P over S, a stream went through all of it once a tile, 5200 clocks of which the products are 1024.
-// Roles: warps 0-3 and 4-7 softmax of streams 0 and 1, 8 K and V loads, 9 and 10 MMAs of streams 0 and 1, 11 Q loads and the
-// descriptors of the items, which every role copies from a ring in shared memory.
+// Roles: warps 0-3 and 4-7 softmax of streams 0 and 1, 8 K and V loads, 9 and 10 MMAs of streams 0 and 1, 11 Q loads, the
+// descriptors of the items, which every role copies from a ring in shared memory, and the look through V tiles (below).
 //
 // Keys behind a row's last one get a weight of 0, but 0 times an infinity is not 0: in the tiles that the mask cuts for any row of the
-// item the MMA warps look for values that are not finite among the keys some row must not see, put zeros in their place, and the
+// item a warp looks for values that are not finite among the keys some row must not see, puts zeros in their place, and the
 // epilogue adds what each row does see of them.
 //
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
@@ -74,6 +74,7 @@ struct PBars {
     uint64_t full[10], empty[10];
     uint64_t q_full[2], q_free[2], s_full[2], s_read[2], p_full[2], pv_done[2], o_free[2];
     uint64_t desc_full[4], desc_empty[4];
+    uint64_t cut_full[8];  // a V tile that is to be looked through has landed; slot = number of such tiles & 7 (the ring holds five V tiles)
     ItemDesc desc[4];
     uint32_t tmem_base;
     int abort;
@@ -90,6 +91,43 @@ __device__ __forceinline__ bool next_item(PBars* bars, int n, ItemDesc& d, volat
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(&bars->desc_empty[n & 3]);
     return d.kvh >= 0;
+}
+
+// Is V tile j of an item looked through before it is used?  Where the mask cuts it for a row of the item, or the sequence ends in it.
+template <int D>
+__device__ __forceinline__ bool is_cut(const ItemDesc& d, int j) { return (j + 1) * PCfg<D>::kKeys > min(d.limit0, d.Lk); }
+
+// Looks through a V tile that has landed: of its rows [lo, valid), which some row of the item must not see, values that are not finite
+// are reported to both streams and replaced by zeros; rows from `valid` on, another sequence's, become zeros.  One warp.
+template <int D>
+__device__ __forceinline__ void clean_tile(unsigned char* vt, int lo, int valid, PBars* bars, int item) {
+    using C = PCfg<D>;
+    const int lane = threadIdx.x & 31, n0 = lo * 8 * C::kHalves, n1 = min(valid, C::kKeys) * 8 * C::kHalves;
+    auto at = [&](int e) -> uint4* {
+        const int r = e / (8 * C::kHalves), w = e % (8 * C::kHalves);
+        return reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16);
+    };
+    // bits 15 and 31: the element's exponent is all ones (its magnitude carries past 0x7f80)
+    auto odd = [](uint32_t x) { return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int e = n0 + lane; e < n1; e += 32) {
+        const uint4 x = *at(e);
+        any |= odd(x.x) | odd(x.y) | odd(x.z) | odd(x.w);
+    }
+    if (__any_sync(0xffffffffu, any != 0)) {
+        if (lane < 2) atomicOr(&bars->odd[lane], 1u << (item & 31));
+        auto keep = [&](uint32_t x) { const uint32_t o = odd(x) >> 15; return x & ~(o * 0xffffu); };
+#pragma unroll 1
+        for (int e = n0 + lane; e < n1; e += 32) {
+            uint4 x = *at(e);
+            *at(e) = make_uint4(keep(x.x), keep(x.y), keep(x.z), keep(x.w));
+        }
+    }
+#pragma unroll 1
+    for (int e = n1 + lane; e < C::kKeys * 8 * C::kHalves; e += 32) *at(e) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    __syncwarp();
 }
 
 // The plan of a call of at most kSelfBatch sequences, by one warp.  Returns whether the lengths are consistent.
@@ -139,20 +177,21 @@ __device__ __forceinline__ bool self_plan_prompt(const PromptParams& p, PBars* b
 }
 
 template <int D>
-__device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const PromptParams& p, unsigned char* sq, PBars* bars, volatile int* abort) {
+__device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const PromptParams& p, unsigned char* sq, unsigned char* ring, PBars* bars, volatile int* abort) {
     using C = PCfg<D>;
     const int lane = threadIdx.x & 31;
     PromptPlan plan = p.plan;
     const bool fine = p.batch <= kSelfBatch ? self_plan_prompt(p, bars, &plan) : *p.plan.fatal == 0;
     if (!fine && lane == 0) bars->fatal = 1;
     const long long total = fine ? (long long)plan.pre[p.batch] * p.Hkv : 0;
-    int loads[2] = {0, 0};
-    for (int turn = 0, n = 0;; ++turn) {
-        const long long t = prompt_turn(turn, blockIdx.x, gridDim.x);
-        const bool done = (long long)turn * gridDim.x >= total;
-        if (!done && t >= total) continue;
-        ItemDesc d = {-1, 0, 0, 0, 0, {0, 0}, {0, 0}, 0};
-        if (!done) {
+    int turn = 0, loads[2] = {0, 0}, g = 0, cuts = 0;
+    // the next item, handed out; kv-head -1: there is none
+    auto hand_out = [&](int n, ItemDesc& d) -> bool {
+        long long t = prompt_turn(turn, blockIdx.x, gridDim.x);
+        while (t >= total && (long long)turn * gridDim.x < total) t = prompt_turn(++turn, blockIdx.x, gridDim.x);
+        ++turn;
+        d = {-1, 0, 0, 0, 0, {0, 0}, {0, 0}, 0};
+        if (t < total) {
             const PromptItem it = prompt_item(plan, p.batch, p.Hkv, t);
             const int t0 = it.place * 2 * p.tile_tokens;
             d.kvh = it.kvh;
@@ -164,22 +203,22 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
             for (int s = 0; s < 2; ++s) {
                 const int toks = min(p.tile_tokens, it.Lq - t0 - s * p.tile_tokens);
                 d.rows[s] = max(toks, 0) * p.G;
-                d.tiles[s] = toks > 0 ? (max(d.limit0 + s * p.tile_tokens + toks - 1, 0) + PCfg<D>::kKeys - 1) / PCfg<D>::kKeys : 0;
+                d.tiles[s] = toks > 0 ? (max(d.limit0 + s * p.tile_tokens + toks - 1, 0) + C::kKeys - 1) / C::kKeys : 0;
             }
         }
-        if (n >= 4 && !wait_all(&bars->desc_empty[n & 3], ((n >> 2) + 1) & 1, abort)) break;
+        if (n >= 4 && !wait_all(&bars->desc_empty[n & 3], ((n >> 2) + 1) & 1, abort)) return false;
         if (lane == 0) {
             bars->desc[n & 3] = d;
             mbar_arrive(&bars->desc_full[n & 3]);  // (release: the waiters read the descriptor behind it)
         }
         __syncwarp();
-        ++n;
-        if (done) break;
-        bool ok = true;
+        return true;
+    };
+    auto load_q = [&](const ItemDesc& d) -> bool {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (d.tiles[s] == 0 || !ok) continue;
-            if (loads[s] > 0 && !wait_all(&bars->q_free[s], (loads[s] - 1) & 1, abort)) { ok = false; continue; }
+            if (d.tiles[s] == 0) continue;
+            if (loads[s] > 0 && !wait_all(&bars->q_free[s], (loads[s] - 1) & 1, abort)) return false;
             if (lane == 0) {
                 mbar_arrive_expect_tx(&bars->q_full[s], p.tile_tokens * p.G * 128 * C::kHalves);
 #pragma unroll
@@ -189,7 +228,26 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
             __syncwarp();
             ++loads[s];
         }
-        if (!ok) break;
+        return true;
+    };
+    ItemDesc d, next;
+    bool ok = hand_out(0, d) && load_q(d);
+    for (int n = 0; ok && d.kvh >= 0; ++n) {
+        if (!hand_out(n + 1, next)) break;  // the loads run ahead into it
+        // a bit of `odd` is used again 32 items on; the roles are at most the four items of the descriptor ring apart
+        if (lane < 2) atomicAnd(&bars->odd[lane], ~(1u << ((n + 16) & 31)));
+        const int nt = max(d.tiles[0], d.tiles[1]);
+        for (int j = max(min(d.limit0, d.Lk) / C::kKeys, 0); ok && j < nt; ++j) {
+            const int k = g + 2 * j + 1, st = k % C::kStages;
+            ok = wait_all(&bars->cut_full[cuts & 7], (cuts >> 3) & 1, abort);
+            if (!ok) break;
+            clean_tile<D>(ring + st * C::kTileBytes, max(min(d.limit0 - j * C::kKeys, C::kKeys), 0), d.Lk - j * C::kKeys, bars, n);
+            if (lane == 0) mbar_arrive(&bars->full[st]);
+            ++cuts;
+        }
+        g += 2 * nt;
+        ok = ok && load_q(next);
+        d = next;
     }
     if (*abort)  // drain the copies in flight before the shared memory is given back
         for (int s = 0; s < 2; ++s)
@@ -204,7 +262,7 @@ template <int D>
 __device__ __forceinline__ void prompt_load_role(const CUtensorMap& kmap, const CUtensorMap& vmap, unsigned char* ring, PBars* bars, volatile int* abort) {
     using C = PCfg<D>;
     const int lane = threadIdx.x & 31;
-    int i = 0;  // tiles pushed
+    int i = 0, cuts = 0;  // tiles pushed, V tiles among them that are looked through
     ItemDesc d;
     bool ok = true;
     for (int n = 0; ok && next_item(bars, n, d, abort); ++n) {
@@ -212,55 +270,27 @@ __device__ __forceinline__ void prompt_load_role(const CUtensorMap& kmap, const 
         for (int j = 0; j < 2 * nt; ++j, ++i) {
             const int st = i % C::kStages;
             if (!wait_all(&bars->empty[st], ((i / C::kStages) & 1) ^ 1, abort)) { ok = false; break; }
+            const bool cut = (j & 1) && is_cut<D>(d, j >> 1);
+            uint64_t* bar = cut ? &bars->cut_full[cuts & 7] : &bars->full[st];
             if (lane == 0) {
-                mbar_arrive_expect_tx(&bars->full[st], C::kTileBytes);
+                mbar_arrive_expect_tx(bar, C::kTileBytes);
 #pragma unroll
                 for (int h = 0; h < C::kHalves; ++h)
-                    tma_load_3d(ring + st * C::kTileBytes + h * C::kHalfBytes, (j & 1) ? &vmap : &kmap, h * 64, d.kvh, d.kv0 + (j >> 1) * C::kKeys,
-                                &bars->full[st]);
+                    tma_load_3d(ring + st * C::kTileBytes + h * C::kHalfBytes, (j & 1) ? &vmap : &kmap, h * 64, d.kvh, d.kv0 + (j >> 1) * C::kKeys, bar);
             }
             __syncwarp();
+            cuts += cut;
         }
     }
-    if (*abort)
-        for (int k = max(0, i - C::kStages); k < i; ++k) {
-            const unsigned long long t0 = global_ns();
+    if (*abort) {  // copies still in flight: those of the ring's stages, on either kind of barrier
+        const unsigned long long t0 = global_ns();
+        for (int k = max(0, cuts - 8); k < cuts; ++k)
+            for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
+                if (mbar_try_wait(&bars->cut_full[k & 7], (k >> 3) & 1)) break;
+        for (int k = max(0, i - C::kStages); k < i; ++k)  // (a stage whose tile nobody has looked through stays open: the limit ends it)
             for (uint32_t it = 0; it < kSpinLimit && global_ns() - t0 < kWaitLimitNs; ++it)
                 if (mbar_try_wait(&bars->full[k % C::kStages], (k / C::kStages) & 1)) break;
-        }
-}
-
-// Values of a V tile that are not finite, rows [lo, hi): found, reported to both streams, and replaced by zeros.  One warp.  (Both streams'
-// warps do so before their own product; whichever comes second may find zeros already, and the report.)
-template <int D>
-__device__ __forceinline__ void take_out_odd(unsigned char* vt, int lo, int hi, PBars* bars, int item) {
-    using C = PCfg<D>;
-    const int lane = threadIdx.x & 31;
-    auto at = [&](int e) -> uint4* {
-        const int r = lo + e / (8 * C::kHalves), w = e % (8 * C::kHalves);
-        return reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16);
-    };
-    const int n = (hi - lo) * 8 * C::kHalves;
-    // bits 15 and 31: the element's exponent is all ones (its magnitude carries past 0x7f80)
-    auto odd = [](uint32_t x) { return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; };
-    uint32_t any = 0;
-#pragma unroll 8
-    for (int e = lane; e < n; e += 32) {
-        const uint4 x = *at(e);
-        any |= odd(x.x) | odd(x.y) | odd(x.z) | odd(x.w);
     }
-    if (!__any_sync(0xffffffffu, any != 0)) return;
-    if (lane < 2) atomicOr(&bars->odd[lane], 1u << (item & 31));
-    __threadfence_block();
-    __syncwarp();
-    auto keep = [&](uint32_t x) { const uint32_t o = odd(x) >> 15; return x & ~(o * 0xffffu); };
-#pragma unroll 1
-    for (int e = lane; e < n; e += 32) {
-        uint4 x = *at(e);
-        *at(e) = make_uint4(keep(x.x), keep(x.y), keep(x.z), keep(x.w));
-    }
-    fence_proxy_async_smem();
-    __syncwarp();
 }
 
 template <int D>
@@ -274,8 +304,6 @@ __device__ __forceinline__ void prompt_mma_role(int s, unsigned char* sq, unsign
     ItemDesc d;
     for (int n = 0; next_item(bars, n, d, abort); ++n) {
         const int mine = d.tiles[s], nt = max(d.tiles[0], d.tiles[1]);
-        // a bit of `odd` is used again 32 items on; the roles are at most the four items of the descriptor ring apart
-        if (lane == 0) atomicAnd(&bars->odd[s], ~(1u << ((n + 16) & 31)));
         auto issue_qk = [&](int j) -> bool {
             const int k = g + 2 * j, st = k % C::kStages;
             if (!wait_all(&bars->full[st], (k / C::kStages) & 1, abort)) return false;
@@ -299,16 +327,6 @@ __device__ __forceinline__ void prompt_mma_role(int s, unsigned char* sq, unsign
             const int k = g + 2 * j + 1, st = k % C::kStages;
             if (!wait_all(&bars->full[st], (k / C::kStages) & 1, abort)) return false;
             unsigned char* vt = ring + st * C::kTileBytes;
-            const int key0 = j * C::kKeys, valid = min(C::kKeys, d.Lk - key0);
-            if (valid < C::kKeys) {  // rows behind the sequence's last key are another's
-                for (int e = lane; e < (C::kKeys - valid) * 8 * C::kHalves; e += 32) {
-                    const int r = valid + e / (8 * C::kHalves), w = e % (8 * C::kHalves);
-                    *reinterpret_cast<uint4*>(vt + (w >> 3) * C::kHalfBytes + r * 128 + (w & 7) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-            }
-            if (key0 + valid > d.limit0) take_out_odd<D>(vt, max(d.limit0 - key0, 0), valid, bars, n);
             // the first product of an item overwrites O: the epilogue of the item before must have read it
             if (j == 0 && loads > 0 && !wait_all(&bars->o_free[s], (loads - 1) & 1, abort)) return false;
             const uint64_t vd = make_smem_desc(smem_u32(vt), C::kHalfBytes, 1024);
@@ -543,6 +561,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
             mbar_init(&bars->pv_done[s], 1);
             mbar_init(&bars->o_free[s], 4);
         }
+        for (int i = 0; i < 8; ++i) mbar_init(&bars->cut_full[i], 1);
         for (int i = 0; i < 4; ++i) { mbar_init(&bars->desc_full[i], 1); mbar_init(&bars->desc_empty[i], 11); }  // 8 softmax, 2 MMA, 1 load warps
         bars->abort = 0;
         bars->odd[0] = bars->odd[1] = 0;
@@ -562,7 +581,7 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(56));
         if (warp == 8) prompt_load_role<D>(kmap, vmap, ring, bars, abort);
-        else if (warp == 11) prompt_q_role<D>(qmap, p, sq, bars, abort);
+        else if (warp == 11) prompt_q_role<D>(qmap, p, sq, ring, bars, abort);
         else prompt_mma_role<D>(warp - 9, sq, ring, bars, tmem, abort);
     }
     if (*abort && tid == 0) atomicOr(p.status, FD_DEV_TIMEOUT);
