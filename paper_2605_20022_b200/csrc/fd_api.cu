@@ -40,6 +40,8 @@ struct fd_ctx {
     int* cp_failed;              // compaction
     fd::FreeScratch* fr_scratch; // free
     fd::PromptPlan prompt;       // work list of the prompt attention
+    fd::PromptSplit* split;      // ... and how its items were shared
+    fd::PromptSplitItem* split_items;
     int* status;
     int max_rows;      // capacity of keys
     int max_rb;        // capacity of the row-block arrays of the plan
@@ -225,6 +227,8 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     const size_t o_cpf = take(sizeof(int));
     const size_t o_frs = take(sizeof(fd::FreeScratch));
     const size_t o_pp = take((5 * (size_t)B + 4) * sizeof(int));
+    const size_t o_spl = take(sizeof(fd::PromptSplit));
+    const size_t o_spi = take((size_t)c->n_ctas * sizeof(fd::PromptSplitItem));
     const size_t o_stat = take(sizeof(int));
     if (cudaMalloc(&c->pool, off) != cudaSuccess) { cudaGetLastError(); delete c; return FD_ERR_WORKSPACE; }
     if (cudaMemset(c->pool, 0, off) != cudaSuccess) { cudaFree(c->pool); delete c; return FD_ERR_CUDA; }
@@ -258,6 +262,8 @@ fd_status fd_create(fd_ctx** out, const fd_config* cfg) {
     c->cp_failed = reinterpret_cast<int*>(c->pool + o_cpf);
     c->fr_scratch = reinterpret_cast<fd::FreeScratch*>(c->pool + o_frs);
     int* pp = reinterpret_cast<int*>(c->pool + o_pp);
+    c->split = reinterpret_cast<fd::PromptSplit*>(c->pool + o_spl);
+    c->split_items = reinterpret_cast<fd::PromptSplitItem*>(c->pool + o_spi);
     c->prompt = {pp, pp + B + 1, pp + 2 * B + 2, pp + 3 * B + 2, pp + 4 * B + 2, pp + 5 * B + 3};
     c->status = reinterpret_cast<int*>(c->pool + o_stat);
     *out = c;
@@ -862,7 +868,7 @@ fd_status fd_attn_prompt(fd_ctx* c, int batch, int total_q_rows, int total_kv_ro
     p.q_stride = q_stride; p.kv_stride = kv_stride;
     p.q_lens = q_lens; p.kv_lens = kv_lens;
     p.out = static_cast<__nv_bfloat16*>(out);
-    p.plan = c->prompt; p.n_ctas = c->n_ctas; p.status = c->status;
+    p.plan = c->prompt; p.part = c->part; p.split = c->split; p.split_items = c->split_items; p.n_ctas = c->n_ctas; p.status = c->status;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;
     if (tc && fd::prompt_tc_prepare(&c->prompt_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
@@ -871,8 +877,9 @@ fd_status fd_attn_prompt(fd_ctx* c, int batch, int total_q_rows, int total_kv_ro
         c->launches += 1;
     }
     if (tc) {
-        if (fd::launch_prompt_tc(c->prompt_state, p, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
-        c->launches += 1;
+        int launched = 0;
+        if (fd::launch_prompt_tc(c->prompt_state, p, &launched, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
+        c->launches += launched;
     } else if (total_q_rows > 0) {  // (no rows: the plan alone checks the lengths)
         fd::launch_prompt_simt(p, s);
         c->launches += 1;

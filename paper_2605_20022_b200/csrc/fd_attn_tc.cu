@@ -109,20 +109,16 @@ __device__ __forceinline__ bool pv_by_group(int range_tiles) { return MODE != kT
 #define FD_STAGGER 1
 #endif
 
-// FP8: warps that widen V.  Four leave the softmax warps 176 registers; at d = 64, where the products of a tile take half the time,
-// four are not enough.  Measured, four / eight: 32k prefix, batch 16, d = 128 309 / 330 us; 4 sequences with 17 branches, d = 64 100 / 77.
-__host__ __device__ constexpr int widen_warps8(int d) { return d == 128 ? 4 : 8; }
-
 template <int D, int MODE, int FMT>
 struct Cfg {
     // the warps behind warp 11 widen the tiles: K and V (FP4), or V alone (FP8)
-    static constexpr int kWidenWarps = FMT == FD_KV_FP4 ? 8 : FMT == FD_KV_FP8 ? widen_warps8(D) : 0;
+    static constexpr int kWidenWarps = wide(FMT) ? 8 : 0;
     static constexpr int kThreads = 384 + 32 * kWidenWarps;
     // Registers per thread of the softmax warps, of warps 8-11 and of the widening warps.  What the groups take adds up to no more
     // than what the launch allocates: configure_kernel compares the two before the kernel's first launch.
-    static constexpr int kRegSoftmax = FMT == FD_KV_FP4 ? 144 : FMT == FD_KV_FP8 ? (kWidenWarps == 4 ? 176 : 144) : 224;
-    static constexpr int kRegHelper = FMT == FD_KV_FP4 ? 48 : FMT == FD_KV_FP8 ? (kWidenWarps == 4 ? 72 : 64) : 56;
-    static constexpr int kRegWiden = kWidenWarps == 4 ? 88 : 64;
+    static constexpr int kRegSoftmax = wide(FMT) ? 144 : 224;
+    static constexpr int kRegHelper = FMT == FD_KV_FP8 ? 64 : wide(FMT) ? 48 : 56;
+    static constexpr int kRegWiden = 64;
     static constexpr int kRegTotal = 256 * kRegSoftmax + 128 * kRegHelper + 32 * kWidenWarps * kRegWiden;
     static_assert(kRegTotal <= 65536, "register split");
     // buffers in the K ring, and again in the V ring (wide formats: of widened tiles, fed from the raw ring)
@@ -474,7 +470,7 @@ __device__ __forceinline__ void widen_tile(const RawWords<D>& in, unsigned char*
 // 128-byte line, and that of the widened ones their units 2 c + k ^ x as well.  d = 64: two rows of four chunks.
 template <int D>
 struct V8Map {
-    static constexpr int kTokens = 32 * widen_warps8(D) / (D / 16);  // of a pass
+    static constexpr int kTokens = kWidenThreads / (D / 16);  // of a pass
     static constexpr int kPasses = kTileTokens / kTokens;
     int tok, c;
     __device__ __forceinline__ V8Map() {
@@ -542,7 +538,7 @@ __device__ __forceinline__ void widen_v8(RawV8<D>& in, const float* v_scales, un
 template <int D>
 __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, float scale_log2e, int rows, uint64_t* q_read, uint32_t parity,
                                           volatile int* abort) {
-    constexpr int kLanes = D / 16, kRows = 32 * widen_warps8(D) / kLanes, kPasses = kMaxRows / kRows;
+    constexpr int kLanes = D / 16, kRows = kWidenThreads / kLanes, kPasses = kMaxRows / kRows;
     const int t = (int)threadIdx.x - 384, c = t % kLanes;
     uint4 v[D == 64 ? kPasses : 1][2];
     auto read = [&](int n, uint4 (&x)[2]) {

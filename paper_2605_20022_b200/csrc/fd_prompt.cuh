@@ -63,6 +63,14 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptPlan& pl, int B, i
 // The i-th item of CTA c of n, or at or beyond the total when it has no more.
 __device__ __forceinline__ long long prompt_turn(int i, int c, int n) { return (long long)i * n + ((i & 1) ? n - 1 - c : c); }
 
+// What the merge of shared items needs to know.
+struct PromptSplit {
+    int parts, items;
+};
+struct PromptSplitItem {
+    int row0, kvh, rows[2];
+};
+
 struct PromptParams {
     int batch, total_q, total_kv;
     int Hq, Hkv, G, d, tile_tokens;  // tokens of a row tile: kMaxRows / G
@@ -73,6 +81,9 @@ struct PromptParams {
     const int32_t* kv_lens;          // nullptr: the same as q_lens
     __nv_bfloat16* out;
     PromptPlan plan;
+    PartialView part;                // [2 n_ctas] slots: what a CTA computes of an item that several share
+    PromptSplit* split;              // how the items were shared, or nullptr: none can be
+    PromptSplitItem* split_items;    // [n_ctas / 2]
     int n_ctas;
     int* status;
 };
@@ -82,7 +93,7 @@ cudaError_t prompt_simt_prepare(int d);
 void launch_prompt_simt(const PromptParams& p, cudaStream_t s);
 cudaError_t prompt_tc_prepare(void** state, const PromptParams& p);
 bool prompt_tc_plans_itself(int batch);  // (then the plan kernel is not needed)
-cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s);
+cudaError_t launch_prompt_tc(void* state, const PromptParams& p, int* launched, cudaStream_t s);  // *launched: kernels
 void prompt_tc_free(void* state);
 
 }  // namespace fd

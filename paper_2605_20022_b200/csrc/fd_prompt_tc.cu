@@ -18,6 +18,11 @@
 // item a warp looks for values that are not finite among the keys some row must not see, puts zeros in their place, and the
 // epilogue adds what each row does see of them.
 //
+// A call of few items (a short chunk behind a long prefix: 8 items for one of 64 tokens at 8 kv-heads) is split along the keys: `parts`
+// CTAs share an item, each takes an equal share of its tiles and leaves (m, l, O) in scratch memory, which a second kernel combines in
+// the order of the parts.  (Combined by the last CTA to deliver, one SM read what all had written, 50 us, and the
+// code for it cost the softmax warps registers: 5 % on every other call.)
+//
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
 // given back, FD_DEV_TIMEOUT is set.
 #include <cuda.h>
@@ -61,14 +66,15 @@ struct PCfg {
     static_assert(kHalfBytes % 1024 == 0 && kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 };
 
-// What the roles know of an item.
+// What the roles know of an item.  Keys are counted from the first one of this CTA's part.
 struct ItemDesc {
     int kvh, row0, kv0, Lk;  // row0: the first output row of tile 0; kv-head -1: no more items
     int limit0;              // keys that token 0 of tile 0 sees
     int rows[2];             // query rows of the two tiles
     int tiles[2];            // key tiles they see
-    int pad;
+    int parts, pad;          // CTAs that share the item
 };
+constexpr int kMaxParts = 16, kMinPartTiles = 4;  // (a part of fewer tiles is not worth its share of the merge)
 
 struct PBars {
     uint64_t full[10], empty[10];
@@ -184,13 +190,22 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
     const bool fine = p.batch <= kSelfBatch ? self_plan_prompt(p, bars, &plan) : *p.plan.fatal == 0;
     if (!fine && lane == 0) bars->fatal = 1;
     const long long total = fine ? (long long)plan.pre[p.batch] * p.Hkv : 0;
-    int turn = 0, loads[2] = {0, 0}, g = 0, cuts = 0;
+    int turn = 0, loads[2] = {0, 0}, g = 0, cuts = 0, parts = 1;
+    if (p.split && total > 0 && 2 * total <= gridDim.x) {  // (then at most that many sequences have items, the first in the plan's order)
+        int longest = 0;
+        for (int i = lane; i < min(p.batch, 1024); i += 32)
+            if (plan.blocks[i] > 0) longest = max(longest, plan.cu_kv[plan.perm[i] + 1] - plan.cu_kv[plan.perm[i]]);
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        const float tiles = (float)longest / C::kKeys;
+        parts = max(1, min(min((int)(gridDim.x / total), (int)(tiles / kMinPartTiles)), kMaxParts));
+    }
+    if (p.split && blockIdx.x == 0 && lane == 0) *p.split = {parts, (int)total};
     // the next item, handed out; kv-head -1: there is none
     auto hand_out = [&](int n, ItemDesc& d) -> bool {
-        long long t = prompt_turn(turn, blockIdx.x, gridDim.x);
-        while (t >= total && (long long)turn * gridDim.x < total) t = prompt_turn(++turn, blockIdx.x, gridDim.x);
+        long long t = parts > 1 ? (turn ? total : blockIdx.x / parts) : prompt_turn(turn, blockIdx.x, gridDim.x);
+        while (parts == 1 && t >= total && (long long)turn * gridDim.x < total) t = prompt_turn(++turn, blockIdx.x, gridDim.x);
         ++turn;
-        d = {-1, 0, 0, 0, 0, {0, 0}, {0, 0}, 0};
+        d = {-1, 0, 0, 0, 0, {0, 0}, {0, 0}, 1, 0};
         if (t < total) {
             const PromptItem it = prompt_item(plan, p.batch, p.Hkv, t);
             const int t0 = it.place * 2 * p.tile_tokens;
@@ -204,6 +219,17 @@ __device__ __forceinline__ void prompt_q_role(const CUtensorMap& qmap, const Pro
                 const int toks = min(p.tile_tokens, it.Lq - t0 - s * p.tile_tokens);
                 d.rows[s] = max(toks, 0) * p.G;
                 d.tiles[s] = toks > 0 ? (max(d.limit0 + s * p.tile_tokens + toks - 1, 0) + C::kKeys - 1) / C::kKeys : 0;
+            }
+            if (parts > 1) {  // this CTA's tiles [lo, hi)
+                const int nt = max(d.tiles[0], d.tiles[1]), part = blockIdx.x % parts;
+                const int lo = (int)((long long)nt * part / parts), hi = (int)((long long)nt * (part + 1) / parts);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) d.tiles[s] = max(min(d.tiles[s], hi) - lo, 0);
+                d.kv0 += lo * C::kKeys;
+                d.Lk -= lo * C::kKeys;
+                d.limit0 -= lo * C::kKeys;
+                d.parts = parts;
+                if (part == 0 && lane == 0) p.split_items[t] = {d.row0, d.kvh, {d.rows[0], d.rows[1]}};
             }
         }
         if (n >= 4 && !wait_all(&bars->desc_empty[n & 3], ((n >> 2) + 1) & 1, abort)) return false;
@@ -438,14 +464,40 @@ __device__ __forceinline__ bool prompt_softmax_tile(uint32_t s_addr, uint32_t p_
 
 // What a row of the item sees of the values that were taken out of its tiles goes into its output, which stands in `dst` without them.
 // (Their weights are positive: an infinity or a NaN of them is the sum's, whatever the rest.)
-__device__ __forceinline__ void add_odd(const PromptParams& p, const ItemDesc& d, int limit, int D, __nv_bfloat16* dst) {
-    for (int c = 0; c < D; ++c) {
-        float x = 0.f;
-        for (int j = max(d.limit0, 0); j < limit; ++j) {
-            const float v = __bfloat162float(p.v[((long long)d.kv0 + j) * p.kv_stride + (long long)d.kvh * D + c]);
-            if (!(fabsf(v) <= 3.4028234e38f)) x += v;
-        }
-        if (x != 0.f) dst[c] = __float2bfloat16(__bfloat162float(dst[c]) + x);
+__device__ __forceinline__ float odd_sum(const PromptParams& p, const ItemDesc& d, int limit, int D, int c) {
+    float x = 0.f;
+    for (int j = max(d.limit0, 0); j < limit; ++j) {
+        const float v = __bfloat162float(p.v[((long long)d.kv0 + j) * p.kv_stride + (long long)d.kvh * D + c]);
+        if (!(fabsf(v) <= 3.4028234e38f)) x += v;
+    }
+    return x;
+}
+
+// A warp's rows of an item that several CTAs share: this CTA's part to scratch memory, for the merge kernel behind this one.  (m = -inf,
+// l = 0: no key of the part is seen.)
+template <int D>
+__device__ __forceinline__ void deliver_part(const PromptParams& p, const ItemDesc& d, int s, int warp, bool live, bool odd, int limit, bool have, uint32_t o_addr,
+                                             float m, float l) {
+    const int r = warp * 32 + (threadIdx.x & 31), slot = 2 * blockIdx.x + s;
+    float4* mine = partial_o4(p.part, D, slot, 0, r);
+#pragma unroll 1
+    for (int ch = 0; ch < D / 16 && have; ++ch) {
+        uint32_t raw[16];
+        tmem_ld16(o_addr + ch * 16, raw);
+        tc_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; k += 4)
+            if (live)
+                mine[(ch * 4 + (k >> 2)) * kMaxRows] =
+                    make_float4(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1]), __uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3]));
+    }
+    if (!live) return;
+    const bool sees = have && limit > 0;
+    p.part.m[slot * kMaxRows + r] = sees ? m : -INFINITY;
+    p.part.l[slot * kMaxRows + r] = sees ? l : 0.f;
+    for (int c = 0; c < D && odd; ++c) {
+        float* o = reinterpret_cast<float*>(mine + (c >> 2) * kMaxRows) + (c & 3);
+        *o += odd_sum(p, d, limit, D, c);
     }
 }
 
@@ -496,6 +548,13 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
             if (!wait_all(&bars->pv_done[s], (u - 1) & 1, abort)) return;
             tc_fence_after();
         }
+        const bool odd = (*static_cast<volatile unsigned*>(&bars->odd[s]) >> (n & 31) & 1u) != 0;
+        const int odd_limit = min(limit, nt * C::kKeys);
+        if (d.parts > 1) {  // (the CTA's only item)
+            if (warp_live)
+                deliver_part<D>(p, d, s, warp, live, odd, odd_limit, nt > 0, o_addr, m, l);
+            continue;
+        }
         const float inv = limit > 0 ? 1.f / l : 0.f;
 #pragma unroll
         for (int ch = 0; ch < D / 32; ++ch) {
@@ -528,9 +587,13 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
                 if (warp * 32 + row < rows) *reinterpret_cast<uint4*>(base + off[i] + ch * 32) = v;
             }
         }
-        if (*static_cast<volatile unsigned*>(&bars->odd[s]) >> (n & 31) & 1u) {
+        if (odd) {
             __syncwarp();
-            if (live) add_odd(p, d, limit, D, base + ((long long)tok * p.Hq + r % G) * D);
+            __nv_bfloat16* dst = base + ((long long)tok * p.Hq + r % G) * D;
+            for (int c = 0; c < D && live; ++c) {
+                const float x = odd_sum(p, d, odd_limit, D, c);
+                if (x != 0.f) dst[c] = __float2bfloat16(__bfloat162float(dst[c]) + x);
+            }
         }
     }
 }
@@ -595,6 +658,53 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     }
 }
 
+// The parts of shared items combined: a block per (item, row tile) and 16 columns, a thread a row, the loads of four parts in flight.
+template <int D>
+__global__ void __launch_bounds__(kMaxRows) prompt_merge_kernel(const PromptParams p) {
+    const PromptSplit sp = *p.split;
+    const int item = blockIdx.x >> 1, s = blockIdx.x & 1, r = threadIdx.x, col = blockIdx.y * 16;
+    if (sp.parts <= 1 || item >= sp.items) return;
+    const PromptSplitItem it = p.split_items[item];
+    if (r >= it.rows[s]) return;
+    const int first = 2 * item * sp.parts + s;  // the parts' slots: every other one from here
+    float top = -INFINITY, sum = 0.f, acc[16], m[kMaxParts];
+#pragma unroll
+    for (int q = 0; q < kMaxParts; ++q) m[q] = q < sp.parts ? p.part.m[(first + 2 * q) * kMaxRows + r] : -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kMaxParts; ++q) top = fmaxf(top, m[q]);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+#pragma unroll
+    for (int q0 = 0; q0 < kMaxParts; q0 += 4) {
+        if (q0 >= sp.parts) break;
+        float4 v[4][4];
+        float l[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int from = first + 2 * min(q0 + q, sp.parts - 1);
+            l[q] = p.part.l[from * kMaxRows + r];
+            const float4* o = partial_o4(p.part, D, from, col, r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[q][k] = o[k * kMaxRows];
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (m[q0 + q] == -INFINITY) continue;  // (by selection: what stands there counts nothing)
+            const float w = exp2f(m[q0 + q] - top);
+            sum += w * l[q];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc[4 * k] += w * v[q][k].x;
+                acc[4 * k + 1] += w * v[q][k].y;
+                acc[4 * k + 2] += w * v[q][k].z;
+                acc[4 * k + 3] += w * v[q][k].w;
+            }
+        }
+    }
+    const int tok = s * p.tile_tokens + r / p.G;
+    store_cols_bf16<16>(p.out + (((long long)it.row0 + tok) * p.Hq + it.kvh * p.G + r % p.G) * D + col, acc, top == -INFINITY ? 0.f : 1.f / sum);
+}
+
 // Tensor maps already encoded, by what they were made from.
 struct PromptMap {
     const void* ptr;
@@ -647,7 +757,7 @@ cudaError_t prompt_tc_prepare(void** state, const PromptParams& p) {
 
 bool prompt_tc_plans_itself(int batch) { return batch <= kSelfBatch; }
 
-cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s) {
+cudaError_t launch_prompt_tc(void* state, const PromptParams& p, int* launched, cudaStream_t s) {
     PromptState* st = static_cast<PromptState*>(state);
     CUtensorMap q, k, v;
     // (no keys at all: no item loads any, but a map has to name some memory)
@@ -657,8 +767,21 @@ cudaError_t launch_prompt_tc(void* state, const PromptParams& p, cudaStream_t s)
         !find_map(st, kp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &k) ||
         !find_map(st, vp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &v))
         return cudaErrorInvalidValue;
-    if (p.d == 64) prompt_tc_kernel<64><<<p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s>>>(q, k, v, p);
-    else prompt_tc_kernel<128><<<p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s>>>(q, k, v, p);
+    // The lengths are on the device.  From the totals: there are at least total_q / (2 tile_tokens) blocks, and sharing begins at 2
+    // kMinPartTiles tiles; where that leaves it possible, the merge follows, and finds out.
+    PromptParams a = p;
+    const long long blocks = (p.total_q + 2LL * p.tile_tokens - 1) / (2 * p.tile_tokens);
+    const bool may_split = 2 * blocks * p.Hkv <= p.n_ctas && p.total_kv >= 2 * kMinPartTiles * PCfg<128>::kKeys;
+    if (!may_split) a.split = nullptr;
+    if (p.d == 64) prompt_tc_kernel<64><<<p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s>>>(q, k, v, a);
+    else prompt_tc_kernel<128><<<p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s>>>(q, k, v, a);
+    *launched = 1;
+    if (may_split) {
+        const dim3 grid(p.n_ctas / 2 * 2, p.d / 16);
+        if (p.d == 64) prompt_merge_kernel<64><<<grid, kMaxRows, 0, s>>>(a);
+        else prompt_merge_kernel<128><<<grid, kMaxRows, 0, s>>>(a);
+        *launched = 2;
+    }
     return cudaSuccess;
 }
 

@@ -32,6 +32,14 @@ CASES = {
     "chunks behind earlier keys, 64": (16, 4, 64, [130, 1, 70], [131, 4000, 513]),
     "rows without a key": (8, 2, 128, [10, 40, 300, 3, 70], [4, 0, 130, 3, 1]),
     "no key at all": (4, 1, 128, [10, 40], [0, 0]),
+    # few items: several CTAs share one along the keys
+    "one row behind many keys": (8, 2, 128, [1], [5000]),
+    "short chunks behind long prefixes": (32, 8, 128, [64, 3], [9000, 2000]),
+    "short chunks behind long prefixes, 64": (16, 2, 64, [17, 1, 0, 40], [3000, 700, 5, 100]),
+    "a shared item with rows that see no key": (4, 1, 128, [300, 7], [40, 4000]),
+    "a shared item, both tiles, one head": (1, 1, 128, [200], [6400]),
+    "a shared item among 40 sequences": (2, 1, 64, [3 if b == 7 else 0 for b in range(40)], [4000 if b == 7 else 5 * (b % 3) for b in range(40)]),
+    "as many parts as there may be": (4, 1, 64, [33], [20000]),
     "many short": (8, 2, 64, [(5 * b) % 9 for b in range(300)], None),
     "a long one among short ones": (32, 8, 128, [3, 2500, 17, 1, 900, 40], None),
     "more items than SMs": (32, 8, 128, [2100, 1700], None),
@@ -171,6 +179,33 @@ def test_what_a_sequence_must_not_see(d, path):
         v3[253 + 160, 1, 0], v3[253 + 170, 1, 0] = float("inf"), -float("inf")
         got = _call(ctx, q, k, v3, ql, None)[253:553, 4:, 0].float()
         assert torch.isfinite(got[:160]).all() and (got[160:170] == float("inf")).all() and torch.isnan(got[170:]).all()
+        assert fd.fd_last_device_status(ctx) == 0
+    finally:
+        fd.fd_destroy(ctx)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_not_finite_in_a_shared_item(d):
+    """One item split along the keys: what is not finite in a part every row sees, in the part the mask cuts, and in another sequence."""
+    Lq, Lk, Hq, Hkv = 60, 5000, 4, 1
+    g = torch.Generator(device="cuda").manual_seed(d)
+    q = torch.randn((Lq + 3, Hq, d), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((Lk + 3, Hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k[Lk:], v[Lk:] = float("nan"), float("inf")
+    ctx = _ctx(Hq, Hkv, d, 2)
+    try:
+        clean = _call(ctx, q, k, v, [Lq, 3], [Lk, 3])[:Lq]
+        for at, value in ((0, float("inf")), (2000, float("nan")), (Lk - Lq, float("inf")), (Lk - Lq + 1, -float("inf")), (Lk - 20, float("nan")), (Lk - 1, float("inf"))):
+            v3 = v.clone()
+            v3[at, 0, 5] = value
+            got = _call(ctx, q, k, v3, [Lq, 3], [Lk, 3])[:Lq]
+            row = max(0, at - (Lk - Lq))                        # the first row that sees it
+            assert torch.equal(got[:row].view(torch.int16), clean[:row].view(torch.int16))
+            kept = torch.ones(d, dtype=torch.bool)
+            kept[5] = False
+            assert torch.equal(got[..., kept], clean[..., kept])
+            behind = got[row:, :, 5].float()
+            assert torch.isnan(behind).all() if value != value else (behind == value).all()
         assert fd.fd_last_device_status(ctx) == 0
     finally:
         fd.fd_destroy(ctx)
