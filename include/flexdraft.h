@@ -452,8 +452,11 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, con
  *
  * fd_attn_draft_verify_fp8 is fd_attn_draft_verify_blocks for it: same arguments (n_blocks may be NULL), same mask, same
  * errors, same forms (FD_TC_*), pinned plans and overlap of consecutive attention calls included.  Slots no valid token owns may
- * hold any bit pattern.  Arithmetic: the values of the cache enter exactly, q and the softmax weights as in
- * fd_attn_draft_verify_fp4, sums in fp32; bf16 output.
+ * hold any bit pattern.  Arithmetic: the values of the cache enter exactly, elements of q exactly down to 2^-9 of their row's
+ * largest (below that to within 2^-17 of it), the softmax weights as in fd_attn_draft_verify_fp4, sums in fp32; bf16 output.
+ * When to choose it: it holds twice the tokens in the same memory at four significant bits.  Its attention is faster than the bf16
+ * cache's on long prefixes (32k, batch 16: 320 us against 350), slower on small ones (64 sequences of 1k to 4k: 133 us against
+ * 116; 8 sequences: 49 against 38; one: 13 against 11).
  */
 fd_status fd_kv_append_fp8(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
                            void* kv_cache, int num_pages, const int32_t* page_table, const int32_t* prefix_lens,
@@ -537,8 +540,7 @@ fd_status fd_attn_prompt(fd_ctx* ctx, int batch, int total_q_rows, int total_kv_
  *   copy_src, copy_dst   device, [max_copies] int32, written, -1 behind the moves;  min(m, n_free) are enough
  *
  * An id listed twice or outside the pool (FD_DEV_BAD_PAGE), a list longer than the pool, more moves than max_copies
- * (FD_DEV_BAD_LENGTHS): tables, list and shared stay, page_map is the identity, n_copies = 0, the copies are unspecified
- * pairs of which none counts.
+ * (FD_DEV_BAD_LENGTHS): tables, list and shared stay, page_map is the identity, n_copies = 0, the copies are -1.
  *
  * fd_kv_copy_pages: page copy_dst[i] of one layer's cache becomes a copy of page copy_src[i], for i < *n_copies (NULL: for
  * i < max_copies).  A pair with a negative id is skipped; one with an id beyond the pool too (FD_DEV_BAD_PAGE).  The copies of a call

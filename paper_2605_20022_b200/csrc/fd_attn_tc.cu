@@ -41,12 +41,13 @@
 // their loops, in-flight TMA copies are drained, TMEM is released and FD_DEV_TIMEOUT is set.
 //
 // 4-bit and 8-bit pages (wide formats).  Same walk, same epilogue and merges; a tile differs in three places.
-//     loads    : codes and scales of a page come by untiled bulk copies into a raw ring: in 4 bits K and V of a page, which lie side
-//                by side, in one copy, 3.6 times fewer bytes than bf16; in 8 bits a tile's K and its V are stages of their own,
-//                half a tile's bytes each, in the order in which they are widened;
-//     widening : eight warps turn a raw tile into fp16 K and V tiles in the layout the MMAs read.  code * scale is exact in
-//                fp16 in both formats (fd_fp4.cuh, fd_fp8.cuh); k_scale goes into the scale of the scores,
-//                v_scale into the output.  Q is converted to fp16 by the same warps, a row against a power of two of its own;
+//     loads    : codes and scales of a page come into a raw ring, K and V together: in 4 bits, where they lie side by side, by one
+//                untiled bulk copy, 3.6 times fewer bytes than bf16; in 8 bits by one TMA box, the scales by plain loads;
+//     widening : eight warps turn a raw tile into fp16 tiles in the layout the MMAs read.  code * scale is exact in
+//                fp16 in both formats (fd_fp4.cuh, fd_fp8.cuh).  In 4 bits K and V; k_scale goes into the scale of the scores,
+//                v_scale into the output; Q is converted to fp16 by the same warps, a row against a power of two of its own.  In
+//                8 bits V alone: K's codes are an operand of the MMA as they are, against Q as a sum of two e4m3 tiles, and
+//                the softmax multiplies the 16 columns of a page by its scale;
 //     softmax  : P is fp16.  Three S / P buffers and one O; the groups take turns and share the reference of a row.
 // TMEM columns: S / P buffers [0,128) [128,256) [256,384), O [384,384+d).
 //
@@ -63,6 +64,14 @@
 // Measured and dropped, batch 16 on 32k / batch 64, one token each: S^T = K Q^T with K widened into TMEM, no K tile in shared
 // memory, 394 / 95-115 us, but 155-183 us at up to 16 rows; two S buffers and two accumulators, as in the bf16 form, 344 / 159;
 // four widening warps 472 / 190; four for K and four for V, 431 / 187.
+//
+// The 8-bit form (d = 128): batch 16 on 32k 320 us (859 TFLOP/s, 3.4 TB/s of cache; 260 to 318 with every page in L2), batch 64 133.  Half
+// the widening is gone, and what bounds it is the same: hand-overs and, at a piece's ends, code that is not in the instruction
+// cache.  Measured on the way, batch 16 on 32k / batch 64: both widened as in 4 bits, K and V a bulk copy each 464 / 182; K as it is, one box a page
+// 335 / 173; eight widening warps 346 / 144; scales a tile ahead, Q by a rolled loop, one form of the widening 327 / 132.
+// Dropped: four widening warps and 176 registers for the softmax 309 / 146 (d = 64 99 us where eight take 77); two S buffers and two accumulators, the
+// bf16 form's, whose whole row in registers spills at the 176 to 200 there are, 458 / 164; 152 or 160 registers for the softmax
+// 389 / 139 to 142.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -131,7 +140,6 @@ struct Cfg {
     static constexpr int kRawBytes = 8 * kRawPage;           // ... of a tile
     // Behind Q: the K ring -- for FP8 the raw ring, whose K the MMAs read as it is -- then the V ring, then (FP4) the raw ring.
     static constexpr int kVOffset = kQBytes + (FMT == FD_KV_FP8 ? kRawStages * kRawBytes : kStages * kKBytes);
-    static constexpr int kRawOffset = FMT == FD_KV_FP8 ? kQBytes : kVOffset + kStages * kKBytes;
     static constexpr int kBarOffset = kVOffset + kStages * kKBytes + (FMT == FD_KV_FP4 ? kRawStages * kRawBytes : 0);
     static constexpr int kCsOffset = kBarOffset + 320;           // window of the CTA range starts
     static constexpr int kDescOffset = kBarOffset + 448;         // ring of piece descriptors
@@ -141,7 +149,6 @@ struct Cfg {
     static constexpr int kWideOffset = kRbOffset + 1024;         // wide formats: WideShared
     static constexpr int kSmemBytes = kRbOffset + 1024 + (wide(FMT) ? 5120 : 0);  // the dynamic shared memory is declared 1024-byte aligned
     static constexpr int kDescSlots = wide(FMT) ? 8 : 4;  // ring of piece descriptors: see publish_piece
-    static constexpr int kKSteps = D / 16;
     static constexpr int kHalves = D / 64;
     // A K or V tile in shared memory: [8-token group][half of d][8 rows][128 B] -- what one TMA box per page
     // (two groups) lands; for either half the 16 groups lie kGroupBytes apart, the stride the MMA descriptors name.
@@ -334,8 +341,8 @@ __device__ __forceinline__ void load_role_fp4(const AttnParams& p, int n_rb, uns
 }
 
 // FP8 load warp.  One TMA box a page brings the codes of K and V, as [8-token group][K, V][8 rows][d]: the groups of K then lie a
-// fixed stride apart, as those of V do, and K is an operand of Q K^T as it stands.  (Two untiled copies a page, K and V apart, took 464 us
-// where this takes 335: what a copy costs the TMA unit is mostly per copy.)  The scales, 16 bytes behind the codes of either,
+// fixed stride apart, as those of V do, and K is an operand of Q K^T as it stands.  (Two untiled copies a page, K and V apart, took half as
+// long again in all: what a copy costs the TMA unit is mostly per copy.)  The scales, 16 bytes behind the codes of either,
 // come by plain loads, a tile ahead.
 template <int D, int MODE>
 __device__ __forceinline__ void load_role_fp8(const CUtensorMap& tmap, const AttnParams& p, int n_rb, unsigned char* raw, WideShared* f4, const Range rg,
@@ -811,7 +818,7 @@ __device__ __forceinline__ void mma_role(const AttnParams& p, unsigned char* sq,
                     }
                 } else
 #pragma unroll
-                for (int kk = 0; kk < C::kKSteps; ++kk) {
+                for (int kk = 0; kk < D / 16; ++kk) {
                     constexpr int kQHalf = kMaxRows * 128;
                     umma_ss(tmem + s_col, qd0 + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
                             kd0 + (uint64_t)(((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
@@ -1790,7 +1797,7 @@ __global__ void __launch_bounds__(Cfg<D, MODE, FMT>::kThreads, 1) attn_tc_kernel
         }
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegHelper));
         if constexpr (wide(FMT)) {
-            unsigned char* raw = smem + C::kRawOffset;
+            unsigned char* raw = smem + (FMT == FD_KV_FP8 ? C::kQBytes : C::kVOffset + C::kStages * C::kKBytes);
             if (warp == kKWarp) {
                 if constexpr (FMT == FD_KV_FP8) load_role_fp8<D, MODE>(tmap, p, n_rb, raw, f4, rg, &bars->bad, abort);
                 else load_role_fp4<D, MODE>(p, n_rb, raw, f4, rg, &bars->bad, abort);

@@ -20,8 +20,16 @@
 //
 // A call of few items (a short chunk behind a long prefix: 8 items for one of 64 tokens at 8 kv-heads) is split along the keys: `parts`
 // CTAs share an item, each takes an equal share of its tiles and leaves (m, l, O) in scratch memory, which a second kernel combines in
-// the order of the parts.  (Combined by the last CTA to deliver, one SM read what all had written, 50 us, and the
-// code for it cost the softmax warps registers: 5 % on every other call.)
+// the order of the parts: 64 tokens behind 8128 take 25 us, where one CTA an item takes 125.  (Combined by the last CTA to deliver,
+// one SM read what all had written, 54 us, and the code for it cost the softmax warps registers: 3 to 5 % on every other call.)
+//
+// What it reaches (32 heads over 8 of 128): a prompt of 32768 tokens 7.8 to 8.1 ms, 1.03 to 1.08 PFLOP/s where the library's dense product
+// sustains 1.18 to 1.29 on the same machine; 8192 tokens 0.97 to 1.02 PFLOP/s, 2048 0.75, 16 ragged prompts of 1 to 8192 tokens 600
+// to 650 us, 17 tokens 8.4 us.  What bounds it: a tile and stream takes 940 clocks on average where its products take 640; with
+// two streams the tensor pipe waits for the exponentials (half of a scheduler's cycles) and the hand-overs between them; short prompts wait
+// besides for an item's ends (Q's load, the epilogue) that nothing overlaps.
+// Tried and dropped: the streams' exponentials taking turns (no gain); one pass over S against a guessed maximum (spills: 8192 tokens
+// 860 us for 584); tiles of 96 keys at d = 64 (472 us for 406).
 //
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
 // given back, FD_DEV_TIMEOUT is set.
@@ -39,10 +47,10 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kPThreads = 384;
+constexpr int kPThreads = 384, kPRegSoftmax = 224, kPRegHelper = 56;
 constexpr float kPRescale = 8.0f;  // log2 units
 // Calls of at most this many sequences plan for themselves, a lane a sequence: the one warp that hands out items makes the scans and
-// sorts, 0.4 us instead of a launch in front.
+// sorts (17 tokens: 8.4 us; with the plan kernel in front, which larger batches have, 13.8).
 constexpr int kSelfBatch = 32;
 
 template <int D>
@@ -74,7 +82,11 @@ struct ItemDesc {
     int tiles[2];            // key tiles they see
     int parts, pad;          // CTAs that share the item
 };
-constexpr int kMaxParts = 16, kMinPartTiles = 4;  // (a part of fewer tiles is not worth its share of the merge)
+// A part has at least kMinPartTiles tiles (64 tokens behind 936: 18.0 us, with at least four 19.4, unsplit 24.3); 16 parts at most (5
+// tokens behind 14995: 23.6 us, at most eight 32.3).  Calls of fewer keys than kMinSplitTiles tiles hold are never split: the merge
+// kernel is launched where the lengths, which are on the device, might ask for it, and costs 2 us (8 prompts of 40 tokens: 10.4 us
+// without it, 12.4 with).
+constexpr int kMaxParts = 16, kMinPartTiles = 2, kMinSplitTiles = 8;
 
 struct PBars {
     uint64_t full[10], empty[10];
@@ -493,7 +505,8 @@ __device__ __forceinline__ void deliver_part(const PromptParams& p, const ItemDe
     }
     if (!live) return;
     const bool sees = have && limit > 0;
-    p.part.m[slot * kMaxRows + r] = sees ? m : -INFINITY;
+    // (scores that are all NaN or -inf leave m at -inf: the part counts all the same, and the row becomes NaN)
+    p.part.m[slot * kMaxRows + r] = sees ? fmaxf(m, -3.4028234e38f) : -INFINITY;
     p.part.l[slot * kMaxRows + r] = sees ? l : 0.f;
     for (int c = 0; c < D && odd; ++c) {
         float* o = reinterpret_cast<float*>(mine + (c >> 2) * kMaxRows) + (c & 3);
@@ -509,7 +522,7 @@ __device__ __forceinline__ void prompt_softmax_role(int s, const PromptParams& p
     const uint32_t s_addr = tmem + lane_base + C::col_s(s), p_addr = tmem + lane_base + C::col_p(s), o_addr = tmem + lane_base + C::col_o(s);
     const int tok = r / G;
     // Results leave through shared memory, 32 columns at a time: a thread has a row, but four neighbouring lanes write 64 bytes of one
-    // row, eight rows an instruction (a thread's row by itself is a line of memory for every 16 bytes: FIGURE_EPI).
+    // row, eight rows an instruction (a thread's row by itself is a line of memory for every 16 bytes: 5000 clocks an item where this takes 2300).
     unsigned char* stage = out_stage + (threadIdx.x >> 5) * 2048;
     int off[4];  // where the rows that this lane writes start, from the item's first
 #pragma unroll
@@ -638,11 +651,10 @@ __global__ void __launch_bounds__(kPThreads, 1) prompt_tc_kernel(const __grid_co
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
     if (warp < 8) {
-        // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168, what the launch allocated
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(224));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPRegSoftmax));
         prompt_softmax_role<D>(warp >> 2, p, out_stage, bars, tmem, abort);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(56));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPRegHelper));
         if (warp == 8) prompt_load_role<D>(kmap, vmap, ring, bars, abort);
         else if (warp == 11) prompt_q_role<D>(qmap, p, sq, ring, bars, abort);
         else prompt_mma_role<D>(warp - 9, sq, ring, bars, tmem, abort);
@@ -750,6 +762,10 @@ cudaError_t prompt_tc_prepare(void** state, const PromptParams& p) {
     if (e == cudaSuccess)
         e = p.d == 64 ? cudaFuncSetAttribute(prompt_tc_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<64>::kSmemBytes)
                       : cudaFuncSetAttribute(prompt_tc_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<128>::kSmemBytes);
+    // the register split draws on what the launch allocates: a request beyond that would wait for ever
+    cudaFuncAttributes attr = {};
+    if (e == cudaSuccess) e = p.d == 64 ? cudaFuncGetAttributes(&attr, prompt_tc_kernel<64>) : cudaFuncGetAttributes(&attr, prompt_tc_kernel<128>);
+    if (e == cudaSuccess && attr.numRegs * kPThreads < 256 * kPRegSoftmax + 128 * kPRegHelper) e = cudaErrorInvalidConfiguration;
     if (e != cudaSuccess) { delete st; return e; }
     *state = st;
     return cudaSuccess;
@@ -767,11 +783,11 @@ cudaError_t launch_prompt_tc(void* state, const PromptParams& p, int* launched, 
         !find_map(st, kp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &k) ||
         !find_map(st, vp, p.kv_stride, kv_rows, p.Hkv, p.d, 1, p.d == 128 ? PCfg<128>::kKeys : PCfg<64>::kKeys, &v))
         return cudaErrorInvalidValue;
-    // The lengths are on the device.  From the totals: there are at least total_q / (2 tile_tokens) blocks, and sharing begins at 2
-    // kMinPartTiles tiles; where that leaves it possible, the merge follows, and finds out.
+    // The lengths are on the device.  From the totals: there are at least total_q / (2 tile_tokens) blocks; where that leaves sharing
+    // possible, the merge follows, and finds out.
     PromptParams a = p;
     const long long blocks = (p.total_q + 2LL * p.tile_tokens - 1) / (2 * p.tile_tokens);
-    const bool may_split = 2 * blocks * p.Hkv <= p.n_ctas && p.total_kv >= 2 * kMinPartTiles * PCfg<128>::kKeys;
+    const bool may_split = 2 * blocks * p.Hkv <= p.n_ctas && p.total_kv >= kMinSplitTiles * PCfg<128>::kKeys;
     if (!may_split) a.split = nullptr;
     if (p.d == 64) prompt_tc_kernel<64><<<p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s>>>(q, k, v, a);
     else prompt_tc_kernel<128><<<p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s>>>(q, k, v, a);

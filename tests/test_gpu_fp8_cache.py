@@ -1,7 +1,7 @@
 """GPU tests of the 8-bit cache: append and read byte for byte against the 64-bit reference, attention against the oracle.
 
-Attention tolerance: as for the 4-bit cache (test_gpu_serving.py).  The values of the cache and the queries enter exactly; the
-softmax weights are held in at least 11 bits (relative 2^-11) before the product with V, exponentials and fp32 sums add relative
+Attention tolerance: as for the 4-bit cache (test_gpu_serving.py).  The values of the cache enter exactly, and the queries but for
+elements below 2^-9 of their row's largest, which are off by at most 2^-17 of it (here less than 2^-12 of a weight); the softmax weights are held in at least 11 bits (relative 2^-11) before the product with V, exponentials and fp32 sums add relative
 2^-14, the output is rounded to bf16 (2^-8, half a step), and weights below fp16's steps are off by at most 2^-32 of the row's
 largest: |err| <= 2^-8 |ref| + 2^-10 sum_j p_j |v_j| + 2^-32 keys max |v|."""
 import zlib
@@ -258,6 +258,107 @@ def test_attention_scores_that_rise_and_fall_along_the_sequence(Hq, Hkv, d, by, 
         for _ in range(10):
             again, _ = attn_gpu(ctx, step, q, cache)
             assert np.array_equal(got, again), "two runs on the same inputs differ bitwise"
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("size,scale", [(3.0e5, 1e-7), (1e-6, 1e4), (8.0, 0.0), (1e30, 1e-32)])
+def test_attention_queries_of_any_size(path, size, scale):
+    """Queries far outside and far inside an 8-bit type's range: rows of one call differ by factors of a thousand, elements within a row by
+    a hundred."""
+    step = wl.make_step("sizes", wl.Shape(8, 2, 128, 1000), [300, 40, 1000], [12, 32, 5], [4, 16, 0], seed=12)
+    g = torch.Generator().manual_seed(1)
+    q = wl.make_q(step).float() * 10.0 ** torch.randint(-1, 2, (1, 1, 128), generator=g)
+    q = q * size
+    q[3] *= 1e-3
+    q[7, 2] = 0.0
+    q = q.bfloat16()
+    cache = ref.make_cache(wl.make_kv(step))
+    with Ctx(step, path, scale=scale) as ctx:
+        got, status = attn_gpu(ctx, step, q, cache)
+    assert status == 0
+    check(got, attn_ref(step, q, cache, scale=scale or None), "sizes")
+
+
+@pytest.mark.parametrize("pin", [False, True])
+@pytest.mark.parametrize("path", PATHS)
+def test_captured_call_forgets_the_bad_page_of_an_earlier_replay(path, pin):
+    """A page id outside the pool zeroes its sequence in that replay and in no other."""
+    step = wl.make_step("replay", wl.Shape(8, 2, 128, 1000), [300, 700, 40], [8, 8, 8], [4, 4, 4], seed=8)
+    q, cache = wl.make_q(step).cuda(), ref.make_cache(wl.make_kv(step))
+    c, table = torch.from_numpy(cache).cuda(), step.page_table.cuda()
+    ints, nm, out = [table, step.prefix_lens.cuda(), step.q_lens.cuda()], step.n_mask.cuda(), torch.zeros_like(q)
+    with Ctx(step, path) as ctx:
+        call = lambda: fd.fd_attn_draft_verify_fp8(ctx.h, 3, 24, q, c, step.num_pages, *ints, nm, None, out)  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            if pin:
+                fd.fd_plan_pin(ctx.h, 3, 24, ints[1], ints[2], nm)
+            call()
+        for bad in (False, True, False, True, False):
+            table.copy_(step.page_table)
+            if bad:
+                table[1, 20] = step.num_pages
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.double().cpu().numpy()
+            assert fd.fd_last_device_status(ctx.h) == (fd.FD_DEV_BAD_PAGE if bad else 0)
+            exp, tol = attn_ref(step, q.cpu(), cache)
+            if bad:
+                assert (got[8:16] == 0).all()
+                got, exp, tol = np.delete(got, range(8, 16), 0), np.delete(exp, range(8, 16), 0), np.delete(tol, range(8, 16), 0)
+            check(got, (exp, tol), "replay")
+        if pin:
+            fd.fd_plan_unpin(ctx.h)
+
+
+def test_norm_rope_into_rows():
+    """FD_KV_ROWS: the bytes that FD_KV_BF16 puts into pages, as rows; padding and slots beyond the rows; the 8-bit format is refused."""
+    Hq, Hkv, d, T, pages = 8, 2, 128, 37, 4
+    g = torch.Generator().manual_seed(3)
+    qkv = torch.randn((T, (Hq + 2 * Hkv) * d), generator=g).bfloat16().cuda()
+    w = (1 + 0.1 * torch.randn(d, generator=g)).bfloat16().cuda()
+    cos_sin = torch.randn((64, d), generator=g).cuda()
+    pos = torch.randint(0, 64, (T,), generator=g).int().cuda()
+    slot = torch.randperm(pages * 16, generator=g)[:T].int()
+    slot[5] = -1
+    ctx = fd.fd_create(Hq, Hkv, d, 10, 1, 64, 8)
+    try:
+        for style, rot in ((fd.FD_ROPE_HALVES, d), (fd.FD_ROPE_ADJACENT, d), (fd.FD_ROPE_HALVES, 64), (fd.FD_ROPE_HALVES, 0)):
+            q1, q2 = (torch.zeros((T, Hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            paged, rows = torch.zeros((pages, 2, Hkv, 16, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, pages * 16, Hkv, d), dtype=torch.bfloat16, device="cuda")
+            args = [ctx, T, qkv, qkv.stride(0), w, w, 1e-6, cos_sin[:, :max(rot, 1)].contiguous(), 64, rot, style, pos, slot.cuda()]
+            fd.fd_qk_norm_rope_append(*args, q1, paged, pages, fd.FD_KV_BF16)
+            fd.fd_qk_norm_rope_append(*args, q2, rows, pages, fd.FD_KV_ROWS)
+            assert fd.fd_last_device_status(ctx) == 0
+            assert torch.equal(q1, q2) and torch.equal(paged.permute(1, 0, 3, 2, 4).reshape(2, pages * 16, Hkv, d), rows) and (rows != 0).any()
+        beyond = slot.clone()
+        beyond[7] = pages * 16
+        fd.fd_qk_norm_rope_append(*args[:-1], beyond.cuda(), q2, rows, pages, fd.FD_KV_ROWS)
+        assert fd.fd_last_device_status(ctx) == fd.FD_DEV_BAD_PAGE
+        for fmt in (fd.FD_KV_FP8, 4, -1):
+            assert fd.fd_qk_norm_rope_append(*args, q2, rows, pages, fmt, raise_on_error=False) == fd.FD_ERR_INVALID_ARG
+    finally:
+        fd.fd_destroy(ctx)
+
+
+@pytest.mark.parametrize("Hkv,d,rows", [(546, 128, 300), (2961, 64, 40), (4097, 128, 2)])
+def test_append_and_read_of_very_long_rows(Hkv, d, rows):
+    step = wl.make_step("long rows", wl.Shape(Hkv, Hkv, d, 10), [5], [rows], [0], seed=2)
+    k, v = (torch.randn((rows, Hkv, d), generator=torch.Generator().manual_seed(i)).bfloat16() for i in (1, 2))
+    cache = _pool(step, Hkv, d, 3)
+    with Ctx(step, max_q_len=rows) as ctx:
+        dev, tail = torch.from_numpy(cache).cuda(), [step.page_table.cuda(), step.prefix_lens.cuda(), step.q_lens.cuda()]
+        fd.fd_kv_append_fp8(ctx.h, 1, rows, k.cuda(), v.cuda(), dev, step.num_pages, *tail)
+        ko, vo = torch.full_like(k, float("nan")).cuda(), torch.full_like(v, float("nan")).cuda()
+        fd.fd_kv_read_fp8(ctx.h, 1, rows, dev, step.num_pages, *tail, ko, vo)
+        assert fd.fd_last_device_status(ctx.h) == 0
+    # the prefix's rows are the pool's, of any scale, and set the first block's: what is held is the definition's, exactly
+    held = ref.values(*ref.split(ref.append(cache, d, step, k, v), d))
+    for got, which in ((ko, 0), (vo, 1)):
+        exp = np.stack([held[int(step.page_table[b, j // 16]), :, which, j % 16] for b, _, j in rows_of(step)])
+        np.testing.assert_array_equal(got.double().cpu().numpy(), exp)
 
 
 @pytest.mark.parametrize("path", PATHS)

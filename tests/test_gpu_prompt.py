@@ -212,6 +212,33 @@ def test_values_that_are_not_finite_in_a_shared_item(d):
 
 
 @pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("Lq,Lk", [(60, 5000), (9, 90), (300, 300)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_and_keys_that_are_not_finite(d, Lq, Lk, path):
+    """A query that is NaN, or infinite, makes its row NaN and no other, in whole items and in shared ones; a key that is NaN the rows that
+    see it."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    q = torch.randn((Lq, 4, d), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((Lk, 1, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    ctx = _ctx(4, 1, d, 1, path)
+    try:
+        clean = _call(ctx, q, k, v, [Lq], [Lk])
+        q2 = q.clone()
+        q2[3, 1], q2[5, 2, 7] = float("nan"), float("inf")      # (an infinite element: scores of both signs' infinities, inf - inf)
+        got = _call(ctx, q2, k, v, [Lq], [Lk])
+        gone = torch.zeros((Lq, 4), dtype=torch.bool, device="cuda")
+        gone[3, 1] = gone[5, 2] = True
+        assert torch.isnan(got[gone]).all() and torch.equal(got[~gone], clean[~gone])
+        k2, row = k.clone(), Lq // 2
+        k2[Lk - Lq + row, 0, 1] = float("nan")
+        got = _call(ctx, q, k2, v, [Lq], [Lk])
+        assert torch.isnan(got[row:]).all() and torch.equal(got[:row], clean[:row])
+        assert fd.fd_last_device_status(ctx) == 0
+    finally:
+        fd.fd_destroy(ctx)
+
+
+@pytest.mark.parametrize("path", PATHS)
 @pytest.mark.parametrize("size,scale", [(3e4, 1e-6), (1e-4, 300.0), (1.0, 0.5)])
 def test_prompt_attention_scales(size, scale, path):
     q, k, v, ql, kl = _inputs("tile edges", False, seed=3)
