@@ -8,7 +8,7 @@
 //          entries: one launch, no CTA waits for another.  512 samples of 256 pages each 6.8 us, one sample 3.6.
 // free     which occurrence of a shared page releases it must not depend on timing, so it takes passes over the occurrences with
 //          barriers between them: count owners down, let a page without owners be claimed by its first occurrence, count the
-//          claims, write the list.  Few pages: one CTA, one launch, 4.5 us for 64.  Many: a launch for each pass, 19 us for 131 k
+//          claims, write the list.  Few pages: one CTA, one launch, 5.9 us for 64.  Many: a launch for each pass, 19 us for 131 k
 //          -- bound by the random words of `shared`, an atomic for each page owned and three reads (one cluster of eight CTAs, with its
 //          hardware barrier between the passes, took 98).
 // compact  mark, count and rank, list the moves: passes over the ids, a thread-block cluster with its barrier between them, since they
@@ -176,26 +176,28 @@ void launch_kv_fork(const ForkParams& p, cudaStream_t s) {
 // ------------------------------------------------------------------------------------------------ free
 // The occurrences of pages in the listed sequences, numbered e = 0 .. T - 1 (sequence by sequence, page by page); a warp takes a
 // contiguous run of them.
-constexpr int kFreeThreads = 512;
-// Entries up to which one CTA does it in one launch: 1024 take 6.5 us so and 11.5 in four launches, 4096 17.4 and 16.0, 8192 31.6 and 16.8.
-constexpr long long kFreeSmall = 7 * kFreeThreads;
+constexpr int kFreeThreads = 512, kFreeSmallThreads = 1024;  // (one CTA alone: more loads in flight)
+// Entries up to which one CTA does it in one launch; the table's width gives them, since the lengths are on the device, and sequences
+// mostly hold fewer.  64 pages take 5.9 us so and 9.5 in four launches, 1024 6.3 and 11.5, 4096 12.1 and 16.0, 8192 19.4 and 16.8.
+constexpr long long kFreeSmall = 8192;
 constexpr int kClaim = 0x40000000;  // a released page holds e - T - 1 - kClaim once occurrence e (of T) has claimed it: below any count
 
 struct FreeShared {
     int cu[kMaxBatch + 1];  // exclusive scan of the pages of the listed sequences
     unsigned seen[kMaxBatch / 32];
-    int wsum[kFreeThreads / 32];
+    int wsum[32];
 };
 
 // Checks and scan.  Returns whether the call is to be refused (the same in every thread).
+template <int THREADS>
 __device__ __forceinline__ bool free_scan(const FreeParams& p, FreeShared& sh, int n_free, int* T) {
     const int tid = threadIdx.x, N = p.n_seqs;
-    for (int i = tid; i < kMaxBatch / 32; i += kFreeThreads) sh.seen[i] = 0;
+    for (int i = tid; i < kMaxBatch / 32; i += THREADS) sh.seen[i] = 0;
     if (tid == 0) sh.cu[0] = 0;
     __syncthreads();
     bool bad = n_free < 0 || n_free > p.num_pages;
     long long total = 0;
-    for (int base = 0; base < N; base += kFreeThreads) {
+    for (int base = 0; base < N; base += THREADS) {
         const int i = base + tid;
         int pages = 0;
         if (i < N) {
@@ -209,10 +211,10 @@ __device__ __forceinline__ bool free_scan(const FreeParams& p, FreeShared& sh, i
                 if (atomicOr(&sh.seen[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u) bad = true;  // listed twice
             }
         }
-        if (pages > 0x1fffff) bad = true;  // (512 of them must not pass 32 bits)
+        if (pages > 0x1fffff) bad = true;  // (1024 of them must not pass 32 bits)
         pages = min(pages, 0x1fffff);
         int sum;
-        const int before = block_scan<kFreeThreads>(pages, sh.wsum, &sum);
+        const int before = block_scan<THREADS>(pages, sh.wsum, &sum);
         if (i < N) sh.cu[i + 1] = (int)min(total + before + pages, 0x3fffffffLL);
         total += sum;
     }
@@ -300,28 +302,28 @@ __device__ __forceinline__ void run_of(int warp, int warps, int T, int* lo, int*
 }
 
 // Few pages: one CTA, one launch.
-__global__ void __launch_bounds__(kFreeThreads) free_small_kernel(FreeParams p) {
+__global__ void __launch_bounds__(kFreeSmallThreads) free_small_kernel(FreeParams p) {
     __shared__ FreeShared sh;
     const int tid = threadIdx.x, warp = tid >> 5, n_free = *p.n_free;
     int T, lo, hi, all;
-    if (free_scan(p, sh, n_free, &T)) {
+    if (free_scan<kFreeSmallThreads>(p, sh, n_free, &T)) {
         if (tid == 0) {
             atomicOr(p.status, FD_DEV_BAD_LENGTHS);
             *p.n_free_out = n_free;
         }
         return;
     }
-    run_of(warp, kFreeThreads / 32, T, &lo, &hi);
+    run_of(warp, kFreeSmallThreads / 32, T, &lo, &hi);
     bool bad_page = free_count_down(p, sh, lo, hi);
     __syncthreads();
     free_claim(p, sh, T, lo, hi);
     __syncthreads();
     const int mine = free_claims(p, sh, T, lo, hi);
-    const int before = block_scan<kFreeThreads>((tid & 31) == 0 ? mine : 0, sh.wsum, &all);
+    const int before = block_scan<kFreeSmallThreads>((tid & 31) == 0 ? mine : 0, sh.wsum, &all);
     // the warps behind this one push first: the run ends where theirs and its own have been pushed
     bad_page |= free_push(p, sh, T, lo, hi, n_free + all - __shfl_sync(0xffffffffu, before, 0));
     if (bad_page) atomicOr(p.status, FD_DEV_BAD_PAGE);
-    for (int i = tid; i < p.n_seqs; i += kFreeThreads) p.prefix_lens[p.seqs[i]] = 0;
+    for (int i = tid; i < p.n_seqs; i += kFreeSmallThreads) p.prefix_lens[p.seqs[i]] = 0;
     if (tid == 0) *p.n_free_out = min(n_free + all, p.num_pages);
 }
 
@@ -335,7 +337,7 @@ __global__ void __launch_bounds__(kFreeThreads) free_pass_kernel(FreeParams p) {
     bool bad;
     if (PASS == 0) {
         n_free = *p.n_free;
-        bad = free_scan(p, sh, n_free, &T);
+        bad = free_scan<kFreeThreads>(p, sh, n_free, &T);
         if (blockIdx.x == 0) {
             for (int i = tid; i <= N; i += kFreeThreads) p.scratch->cu[i] = sh.cu[i];
             if (tid == 0) {
@@ -387,7 +389,7 @@ int launch_kv_free(const FreeParams& p, cudaStream_t s) {
     // (the lengths are on the device: the table's width bounds what a sequence holds)
     const long long most = (long long)p.n_seqs * p.max_pages;
     if (most <= kFreeSmall) {
-        free_small_kernel<<<1, kFreeThreads, 0, s>>>(p);
+        free_small_kernel<<<1, kFreeSmallThreads, 0, s>>>(p);
         return 1;
     }
     const int grid = (int)std::min<long long>((most + 4 * kFreeThreads - 1) / (4 * kFreeThreads), std::min(p.n_sms, 1024));
