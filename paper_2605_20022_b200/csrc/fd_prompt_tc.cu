@@ -24,12 +24,13 @@
 // one SM read what all had written, 54 us, and the code for it cost the softmax warps registers: 3 to 5 % on every other call.)
 //
 // What it reaches (32 heads over 8 of 128): a prompt of 32768 tokens 7.8 to 8.1 ms, 1.03 to 1.08 PFLOP/s where the library's dense product
-// sustains 1.18 to 1.29 on the same machine; 8192 tokens 0.97 to 1.02 PFLOP/s, 2048 0.75, 16 ragged prompts of 1 to 8192 tokens 600
-// to 650 us, 17 tokens 8.4 us.  What bounds it: a tile and stream takes 940 clocks on average where its products take 640; with
-// two streams the tensor pipe waits for the exponentials (half of a scheduler's cycles) and the hand-overs between them; short prompts wait
-// besides for an item's ends (Q's load, the epilogue) that nothing overlaps.
-// Tried and dropped: the streams' exponentials taking turns (no gain); one pass over S against a guessed maximum (spills: 8192 tokens
-// 860 us for 584); tiles of 96 keys at d = 64 (472 us for 406).
+// sustains 1.18 to 1.29 on the same machine; 8192 tokens 0.97 to 1.02 PFLOP/s, 2048 0.75, 16 ragged prompts of 100 to 4000 tokens 600
+// to 650 us, 17 tokens 8.4 us.  What bounds it: 128 keys of a stream take 1880 clocks of a SM, in which the tensor pipe and the exponential
+// unit are busy for 1024 each; in the rest both wait for hand-overs between a stream's softmax and its products, which two streams
+// cover in part.  Short prompts wait besides for an item's ends (Q's load, the epilogue) that nothing overlaps.
+// Tried and dropped (PFLOP/s at 32768 tokens, this form 1.05): a quarter of the exponentials by a polynomial on the FMA pipe 1.03, half of
+// them 0.99; the next row of S loaded in front of P's stores 0.97; the streams' exponentials taking turns, no gain; one pass over S
+// against a guessed maximum (spills: 8192 tokens 860 us for 584); at d = 64 tiles of 96 keys (472 us for 406).
 //
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
 // given back, FD_DEV_TIMEOUT is set.
