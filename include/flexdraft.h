@@ -453,7 +453,8 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, con
  * fd_attn_draft_verify_fp8 is fd_attn_draft_verify_blocks for it: same arguments (n_blocks may be NULL), same mask, same
  * errors, same forms (FD_TC_*), pinned plans and overlap of consecutive attention calls included.  Slots no valid token owns may
  * hold any bit pattern.  Arithmetic: the values of the cache enter exactly, elements of q exactly down to 2^-9 of their row's
- * largest (below that to within 2^-17 of it), the softmax weights as in fd_attn_draft_verify_fp4, sums in fp32; bf16 output.
+ * largest (below that to within 2^-17 of it), the softmax weights as in fd_attn_draft_verify_fp4, sums in fp32; bf16 output.  A row
+ * of q that holds a NaN or an infinity becomes NaN.
  * When to choose it: it holds twice the tokens in the same memory at four significant bits.  Its attention is faster than the bf16
  * cache's on long prefixes (32k, batch 16: 320 us against 350), slower on small ones (64 sequences of 1k to 4k: 133 us against
  * 116; 8 sequences: 49 against 38; one: 13 against 11).

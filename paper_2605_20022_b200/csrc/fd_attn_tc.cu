@@ -580,7 +580,8 @@ __device__ __forceinline__ bool q_to_e4m3(unsigned char* sq, float* row_scale, f
         unsigned char* at = sq + r * D + ((c ^ (D == 128 ? r & 7 : (r & 7) >> 1)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + kMaxRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        if (c == 0) row_scale[r] = fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);  // (as in q_to_half)
+        // (as in q_to_half; a row with an infinity or a NaN: NaN, since e4m3 has no infinity to hold)
+        if (c == 0) row_scale[r] = e == 255 ? __uint_as_float(0x7fffffffu) : fminf(fmaxf(scale_log2e * exp2f((float)(e - 134)), 1.17549435e-38f), 3.4028234e38f);
     };
     if (D == 128) {
 #pragma unroll 1
@@ -1445,7 +1446,10 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Bars* bars, fl
                 const float m1 = ex[r], l1 = ex[kMaxRows + r];
                 mm = f4->ref[w.piece & 1][r];
                 f4->ref[(w.piece + 1) & 1][r] = -INFINITY;  // (the next piece's: the one before this has long been read)
-                L = (m == -INFINITY ? 0.f : exp2f(m - mm) * l) + (pc.nt < 2 || m1 == -INFINITY ? 0.f : exp2f(m1 - mm) * l1);
+                // (8 bits: a row whose scores are all NaN has kept m at -inf and has NaN in l; it goes on as a part that was seen)
+                const float none = FMT == FD_KV_FP8 ? l : 0.f, none1 = FMT == FD_KV_FP8 ? l1 : 0.f;
+                L = (m == -INFINITY ? none : exp2f(m - mm) * l) + (pc.nt < 2 ? 0.f : m1 == -INFINITY ? none1 : exp2f(m1 - mm) * l1);
+                if (FMT == FD_KV_FP8 && L != L) mm = 0.f;
                 a0 = 1.f;
             } else {
                 const float m1 = two ? ex[r] : -INFINITY, l1 = ex[kMaxRows + r];

@@ -279,6 +279,41 @@ def test_attention_queries_of_any_size(path, size, scale):
     check(got, attn_ref(step, q, cache, scale=scale or None), "sizes")
 
 
+def _quick_cache(kv):
+    """ref.make_cache of large caches: the same bytes, by torch's conversion."""
+    x = kv.cuda().float().permute(0, 2, 1, 3, 4)
+    live = (x.abs() < 1e20).all(-1, keepdim=True)
+    x = torch.where(live, x, 0.0)
+    amax = x.abs().amax((-1, -2))
+    m, e = torch.frexp(amax / 448)
+    e = torch.where(amax > 0, e - (m == 0.5).int(), -15).clamp(-15, 7)
+    power = lambda n: ((n + 127) << 23).int().view(torch.float32)  # noqa: E731
+    codes = (x * power(-e)[..., None, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    scale = power(e)[..., None]
+    tail = torch.cat([scale, torch.zeros(scale.shape[:-1] + (3,), device="cuda")], -1).view(torch.uint8)
+    return torch.cat([codes.flatten(-2), tail], -1)
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 128), (8, 4, 64)])
+@pytest.mark.parametrize("pl,ql", [([300, 40], [12, 32]), ([40000], [8]), ([5000] * 40, [6] * 40)])
+def test_attention_queries_that_are_not_finite(pl, ql, Hq, Hkv, d, path):
+    """A query that is NaN or infinite makes its own row NaN, in sequences that one CTA works on and in those that several share."""
+    step = wl.make_step("not finite", wl.Shape(Hq, Hkv, d, 1000), pl, ql, [2] * len(pl), seed=12)
+    q, kv = wl.make_q(step), wl.make_kv(step)
+    cache = _quick_cache(kv)
+    if len(pl) == 2:
+        assert torch.equal(cache, torch.from_numpy(ref.make_cache(kv)).cuda())
+    gone = torch.zeros(q.shape[:2], dtype=torch.bool)
+    gone[3, 1] = gone[5, 2] = gone[7, 0] = True
+    with Ctx(step, path) as ctx:
+        clean, _ = attn_gpu(ctx, step, q, cache)
+        q[3, 1, 7], q[5, 2], q[7, 0, 3] = float("nan"), float("nan"), -float("inf")
+        got, status = attn_gpu(ctx, step, q, cache)
+    assert status == 0 and np.isnan(got[gone.numpy()]).all()
+    np.testing.assert_array_equal(got[~gone.numpy()], clean[~gone.numpy()])
+
+
 @pytest.mark.parametrize("pin", [False, True])
 @pytest.mark.parametrize("path", PATHS)
 def test_captured_call_forgets_the_bad_page_of_an_earlier_replay(path, pin):
