@@ -7,8 +7,9 @@
 // nothing is ordered by timing.  Read: 16 codes a thread.
 // Both: a CTA takes a run of pages (rows) whose sequences and page ids it looks up first, a thread each.
 // 24 prompts of 8 heads of 64 (20 k rows) take 13.5 us to append and 14.7 to read back, replayed from a graph (9.6 us of bytes each):
-// the loads' latency with the warps that registers leave resident.  A few rows (64 sequences, 1-16 each): 7.0 and 4.4, a chain of
-// lengths, scan, page table, block.
+// two thirds of the time is bytes, the rest launch, scan and look-ups.  (Dropped: five or six CTAs an SM for the append 15.6 and 17.0 us; four
+// loads in flight a thread for the read 16.2.)  A few rows (64 sequences, 1-16 each): 7.0 and 4.4, a chain of lengths, scan, page
+// table, block.
 #include <algorithm>
 
 #include "fd_fp8.cuh"
