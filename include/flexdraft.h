@@ -304,8 +304,8 @@ fd_status fd_attn_draft_verify_blocks(fd_ctx* ctx, int batch, int total_q_rows,
  * Pages for the query blocks of a step, and where each of its rows goes: the counterpart of fd_kv_commit, which
  * releases pages.  (The paper describes no page management; the bookkeeping implemented here mirrors the commit's.)
  * The free list is a stack of page ids, free_pages[0 .. n_free).  First the n_freed ids the last commit released
- * are pushed onto it (freed_pages / n_freed exactly as fd_kv_commit wrote them; both NULL: nothing to push).  Then,
- * for b ascending:
+ * are pushed onto it (freed_pages / n_freed exactly as fd_kv_commit wrote them; both NULL: nothing to push; batch 0:
+ * nothing but that, which fd_kv_fork and fd_kv_compact ask for).  Then, for b ascending:
  *
  *     for p = ceil(n_b / P) .. ceil((n_b + Lq_b) / P) - 1 ascending:
  *         page_table[b][p] = the id popped from the top of the free list
@@ -509,7 +509,15 @@ fd_status fd_attn_prompt(fd_ctx* ctx, int batch, int total_q_rows, int total_kv_
  *   free_pages, n_free, n_free_out   the free list, as in fd_kv_reserve (n_free_out may be n_free itself)
  *   num_pages * P < 2^31
  *
- * Call them between steps (behind fd_kv_commit): pages reserved for a query block that has not been committed are not looked at.
+ * Call them between steps, behind fd_kv_commit: fork and free do not look at pages reserved for a query block that has not been
+ * committed.  The ids that the commit released have to be on the free list by then.  fd_kv_compact takes every id that is not on it
+ * for a page in use and gives it another number, so that a commit's ids pushed behind it would be on the list twice and two sequences
+ * would write the same page; fd_kv_fork finds pages on the list only.  A reservation for no sequence pushes them (and the next
+ * reservation then gets none of them):
+ *
+ *     fd_kv_reserve(ctx, 0, 0, NULL, NULL, NULL, NULL, NULL, freed_pages, n_freed, free_pages, n_free, n_free, num_pages, NULL, NULL, stream)
+ *
+ * Whatever else holds ids outside of page_table and the list while fd_kv_compact runs has to replace them by page_map[id].
  *
  * fd_kv_fork: child children[i] becomes a copy of parents[i], for i ascending.  With n = prefix_lens[parent], f = floor(n / P):
  *
