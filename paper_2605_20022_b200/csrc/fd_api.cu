@@ -873,13 +873,14 @@ fd_status fd_attn_prompt(fd_ctx* c, int batch, int total_q_rows, int total_kv_ro
     const bool tc = c->attn_path == FD_ATTN_TCGEN05 && total_q_rows > 0;
     if (tc && fd::prompt_tc_prepare(&c->prompt_state, p) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
     if (!tc || !fd::prompt_tc_plans_itself(batch)) {
-        fd::launch_prompt_plan(p, s);
+        if (fd::launch_prompt_plan(p, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
         c->launches += 1;
     }
     if (tc) {
         int launched = 0;
-        if (fd::launch_prompt_tc(c->prompt_state, p, &launched, s) != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
+        const cudaError_t e = fd::launch_prompt_tc(c->prompt_state, p, &launched, s);
         c->launches += launched;
+        if (e != cudaSuccess) { cudaGetLastError(); return FD_ERR_CUDA; }
     } else if (total_q_rows > 0) {  // (no rows: the plan alone checks the lengths)
         fd::launch_prompt_simt(p, s);
         c->launches += 1;

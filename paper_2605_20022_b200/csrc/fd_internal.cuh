@@ -289,6 +289,18 @@ __device__ inline void merge_row(const AttnParams& p, const CtaStarts& cs, int c
 // itself (few row blocks); or one cluster per segment, merged through distributed shared memory.
 enum { kTcPlanned = 0, kTcSelfPlanned = 1, kTcCluster = 2 };
 
+// A launch whose refusal is known at once (<<<>>> leaves it to the next look at the last error, which may be an older one): where
+// kernels read what this one writes, none of them follows then.
+template <class... Params, class... Args>
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Launchers (defined next to their kernels).
 void launch_plan(const AttnParams& p, cudaStream_t s);
 cudaError_t attn_simt_prepare(int d);
@@ -459,7 +471,7 @@ struct FreeParams {
     int n_sms;
     int* status;
 };
-int launch_kv_free(const FreeParams& p, cudaStream_t s);  // returns the number of kernels launched
+int launch_kv_free(const FreeParams& p, cudaStream_t s);  // returns the number of kernels launched (a refused one is the last)
 
 struct CompactParams {
     int batch, num_pages, max_pages, max_copies;
@@ -475,7 +487,7 @@ struct CompactParams {
     int n_sms;
     int* status;
 };
-int launch_kv_compact(const CompactParams& p, cudaStream_t s);  // returns the number of kernels launched
+int launch_kv_compact(const CompactParams& p, cudaStream_t s);  // returns the number of kernels launched (a refused one is the last)
 
 struct CopyPagesParams {
     int max_copies, num_pages;

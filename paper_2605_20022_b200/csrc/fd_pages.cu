@@ -393,18 +393,19 @@ int launch_kv_free(const FreeParams& p, cudaStream_t s) {
         return 1;
     }
     const int grid = (int)std::min<long long>((most + 4 * kFreeThreads - 1) / (4 * kFreeThreads), std::min(p.n_sms, 1024));
-    free_pass_kernel<0><<<grid, kFreeThreads, 0, s>>>(p);
-    free_pass_kernel<1><<<grid, kFreeThreads, 0, s>>>(p);
-    free_pass_kernel<2><<<grid, kFreeThreads, 0, s>>>(p);
-    free_pass_kernel<3><<<grid, kFreeThreads, 0, s>>>(p);
-    return 4;
+    int n = 0;
+    for (auto pass : {free_pass_kernel<0>, free_pass_kernel<1>, free_pass_kernel<2>, free_pass_kernel<3>}) {
+        if (launch(pass, grid, kFreeThreads, 0, s, p) != cudaSuccess) break;
+        ++n;
+    }
+    return n;
 }
 
 // ------------------------------------------------------------------------------------------------ compact
 constexpr int kClusterThreads = 1024, kMaxPageCluster = 8;
 
 template <class K, class P>
-static void launch_cluster(K kernel, const P& p, int ctas, cudaStream_t s) {
+static cudaError_t launch_cluster(K kernel, const P& p, int ctas, cudaStream_t s) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -414,7 +415,7 @@ static void launch_cluster(K kernel, const P& p, int ctas, cudaStream_t s) {
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, p);
+    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 __global__ void __launch_bounds__(kClusterThreads) compact_kernel(CompactParams p) {
@@ -511,10 +512,10 @@ __global__ void __launch_bounds__(256) rename_kernel(CompactParams p) {
 }
 
 int launch_kv_compact(const CompactParams& p, cudaStream_t s) {
-    launch_cluster(compact_kernel, p, p.num_pages <= 2 * kClusterThreads ? 1 : kMaxPageCluster, s);
+    if (launch_cluster(compact_kernel, p, p.num_pages <= 2 * kClusterThreads ? 1 : kMaxPageCluster, s) != cudaSuccess) return 0;
     const long long work = (std::max<long long>((long long)p.batch * p.max_pages, p.num_pages) + 1023) / 1024;
-    rename_kernel<<<(int)std::max(1LL, std::min<long long>(work, 4LL * p.n_sms)), 256, 0, s>>>(p);
-    return 2;
+    const int grid = (int)std::max(1LL, std::min<long long>(work, 4LL * p.n_sms));
+    return launch(rename_kernel, grid, 256, 0, s, p) == cudaSuccess ? 2 : 1;
 }
 
 // ------------------------------------------------------------------------------------------------ copy

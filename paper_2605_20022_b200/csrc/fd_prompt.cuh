@@ -88,7 +88,7 @@ struct PromptParams {
     int* status;
 };
 
-void launch_prompt_plan(const PromptParams& p, cudaStream_t s);
+cudaError_t launch_prompt_plan(const PromptParams& p, cudaStream_t s);
 cudaError_t prompt_simt_prepare(int d);
 void launch_prompt_simt(const PromptParams& p, cudaStream_t s);
 cudaError_t prompt_tc_prepare(void** state, const PromptParams& p);

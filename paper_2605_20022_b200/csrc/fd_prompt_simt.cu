@@ -81,10 +81,10 @@ __global__ void __launch_bounds__(kPlanThreads) prompt_plan_kernel(PromptParams 
     }
 }
 
-void launch_prompt_plan(const PromptParams& p, cudaStream_t s) {
+cudaError_t launch_prompt_plan(const PromptParams& p, cudaStream_t s) {
     int n = 1;
     while (n < p.batch) n <<= 1;
-    prompt_plan_kernel<<<1, kPlanThreads, 0, s>>>(p, n);
+    return launch(prompt_plan_kernel, 1, kPlanThreads, 0, s, p, n);
 }
 
 // One thread a query row; K and V pass through shared memory 16 keys at a time; the online softmax in the log2 domain.

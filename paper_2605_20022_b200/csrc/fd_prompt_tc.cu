@@ -790,16 +790,15 @@ cudaError_t launch_prompt_tc(void* state, const PromptParams& p, int* launched, 
     const long long blocks = (p.total_q + 2LL * p.tile_tokens - 1) / (2 * p.tile_tokens);
     const bool may_split = 2 * blocks * p.Hkv <= p.n_ctas && p.total_kv >= kMinSplitTiles * PCfg<128>::kKeys;
     if (!may_split) a.split = nullptr;
-    if (p.d == 64) prompt_tc_kernel<64><<<p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s>>>(q, k, v, a);
-    else prompt_tc_kernel<128><<<p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s>>>(q, k, v, a);
-    *launched = 1;
-    if (may_split) {
+    cudaError_t e = p.d == 64 ? launch(prompt_tc_kernel<64>, p.n_ctas, kPThreads, PCfg<64>::kSmemBytes, s, q, k, v, a)
+                              : launch(prompt_tc_kernel<128>, p.n_ctas, kPThreads, PCfg<128>::kSmemBytes, s, q, k, v, a);
+    *launched = e == cudaSuccess;
+    if (may_split && e == cudaSuccess) {
         const dim3 grid(p.n_ctas / 2 * 2, p.d / 16);
-        if (p.d == 64) prompt_merge_kernel<64><<<grid, kMaxRows, 0, s>>>(a);
-        else prompt_merge_kernel<128><<<grid, kMaxRows, 0, s>>>(a);
-        *launched = 2;
+        e = launch(p.d == 64 ? prompt_merge_kernel<64> : prompt_merge_kernel<128>, grid, kMaxRows, 0, s, a);
+        *launched += e == cudaSuccess;
     }
-    return cudaSuccess;
+    return e;
 }
 
 void prompt_tc_free(void* state) { delete static_cast<PromptState*>(state); }
