@@ -268,7 +268,8 @@ fd_status fd_plan_ranges_host(int batch, int n_kv_heads, const int32_t* prefix_l
  *   page_table     device, [B, max_pages_per_seq] int32: pages for positions up to n_b + Lq_b - 1 must be allocated
  *   prefix_lens, q_lens   device, [B] int32
  *
- * A sequence whose rows would pass T or the page table is skipped (FD_DEV_BAD_LENGTHS); a slot whose page
+ * A sequence whose rows would pass T or the page table, or whose block is longer than max_q_len, is skipped
+ * (FD_DEV_BAD_LENGTHS; append a longer one in pieces, n_b growing by what has been appended); a slot whose page
  * id is outside the pool is skipped (FD_DEV_BAD_PAGE).
  */
 fd_status fd_kv_append(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
@@ -446,7 +447,7 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, con
  * fd_kv_append_fp8 is fd_kv_append for it, fd_kv_read_fp8 the reverse: k_out / v_out [T, Hkv, d] bf16 get the values held
  * at positions n_b .. n_b + Lq_b - 1 (any range of the sequence: pass the range's start as prefix_lens), exactly.  Lq_b is not
  * bounded by max_q_len in either.  A sequence that is skipped, or a slot whose page id is outside the pool, leaves its rows of
- * k_out / v_out as zeros.  Arguments and device-detected errors are fd_kv_append's.  A page that two sequences of a call name is
+ * k_out / v_out as zeros.  Arguments and device-detected errors are otherwise fd_kv_append's.  A page that two sequences of a call name is
  * written by both: let each append to pages of its own, as fd_kv_reserve and fd_kv_fork hand out.  Neither call overlaps the
  * calls around it: under a pinned plan the attention call behind one starts when it has completed.
  *

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendParams p, int rows
     }
     __syncthreads();
     const long long row0 = s_row0;
-    if (n < 0 || row0 + Lq > p.total_rows || (long long)n + Lq > (long long)p.max_pages * 16) {
+    if (n < 0 || Lq > p.max_q_len || row0 + Lq > p.total_rows || (long long)n + Lq > (long long)p.max_pages * 16) {
         if (p.chained) asm volatile("griddepcontrol.wait;" ::: "memory");  // (before the write to the status word, too)
         if (tid == 0 && i0 == 0) atomicOr(p.status, FD_DEV_BAD_LENGTHS);
         return;
