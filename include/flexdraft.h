@@ -322,7 +322,8 @@ fd_status fd_attn_draft_verify_blocks(fd_ctx* ctx, int batch, int total_q_rows,
  *
  *   total_q_rows    T; must equal sum_b q_lens[b]
  *   page_table      device, [B, max_pages_per_seq] int32, in/out
- *   prefix_lens, q_lens, n_mask   device, [B] int32;  n_blocks   device, [B] int32 or NULL (one block each)
+ *   prefix_lens, q_lens, n_mask   device, [B] int32;  n_blocks   device, [B] int32 or NULL (one block each).  A block without
+ *                   mask tokens (a prompt) may be longer than max_q_len
  *   freed_pages     device, int32, read only;  n_freed   device, [1] int32
  *   free_pages      device, [num_pages] int32, in/out
  *   n_free          device, [1] int32: ids on the free list before the call
@@ -353,7 +354,7 @@ fd_status fd_kv_reserve(fd_ctx* ctx, int batch, int total_q_rows, int32_t* page_
  *
  * with pos = positions[t].  q goes to q_out[t]; k and v go to the cache slot slot_map[t] (page slot / P, token slot % P).
  *
- *   total_q_rows    T >= 0; at most max_batch * max_q_len
+ *   total_q_rows    T >= 0; at most max_batch * max_q_len, any number with FD_KV_ROWS
  *   qkv             device, bf16, 16-byte aligned; row t starts at element t * row_stride (a multiple of 8, at least
  *                   (Hq + 2 Hkv) * d)
  *   q_weight, k_weight   device, [d] bf16, 16-byte aligned, or NULL: no norm
@@ -491,6 +492,12 @@ fd_status fd_attn_draft_verify_fp8(fd_ctx* ctx, int batch, int total_q_rows, con
  *
  * Inconsistent lengths zero all T rows (FD_DEV_BAD_LENGTHS).  What a row must not see -- another sequence, a later position --
  * never reaches it, infinities and NaN included.
+ *
+ * A prompt's way into a cache, whatever max_q_len: fd_kv_reserve, fd_qk_norm_rope_append with FD_KV_ROWS, this call,
+ * fd_kv_append_fp8 or fd_kv_append_fp4 (into bf16 pages fd_kv_append, in pieces of max_q_len rows), and fd_kv_commit with
+ * accepted_len[b] = Lq_b - 1.  A chunk behind earlier keys takes all of them as rows: fd_kv_read_fp8 and fd_kv_read_fp4 bring them out
+ * of pages.  Over pages as they are -- bf16 ones have no such call -- fd_attn_draft_verify and its 4-bit and 8-bit forms are causal
+ * attention too where n_mask is 0, for chunks of up to max_q_len rows that have been appended.
  * Arithmetic: bf16 inputs, fp32 scores / softmax / accumulation, softmax weights rounded to bf16 in front of the product with v,
  * bf16 output.
  */
@@ -682,7 +689,8 @@ fd_status fd_verify_accept_sample(fd_ctx* ctx, int batch, int total_cand_rows, c
  *   page_table    device, [B, max_pages_per_seq] int32, in/out
  *   prefix_lens   device, [B] int32, in/out
  *   q_lens, accepted_len   device, [B] int32
- *   freed_pages   device, int32, capacity >= B * (ceil(max_q_len / P) + 1), packed output
+ *   freed_pages   device, int32, packed output; capacity >= B * (ceil(max_q_len / P) + 1), or, where a block is longer than
+ *                 max_q_len, sum_b (ceil(Lq_b / P) + 1)
  *   n_freed       device, [1] int32, output
  */
 fd_status fd_kv_commit(fd_ctx* ctx, int batch, int32_t* page_table, int32_t* prefix_lens,

@@ -697,7 +697,7 @@ fd_status fd_kv_reserve(fd_ctx* c, int batch, int total_q_rows, int32_t* page_ta
                         const int32_t* n_freed, int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out,
                         int num_pages, int32_t* slot_map, int32_t* positions, void* stream) {
     if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
-    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || total_q_rows > c->max_rows || num_pages < 1) return FD_ERR_INVALID_ARG;
+    if (!c || batch < 0 || batch > c->cfg.max_batch || total_q_rows < 0 || num_pages < 1) return FD_ERR_INVALID_ARG;
     if (!free_pages || !n_free || !n_free_out || (freed_pages == nullptr) != (n_freed == nullptr)) return FD_ERR_INVALID_ARG;
     if (batch == 0 && total_q_rows > 0) return FD_ERR_INVALID_ARG;
     if (batch > 0 && (!page_table || !prefix_lens || !q_lens || !n_mask)) return FD_ERR_INVALID_ARG;
@@ -719,7 +719,8 @@ fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, i
                                  int rope_style, const int32_t* positions, const int32_t* slot_map, void* q_out,
                                  void* kv_cache, int num_pages, int kv_format, float k_scale, float v_scale, void* stream) {
     if (c) { c->pin_chain = false; c->after_attn = false; }  // (not an attention or append call)
-    if (!c || total_q_rows < 0 || total_q_rows > c->max_rows || num_pages < 0 || !(eps >= 0.f)) return FD_ERR_INVALID_ARG;
+    if (!c || total_q_rows < 0 || num_pages < 0 || !(eps >= 0.f)) return FD_ERR_INVALID_ARG;
+    if (kv_format != FD_KV_ROWS && total_q_rows > c->max_rows) return FD_ERR_INVALID_ARG;  // (rows: prompts of any length)
     if (kv_format != FD_KV_BF16 && kv_format != FD_KV_FP4 && kv_format != FD_KV_ROWS) return FD_ERR_INVALID_ARG;
     if (rope_style != FD_ROPE_HALVES && rope_style != FD_ROPE_ADJACENT) return FD_ERR_INVALID_ARG;
     const int d = c->cfg.head_dim, heads = c->cfg.n_q_heads + 2 * c->cfg.n_kv_heads;

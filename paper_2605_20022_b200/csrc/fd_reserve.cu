@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(ReserveParams p) {
         long long r = 0, w = 0;
         if (b < B) {
             const long long n = p.prefix_lens[b], L = p.q_lens[b], M = p.n_mask[b], nb = p.n_blocks ? p.n_blocks[b] : 1;
-            if (n < 0 || L < 0 || M < 0 || M > L || L > p.max_q_len || n + L > (long long)p.max_pages * 16 || nb < 0 ||
+            if (n < 0 || L < 0 || M < 0 || M > L || (M > 0 && L > p.max_q_len) || n + L > (long long)p.max_pages * 16 || nb < 0 ||
                 (nb > 1 && (M % nb != 0 || nb > L - M))) {
                 bad = true;
             } else {
