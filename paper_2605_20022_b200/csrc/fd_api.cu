@@ -745,14 +745,9 @@ fd_status fd_qk_norm_rope_append(fd_ctx* c, int total_q_rows, const void* qkv, i
     p.eps = eps; p.cos_sin = cos_sin; p.max_positions = max_positions; p.rot_dim = rot_dim; p.adjacent = rope_style == FD_ROPE_ADJACENT;
     p.positions = positions; p.slot_map = slot_map;
     p.q_out = static_cast<__nv_bfloat16*>(q_out);
+    p.fmt = kv_format;
     if (kv_format == FD_KV_FP4) p.kv4 = static_cast<unsigned char*>(kv_cache);
     else p.kv = static_cast<__nv_bfloat16*>(kv_cache);
-    const long long row = (long long)c->cfg.n_kv_heads * d;
-    if (kv_format == FD_KV_ROWS) {
-        p.page_step = 16 * row; p.tok_step = row; p.head_step = d; p.v_step = num_pages * 16LL * row;
-    } else {
-        p.page_step = 32 * row; p.tok_step = d; p.head_step = 16 * d; p.v_step = 16 * row;
-    }
     p.k_scale = k_scale; p.v_scale = v_scale; p.n_sms = c->n_sms; p.status = c->status;
     fd::launch_norm_rope(p, static_cast<cudaStream_t>(stream));
     c->launches += 1;

@@ -513,11 +513,10 @@ struct NormRopeParams {
     const int32_t* positions;
     const int32_t* slot_map;
     __nv_bfloat16* q_out;
-    __nv_bfloat16* kv;        // the cache, or rows, in bf16: where slot (page, token) of K of kv-head h starts is
-    long long page_step, tok_step, head_step, v_step;  //    page * page_step + token * tok_step + h * head_step, V's v_step behind
+    __nv_bfloat16* kv;        // the cache, or rows, in bf16
     unsigned char* kv4;       // or the 4-bit cache
     float k_scale, v_scale;
-    int n_sms;
+    int n_sms, fmt;           // fmt: FD_KV_*, what k and v go to
     int* status;
 };
 void launch_norm_rope(const NormRopeParams& p, cudaStream_t s);
