@@ -729,7 +729,6 @@ struct PromptState {
     static constexpr int kSlots = 256;  // layers x (q, k, v) of a model, give or take
     PFN_cuTensorMapEncodeTiled_v12000 encode;
     PromptMap slots[kSlots];
-    const CUtensorMap *q, *k, *v;
 };
 
 }  // namespace
