@@ -8,7 +8,7 @@
 //          entries: one launch, no CTA waits for another.  512 samples of 256 pages each 6.8 us, one sample 3.6.
 // free     which occurrence of a shared page releases it must not depend on timing, so it takes passes over the occurrences with
 //          barriers between them: count owners down, let a page without owners be claimed by its first occurrence, count the
-//          claims, write the list.  Few pages: one CTA, one launch, 5.9 us for 64.  Many: a launch for each pass, 19 us for 131 k
+//          claims, write the list.  Few pages: one CTA, one launch, 7 us for 64.  Many: a launch for each pass, 19 us for 131 k
 //          -- bound by the random words of `shared`, an atomic for each page owned and three reads (one cluster of eight CTAs, with its
 //          hardware barrier between the passes, took 98).
 // compact  mark, count and rank, list the moves: passes over the ids, a thread-block cluster with its barrier between them, since they
@@ -177,9 +177,12 @@ void launch_kv_fork(const ForkParams& p, cudaStream_t s) {
 // The occurrences of pages in the listed sequences, numbered e = 0 .. T - 1 (sequence by sequence, page by page); a warp takes a
 // contiguous run of them.
 constexpr int kFreeThreads = 512, kFreeSmallThreads = 1024;  // (one CTA alone: more loads in flight)
-// Entries up to which one CTA does it in one launch; the table's width gives them, since the lengths are on the device, and sequences
-// mostly hold fewer.  64 pages take 5.9 us so and 9.5 in four launches, 1024 6.3 and 11.5, 4096 12.1 and 16.0, 8192 19.4 and 16.8.
-constexpr long long kFreeSmall = 8192;
+// Entries of the listed sequences' rows up to which one CTA does it in one launch (the lengths are on the device: what the sequences hold
+// is not known here).  One CTA / four launches, random ids with one owner each, in a graph behind the copies that restore the books:
+// 64 pages held of 64 entries 7.0 / 11.5 us, 1024 of 1024 8.2 / 14.4, 2048 of 4096 14.1 / 17.1, 4096 of 4096 21.6 / 23.1;
+// 2048 of 8192 14.1 / 13.3, 4096 of 8192 22.1 / 18.1, 8192 of 8192 35.7 / 24.1.  (56 pages of 8 sequences with rows of 2048 entries take
+// four launches: 12.)
+constexpr long long kFreeSmall = 4096;
 constexpr int kClaim = 0x40000000;  // a released page holds e - T - 1 - kClaim once occurrence e (of T) has claimed it: below any count
 
 struct FreeShared {
