@@ -458,8 +458,8 @@ fd_status fd_attn_draft_verify_fp4(fd_ctx* ctx, int batch, int total_q_rows, con
  * largest (below that to within 2^-17 of it), the softmax weights as in fd_attn_draft_verify_fp4, sums in fp32; bf16 output.  A row
  * of q that holds a NaN or an infinity becomes NaN.
  * When to choose it: it holds twice the tokens in the same memory at four significant bits.  Its attention is faster than the bf16
- * cache's on long prefixes (32k, batch 16: 320 us against 350), slower on small ones (64 sequences of 1k to 4k: 131 us against
- * 116; 8 sequences: 48 against 38; one: 13 against 11).
+ * cache's on long prefixes (32k, batch 16: 319 us against 351 in short runs, 376 against 429 call after call for a second), about as fast for
+ * 64 sequences of 1k to 4k (127 against 116, 128 against 135) and slower for few (8 sequences: 43 against 38; one: 12.4 against 10.9).
  */
 fd_status fd_kv_append_fp8(fd_ctx* ctx, int batch, int total_q_rows, const void* k_new, const void* v_new,
                            void* kv_cache, int num_pages, const int32_t* page_table, const int32_t* prefix_lens,

@@ -65,7 +65,7 @@
 // memory, 394 / 95-115 us, but 155-183 us at up to 16 rows; two S buffers and two accumulators, as in the bf16 form, 344 / 159;
 // four widening warps 472 / 190; four for K and four for V, 431 / 187.
 //
-// The 8-bit form (d = 128): batch 16 on 32k 318 us (3.4 TB/s of cache), batch 64 131, batch 1 12.6.  Half
+// The 8-bit form (d = 128): batch 16 on 32k 319 us (3.4 TB/s of cache; 376 call after call, under the power cap), batch 64 127, batch 1 12.4.  Half
 // the widening is gone, and what bounds it is the same: hand-overs and, at a piece's ends, code that is not in the instruction
 // cache.  Measured on the way, batch 16 on 32k / batch 64: both widened as in 4 bits, K and V a bulk copy each 464 / 182; K as it is, one box a page
 // 335 / 173; eight widening warps 346 / 144; scales a tile ahead, Q by a rolled loop, one form of the widening 327 / 132.

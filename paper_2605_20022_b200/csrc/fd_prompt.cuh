@@ -2,12 +2,14 @@
 //
 // A row tile is 128 / G consecutive tokens of a sequence times the G q-heads of one kv-head, at most 128 rows (row r = token r / G,
 // head r % G): all of them read the same keys, whatever the ratio of heads.  A work item is a block of two neighbouring row tiles of
-// one kv-head.  Under the causal mask the cost of a block grows with its place in the sequence, so items are numbered from the last
-// place down: first all blocks at the highest place that any sequence has, then the place below, ...  With the sequences sorted by
+// one kv-head.  Under the causal mask the cost of a block of a whole prompt grows with its place in the sequence, so items are numbered from
+// the last place down: first all blocks at the highest place that any sequence has, then the place below, ...  With the sequences sorted by
 // their number of blocks, longest first, the blocks at places >= j number  S(r) - j r,  r the sequences that have more than j
 // blocks and S the prefix sums of their numbers: a binary search finds an item from B numbers, no list of items is kept.
-// CTA c of N takes items c, 2N - 1 - c, 2N + c, 4N - 1 - c, ...: the costs of a round fall steadily, and going back and forth
-// evens them out.
+// CTA c of N takes items c, 2N - 1 - c, 2N + c, 4N - 1 - c, ...: the costs of a round of whole prompts fall steadily, and going back and
+// forth evens them out.  Earlier keys (kv_lens) add to a block's cost and do not enter the order: where they differ much from sequence to
+// sequence the CTAs finish apart (16 chunks of 64 tokens at 8 kv-heads, one behind 30000 keys, the others behind 300: 427 us, the time of the one
+// sequence's 8 items, where an even share would be 25).
 #pragma once
 
 #include "fd_internal.cuh"

@@ -21,16 +21,19 @@
 // A call of few items (a short chunk behind a long prefix: 8 items for one of 64 tokens at 8 kv-heads) is split along the keys: `parts`
 // CTAs share an item, each takes an equal share of its tiles and leaves (m, l, O) in scratch memory, which a second kernel combines in
 // the order of the parts: 64 tokens behind 8128 take 25 us, where one CTA an item takes 125.  (Combined by the last CTA to deliver,
-// one SM read what all had written, 54 us, and the code for it cost the softmax warps registers: 3 to 5 % on every other call.)
+// one SM read what all had written, 54 us, and the code for it cost the softmax warps registers: 3 to 5 % on every other call.)  All items of
+// a call are shared among the same number of CTAs, or none: from more than half as many items as CTAs on, none is (behind 3584 keys,
+// 8 kv-heads: 512 tokens 48 us for a floor of 19, 640 74 for 25, 1200 121 for 50, 2048 154 for 93).
 //
-// What it reaches (32 heads over 8 of 128): a prompt of 32768 tokens 7.8 to 8.1 ms, 1.03 to 1.08 PFLOP/s where the library's dense product
-// sustains 1.18 to 1.29 on the same machine; 8192 tokens 0.97 to 1.02 PFLOP/s, 2048 0.75, 16 ragged prompts of 100 to 4000 tokens 600
-// to 650 us, 17 tokens 8.4 us.  What bounds it: 128 keys of a stream take 1880 clocks of a SM, in which the tensor pipe and the exponential
+// What it reaches (32 heads over 8 of 128), in runs of 10 ms / call after call for seconds, when the power cap lowers the clock: a prompt
+// of 32768 tokens 7.4 / 8.4 ms, 1.19 / 1.05 PFLOP/s, where the library's dense product of 8192 reaches 1.63 / 1.39 on the same machine;
+// 8192 tokens 486 / 556 us, 1.13 / 0.99; 2048 44 / 45 us, 0.78 / 0.76; 16 ragged prompts of 100 to 4000 tokens 612 / 712 us; 17 tokens 8.4
+// us.  What bounds it: 128 keys of a stream take 1880 clocks of a SM, in which the tensor pipe and the exponential
 // unit are busy for 1024 each; in the rest both wait for hand-overs between a stream's softmax and its products, which two streams
 // cover in part.  Short prompts wait besides for an item's ends (Q's load, the epilogue) that nothing overlaps.
-// Tried and dropped (PFLOP/s at 32768 tokens, this form 1.05): a quarter of the exponentials by a polynomial on the FMA pipe 1.03, half of
-// them 0.99; the next row of S loaded in front of P's stores 0.97; the streams' exponentials taking turns, no gain; one pass over S
-// against a guessed maximum (spills: 8192 tokens 860 us for 584); at d = 64 tiles of 96 keys (472 us for 406).
+// Tried and dropped (PFLOP/s at 32768 tokens, call after call, this form 1.05): a quarter of the exponentials by a polynomial on the FMA
+// pipe 1.03, half of them 0.99; the next row of S loaded in front of P's stores 0.97; the streams' exponentials taking turns, no gain; one
+// pass over S against a guessed maximum (spills: 8192 tokens 860 us, 584 without at that time); at d = 64 tiles of 96 keys (472 us for 406).
 //
 // Every wait is bounded: one that runs out raises a CTA-wide flag, the roles leave, copies in flight are drained, tensor memory is
 // given back, FD_DEV_TIMEOUT is set.
